@@ -365,6 +365,117 @@ int ftts_advance(int32_t* tokens, int32_t* positions, int32_t* seq_lens, int32_t
 int ftts_sample(const float* logits, int32_t B, int32_t V, const ftts_sampling* samp,
                 const float* uniforms, int32_t* sampled_out, void* stream);
 
+/* ---- serving a batch over the paged cache: tables, append, shared-prefix attention --------
+ *
+ * The serving engine keeps its requests in KV pages and batches them in flight (Sec. II-C);
+ * many of them speak in one voice, so their conditioning rows are the same.  The three calls
+ * below form one pass that is driven by lengths on the device and can be captured whole:
+ * ftts_build_tables turns request lengths into block tables and a slot per new token,
+ * ftts_append_kv writes those tokens' keys and values into their pages, and
+ * ftts_shared_attention lets every sequence attend to one shared prefix, cached once, and to
+ * its own tokens.  Heads are 64 wide and pages hold 64 tokens, as everywhere here. */
+
+#define FTTS_MAX_TABLE_BATCH 1024
+
+/*
+ * Block tables and slot maps from request lengths.  For each request b in order, with
+ * has = ceil(cached[b] / 64) and need = ceil((cached[b] + added[b]) / 64):
+ *   block_table[b][0 .. has)       are kept as they are (the pages of its cached tokens),
+ *   block_table[b][has .. need)    take the next ids of free_pages,
+ *   block_table[b][need .. max_pages) become -1.
+ * A request is refused -- it takes no page, its entries from `has` on become -1, its tokens
+ * get no slot and its length does not grow -- if a length is negative, if it needs more than
+ * max_pages pages, or if it needs a page and the free pages do not reach for it and all
+ * before it (then every later request that needs a page is refused too).
+ *   cached       [B] tokens already in the cache, or NULL for none.
+ *   added        [B] tokens to add.
+ *   free_pages   [n_free] page ids, taken from the front; NULL if n_free is 0.
+ *   n_pages      pages of the pool; a token whose page id is outside [0, n_pages) gets no slot.
+ *   row_offsets  [B + 1] out: request b's new tokens are rows row_offsets[b] ..
+ *                row_offsets[b + 1] - 1 of the packed batch (negative lengths count 0;
+ *                sums past 2^31 - 1 stay there).
+ *   seq_lens     [B] out, or NULL: cached + added (refused: cached, at least 0).
+ *   slots        [max_rows] out: page * 64 + slot of each packed row, -1 for rows without one
+ *                and for the rows behind the last request's.
+ *   counts       [2] out: pages taken, requests refused.
+ * No output may overlap an input or another output, except block_table, which is updated in
+ * place (FTTS_E_INVALID_ARG where the host sees it).  1 <= B <= FTTS_MAX_TABLE_BATCH,
+ * 0 <= max_rows <= 2^24 (slots may be NULL if it is 0).
+ */
+int ftts_build_tables(const int32_t* cached, const int32_t* added, int32_t B, const int32_t* free_pages,
+                      int32_t n_free, int32_t n_pages, int32_t* block_table, int32_t max_pages,
+                      int32_t* row_offsets, int32_t* seq_lens, int32_t* slots, int32_t max_rows,
+                      int32_t* counts, void* stream);
+
+/*
+ * Writes n_rows new tokens' keys and values into their pages of one layer.
+ *   src_dtype   FTTS_F32 or FTTS_BF16, of k and v; kv_dtype that of the pool.  fp32 rows going
+ *               into a bf16 pool are rounded to nearest even; bf16 rows into an fp32 pool are
+ *               FTTS_E_DTYPE.
+ *   k, v        row i at k + i * k_stride (elements), its n_kv_head heads of 64 one after
+ *               another; 16-byte aligned, strides a multiple of 16 bytes and at least
+ *               64 * n_kv_head (the columns of packed q/k/v rows, for instance).
+ *   slots       [n_rows] page * 64 + slot; rows whose slot is negative or past the pool are
+ *               skipped.  No two rows may name the same slot (which of them stays is
+ *               unspecified then, head by head).
+ * n_rows 0 is allowed and enqueues nothing.  n_rows <= 2^24, n_kv_head <= 256, layer >= 0
+ * and within the pool.
+ */
+int ftts_append_kv(int32_t src_dtype, int32_t kv_dtype, const void* k, int64_t k_stride, const void* v,
+                   int64_t v_stride, int32_t n_rows, const int32_t* slots, const ftts_kv_pool* kv,
+                   int32_t layer, int32_t n_kv_head, void* stream);
+
+/* A prefix that every sequence of a batch continues: its token t lives in page pages[t / 64]
+ * (device int32 [ceil(len / 64)]) at slot t % 64 of the same pool.  len is a host value,
+ * 0 <= len <= FTTS_MAX_SHARED_PREFIX. */
+#define FTTS_MAX_SHARED_PREFIX (1 << 20)
+typedef struct {
+    const int32_t* pages;
+    int32_t len;
+} ftts_shared_prefix;
+
+typedef struct {
+    int32_t dtype;     /* FTTS_F32 or FTTS_BF16: the queries, the outputs and the pool */
+    int32_t n_head;    /* query heads, <= 256 */
+    int32_t n_kv_head; /* the pool's heads; divides n_head: query head h reads h / (n_head / n_kv_head) */
+    int32_t d_head;    /* must be 64 */
+} ftts_attn_shape;
+
+/* Bytes of device workspace for ftts_shared_attention over up to B sequences, n_rows rows, a
+ * prefix of prefix_len and max_pages pages a sequence (enough for every smaller call too).
+ * Returns 0 for invalid arguments. */
+size_t ftts_shared_attention_workspace_bytes(const ftts_attn_shape* shape, int32_t B, int32_t n_rows,
+                                             int32_t prefix_len, int32_t max_pages);
+
+/*
+ * Attention of a batch of sequences that continue one shared prefix: the prefix's keys and
+ * values are cached once, and where few rows meet a long prefix they are read once for the
+ * whole batch.  Sequence b's n_b query rows are the last n_b of its seq_lens[b] own tokens,
+ * whose keys and values are in its pages already; its row i sees every token of the prefix and
+ * the own tokens 0 .. seq_lens[b] - n_b + i:
+ *   out = sum_j exp(q . k_j / 8 - m) v_j / sum_j exp(q . k_j / 8 - m).
+ *   q, out       row r at q + r * q_stride (elements), head h in columns 64 h .. 64 h + 63;
+ *                16-byte aligned, strides a multiple of 16 bytes and at least 64 * n_head.
+ *                out must not overlap q or the pool.
+ *   row_offsets  [B + 1] device: sequence b's rows are row_offsets[b] .. row_offsets[b + 1] - 1
+ *                (ascending, within [0, n_rows]); rows of no sequence are left as they were.
+ *                NULL: one row per sequence (the single-token form; n_rows must be B).
+ *   prefix       the shared prefix, or NULL for none.
+ *   pt           block table and own lengths; a length past max_pages * 64 ends there, a
+ *                negative one makes its sequence inactive: its rows become 0.
+ * A row that sees no token becomes 0, and tokens in pages outside the pool are not seen; slots
+ * of a page past a sequence's end may hold anything.  A value that is not finite reaches only
+ * rows that see its token.  In bf16 the scores and the sums are fp32 and the output is rounded
+ * once; the weights multiply the values in 16-bit products.
+ * 1 <= B <= FTTS_MAX_BATCH, n_rows <= 2^24.  `ws` holds intermediate results of the call only;
+ * calls that can run at the same time need one each.
+ */
+int ftts_shared_attention(const ftts_attn_shape* shape, const void* q, int64_t q_stride,
+                          const int32_t* row_offsets, int32_t n_rows, int32_t B,
+                          const ftts_shared_prefix* prefix, const ftts_page_table* pt, const ftts_kv_pool* kv,
+                          int32_t layer, void* out, int64_t out_stride, void* ws, size_t ws_bytes,
+                          void* stream);
+
 /* ---- Semantic-to-Mel flow-matching DiT: one guided Euler step ------------------------
  *
  * Sec. II-A: the Semantic-to-Mel module is conditional flow matching with a

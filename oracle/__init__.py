@@ -14,8 +14,10 @@ gpt     -- the exact GPT-2 style decoder forward (Sec. II-A names GPT-2 as the
 quant   -- weight-only quantisation of the GPT linears to W8A16 / W4A16
            (Table I caption, Sec. III-B) and exact dequantisation.
 sample  -- greedy and temperature / top-k / top-p sampling of the next token.
+paged   -- block tables and slot maps, the write of keys and values by slot, and
+           attention behind a shared prefix.
 
 All arithmetic runs in the dtype the caller picks (fp64 for self-checks, fp32
 for parity); readings of points the paper leaves open are listed in each module.
 """
-from . import gpt, quant, sample  # noqa: F401
+from . import gpt, paged, quant, sample  # noqa: F401

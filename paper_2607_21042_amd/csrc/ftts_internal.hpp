@@ -316,6 +316,22 @@ bool bgemm_supported(int wdtype, int K, bool ln);
 hipError_t launch_act_to_f32(int wdtype, const void* src, int rows, int d, float* dst, hipStream_t st);
 hipError_t launch_assemble_prefix(int wdtype, const AssembleArgs& a, int rows, hipStream_t st);
 
+// Attention of a batch of sequences that continue one shared prefix, over the paged cache.
+struct SharedAttnArgs {
+    const void* q;           // row r at q + r * q_ld elements, head h at 64 h
+    void* o;
+    int64_t q_ld, o_ld;
+    const void* kv_base;
+    int n_pages, layer, n_head, n_kv_head, max_pages;
+    const int32_t* block_table;
+    const int32_t* seq_lens;
+    const int32_t* row_offsets;   // [B + 1], or null: row b is sequence b's
+    const int32_t* prefix_pages;
+    int prefix_len;
+    int B, rows;
+};
+hipError_t launch_shared_attention(int dtype, const SharedAttnArgs& a, hipStream_t st);
+
 // Flow-matching DiT step (bf16): time embedding, input rows and guidance.
 struct DitPrepareArgs {
     int T, n_mel, d_cond, d_model;

@@ -23,6 +23,8 @@ F32, BF16, W8A16, W4A16 = 0, 1, 2, 3
 WDTYPE_NAMES = {F32: "f32", BF16: "bf16", W8A16: "w8a16", W4A16: "w4a16"}
 MAX_TOP_K = 64
 MAX_BATCH = 64
+MAX_TABLE_BATCH = 1024
+MAX_SHARED_PREFIX = 1 << 20
 PAGE = 64
 
 _c = ctypes
@@ -75,6 +77,14 @@ class PageTable(_c.Structure):
 
 class Sampling(_c.Structure):
     _fields_ = [("temperature", f32), ("top_k", i32), ("top_p", f32)]
+
+
+class SharedPrefixC(_c.Structure):
+    _fields_ = [("pages", vp), ("len", i32)]
+
+
+class AttnShape(_c.Structure):
+    _fields_ = [("dtype", i32), ("n_head", i32), ("n_kv_head", i32), ("d_head", i32)]
 
 
 class LinearShape(_c.Structure):
@@ -130,6 +140,16 @@ def lib():
                                     vp]
         L.ftts_linear_plan.restype = _c.c_int
         L.ftts_linear_plan.argtypes = [i32, i32, i32, i32, P(LinearShape)]
+        i64 = _c.c_int64
+        L.ftts_build_tables.restype = _c.c_int
+        L.ftts_build_tables.argtypes = [vp, vp, i32, vp, i32, i32, vp, i32, vp, vp, vp, i32, vp, vp]
+        L.ftts_append_kv.restype = _c.c_int
+        L.ftts_append_kv.argtypes = [i32, i32, vp, i64, vp, i64, i32, vp, P(KvPool), i32, i32, vp]
+        L.ftts_shared_attention_workspace_bytes.restype = _c.c_size_t
+        L.ftts_shared_attention_workspace_bytes.argtypes = [P(AttnShape), i32, i32, i32, i32]
+        L.ftts_shared_attention.restype = _c.c_int
+        L.ftts_shared_attention.argtypes = [P(AttnShape), vp, i64, vp, i32, i32, P(SharedPrefixC), P(PageTable),
+                                            P(KvPool), i32, vp, i64, vp, _c.c_size_t, vp]
         _lib = L
     return _lib
 
@@ -306,6 +326,137 @@ def advance(tokens, positions, seq_lens, sampled, remaining=None, stop_token=0, 
                               B, _stream(stream)))
 
 
+# ---- serving a batch over the paged cache: tables, append, shared-prefix attention -----------
+def _i32(name, t, shape=None):
+    """Checks an int32 tensor argument (and its shape)."""
+    if t.dtype != torch.int32:
+        raise FTTSError(-3, f"{name} must be int32")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise FTTSError(-2, f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
+    return t
+
+
+def _rows(name, t):
+    """Data pointer and row stride of a 2-D tensor whose rows are contiguous."""
+    if not t.is_cuda:
+        raise FTTSError(-1, f"{name} must live on the GPU")
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise FTTSError(-2, f"{name} must be 2-D with contiguous rows")
+    # (the stride of a lone row says nothing)
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _wdtype(name, dtype):
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise FTTSError(-3, f"{name} must be fp32 or bf16")
+    return F32 if dtype == torch.float32 else BF16
+
+
+def _on(stream, *tensors):
+    """The device of all the tensors as a context, and the stream to use there."""
+    devices = {t.device for t in tensors if t is not None}
+    if len(devices) != 1:
+        raise FTTSError(-1, f"tensors on different devices: {sorted(map(str, devices))}")
+    dev = devices.pop()
+    if dev.type != "cuda":
+        raise FTTSError(-1, "tensor must live on the GPU")
+    if stream is None:
+        stream = torch.cuda.current_stream(dev)
+    elif getattr(stream, "device", dev) != dev:
+        raise FTTSError(-1, f"stream of {stream.device} for tensors of {dev}")
+    return torch.cuda.device(dev), _stream(stream)
+
+
+def build_tables(added, free_pages, n_pages: int, block_table, row_offsets, slots, counts, cached=None, seq_lens=None,
+                 stream=None):
+    """ftts_build_tables: block tables [B][max_pages] (updated in place), row offsets [B + 1], the
+    slot of each packed row and (optionally) the new lengths, from added [B] and cached [B] tokens
+    and the free page ids; counts [2] receives the pages taken and the requests refused."""
+    B = added.numel()
+    for name, t, shape in (("added", added, (B,)), ("row_offsets", row_offsets, (B + 1,)), ("counts", counts, (2,)),
+                           ("cached", cached, (B,)), ("seq_lens", seq_lens, (B,)), ("free_pages", free_pages, None),
+                           ("slots", slots, None)):
+        if t is not None:
+            _i32(name, t, shape)
+    _i32("block_table", block_table)
+    if block_table.dim() != 2 or block_table.shape[0] != B:
+        raise FTTSError(-2, f"block_table must be [{B}][max_pages]")
+    n_free, max_rows = 0 if free_pages is None else free_pages.numel(), 0 if slots is None else slots.numel()
+    ctx, st = _on(stream, added, free_pages, block_table, row_offsets, slots, counts, cached, seq_lens)
+    with ctx:
+        _check(lib().ftts_build_tables(_ptr(cached), _ptr(added), B, _ptr(free_pages), n_free, n_pages,
+                                       _ptr(block_table), block_table.shape[1], _ptr(row_offsets), _ptr(seq_lens),
+                                       _ptr(slots), max_rows, _ptr(counts), st))
+
+
+def append_kv(k, v, slots, kv, layer: int, stream=None):
+    """ftts_append_kv: rows k and v ([T][n_kv_head * 64], rows may be strided) into layer `layer`
+    of a KVCache at slots [T] (rows with a negative slot are skipped)."""
+    T, heads = k.shape[0], kv.pool.shape[3]
+    if k.dtype != v.dtype:
+        raise FTTSError(-3, "k and v must have one dtype")
+    for name, t in (("k", k), ("v", v)):
+        if tuple(t.shape) != (T, heads * 64):
+            raise FTTSError(-2, f"{name} must be [{T}][{heads * 64}]")
+    if not 0 <= layer < kv.pool.shape[0]:
+        raise FTTSError(-5, f"layer must be in [0, {kv.pool.shape[0]})")
+    _i32("slots", slots, (T,))
+    (kp, ks), (vp_, vs) = _rows("k", k), _rows("v", v)
+    ctx, st = _on(stream, k, v, slots, kv.pool)
+    with ctx:
+        _check(lib().ftts_append_kv(_wdtype("k", k.dtype), kv.dtype, kp, ks, vp_, vs, T, _ptr(slots),
+                                    _c.byref(kv.c), layer, heads, st))
+
+
+class SharedPrefix:
+    """A prefix that every sequence of a batch continues: its device page ids and its length."""
+
+    def __init__(self, pages, length: int):
+        length = int(length)
+        self.pages = _i32("pages", pages).contiguous()
+        if self.pages.numel() < -(-length // PAGE):
+            raise FTTSError(-2, f"{self.pages.numel()} pages do not hold {length} tokens")
+        self.len = length
+        self.c = SharedPrefixC(_ptr(self.pages) if length > 0 else None, length)
+
+
+def shared_attention_workspace_bytes(n_head: int, n_kv_head: int, dtype: int, batch: int, rows: int, prefix_len: int,
+                                     max_pages: int) -> int:
+    """ftts_shared_attention_workspace_bytes (dtype F32 or BF16)."""
+    s = AttnShape(dtype, n_head, n_kv_head, 64)
+    n = lib().ftts_shared_attention_workspace_bytes(_c.byref(s), batch, rows, prefix_len, max_pages)
+    if n == 0:
+        raise FTTSError(-1, lib().ftts_last_error().decode())
+    return n
+
+
+def shared_attention(q, kv, layer: int, page_table, prefix, out, ws, row_offsets=None, stream=None):
+    """ftts_shared_attention: query rows q [T][n_head * 64] of the sequences of `page_table`
+    (one each, or as row_offsets [B + 1] says), which all continue `prefix` (a SharedPrefix or
+    None), to out [T][n_head * 64]; keys and values in layer `layer` of a KVCache."""
+    T, width = q.shape
+    B, max_pages = page_table.block_table.shape
+    if width % 64 or tuple(out.shape) != (T, width):
+        raise FTTSError(-2, "q and out must be [T][n_head * 64]")
+    if q.dtype != out.dtype or q.dtype != kv.pool.dtype:
+        raise FTTSError(-3, "q, out and the pool must have one dtype")
+    if not 0 <= layer < kv.pool.shape[0]:
+        raise FTTSError(-5, f"layer must be in [0, {kv.pool.shape[0]})")
+    if row_offsets is not None:
+        _i32("row_offsets", row_offsets, (B + 1,))
+    if page_table.seq_lens.numel() != B:
+        raise FTTSError(-2, f"the page table needs {B} lengths")
+    (qp, qs), (op, os_) = _rows("q", q), _rows("out", out)
+    ctx, st = _on(stream, q, out, ws, row_offsets, kv.pool, page_table.block_table, page_table.seq_lens,
+                  None if prefix is None or prefix.len == 0 else prefix.pages)
+    shape = AttnShape(_wdtype("q", q.dtype), width // 64, kv.pool.shape[3], 64)
+    with ctx:
+        _check(lib().ftts_shared_attention(_c.byref(shape), qp, qs, _ptr(row_offsets), T, B,
+                                           _c.byref(prefix.c) if prefix is not None else None,
+                                           _c.byref(page_table.c), _c.byref(kv.c), layer, op, os_, _ptr(ws),
+                                           ws.numel() * ws.element_size(), st))
+
+
 # --------------------------------------------------------------------------- device state
 def make_config(shape, wdtype: int, eps: float = 1e-5) -> Config:
     return Config(shape.n_layer, shape.d_model, shape.n_head, shape.d_head, shape.d_ff, shape.vocab, shape.n_pos,
@@ -428,8 +579,23 @@ class KVCache:
         dims = (shape.n_layer, n_pages, 2, shape.n_head, PAGE, shape.d_head)
         self.pool = (torch.full(dims, fill, dtype=dt, device=device) if fill is not None
                      else torch.zeros(dims, dtype=dt, device=device))
-        self.n_pages = n_pages
-        self.c = KvPool(self.pool.data_ptr(), n_pages)
+        self._view()
+
+    def _view(self):
+        self.n_pages, self.dtype = self.pool.shape[1], F32 if self.pool.dtype == torch.float32 else BF16
+        self.c = KvPool(self.pool.data_ptr(), self.n_pages)
+
+    @classmethod
+    def over(cls, pool):
+        """The view of an existing pool tensor [n_layer][n_pages][2][n_kv_head][64][64]."""
+        if pool.dim() != 6 or pool.shape[2] != 2 or tuple(pool.shape[4:]) != (PAGE, 64):
+            raise FTTSError(-2, "a pool is [n_layer][n_pages][2][n_kv_head][64][64]")
+        _wdtype("the pool", pool.dtype)
+        _ptr(pool)
+        self = cls.__new__(cls)
+        self.pool = pool
+        self._view()
+        return self
 
 
 class PageTableView:
