@@ -467,7 +467,7 @@ size_t ftts_shared_attention_workspace_bytes(const ftts_attn_shape* shape, int32
  * of a page past a sequence's end may hold anything.  A value that is not finite reaches only
  * rows that see its token.  In bf16 the scores and the sums are fp32 and the output is rounded
  * once; the weights multiply the values in 16-bit products.
- * 1 <= B <= FTTS_MAX_BATCH, n_rows <= 2^24.  `ws` holds intermediate results of the call only;
+ * 1 <= B <= FTTS_MAX_BATCH, n_rows <= 2^24, n_rows * n_head < 2^31.  `ws` holds intermediate results of the call only;
  * calls that can run at the same time need one each.
  */
 int ftts_shared_attention(const ftts_attn_shape* shape, const void* q, int64_t q_stride,
