@@ -15,7 +15,7 @@
 
 namespace ftts {
 
-constexpr int kSaWaves = 4, kSaQ = 32;
+constexpr int kSaWaves = 2, kSaQ = 32;
 
 // How a call is cut: prefix rows in row_tiles tiles of 32, own rows in own_tiles (an upper bound
 // where the rows per sequence are on the device); c_pre and c_own pages a workgroup, s_pre and
@@ -45,69 +45,121 @@ __device__ __forceinline__ RowTile prefix_rows(const SharedAttnArgs& a, int tile
     t.inactive = false;
     return t;
 }
-// Own tile `tile`: its sequence goes to b (B: past the last one).
-__device__ __forceinline__ RowTile own_rows(const SharedAttnArgs& a, int tile, int kh, int lane, int ql, int& b) {
+// A run of the rows of one sequence: (token, head) pairs first .. first + size - 1 of its n * g.
+struct OwnTile {
+    int b, row0, n, len, first;  // sequence (B: past the last one), its first row, rows and length
+};
+// Tile `tile` of `size` pairs.  Whole waves call it.
+__device__ __forceinline__ OwnTile own_tile(const SharedAttnArgs& a, int tile, int size, int lane) {
     const int g = a.n_head / a.n_kv_head;
-    int n = 1, row0, in;  // rows and first row of the sequence, tile of the sequence
+    OwnTile t;
     if (!a.row_offsets) {
-        const int per = (g + kSaQ - 1) / kSaQ;
-        b = row0 = tile / per;
-        in = tile - b * per;
+        const int per = (g + size - 1) / size;
+        t.b = t.row0 = tile / per;
+        t.n = 1;
+        t.first = (tile - t.b * per) * size;
     } else {
         static_assert(FTTS_MAX_BATCH <= kWave, "one sequence per lane");
         const int lo = lane < a.B ? a.row_offsets[lane] : 0, hi = lane < a.B ? a.row_offsets[lane + 1] : 0;
         const int first = min(max(lo, 0), a.rows), rows = min(max(hi, first), a.rows) - first;
-        int end = (rows * g + kSaQ - 1) / kSaQ;  // (rows * n_head < 2^31)
+        int end = (rows * g + size - 1) / size;  // (rows * n_head < 2^31)
 #pragma unroll
         for (int d = 1; d < kWave; d <<= 1) {
             const int u = __shfl_up(end, d, kWave);
             if (lane >= d) end += u;
         }
-        b = __popcll(__ballot(lane < a.B && end <= tile));
-        if (b >= a.B) return RowTile{-1, 0, 0, 0, false};
-        row0 = __builtin_amdgcn_readlane(first, b);
-        n = __builtin_amdgcn_readlane(rows, b);
-        in = tile - (b ? __builtin_amdgcn_readlane(end, b - 1) : 0);
+        t.b = __popcll(__ballot(lane < a.B && end <= tile));
+        if (t.b >= a.B) return t;
+        t.row0 = __builtin_amdgcn_readlane(first, t.b);
+        t.n = __builtin_amdgcn_readlane(rows, t.b);
+        t.first = (tile - (t.b ? __builtin_amdgcn_readlane(end, t.b - 1) : 0)) * size;
     }
-    const int len = a.seq_lens[b], idx = in * kSaQ + ql, last = min(in * kSaQ + kSaQ, n * g) - 1;
-    auto seen = [&](int i) {  // own tokens that row i of the sequence sees
-        return len < 0 ? 0 : (int)min(max((int64_t)len - n + i + 1, (int64_t)0), (int64_t)a.max_pages * kPage);
-    };
-    RowTile t;
-    t.row = idx <= last ? row0 + idx / g : -1;
-    t.head = kh * g + idx % g;
-    t.most = seen(last / g);
-    t.lim = idx <= last ? seen(idx / g) : t.most;  // (a lane without a row asks for no mask)
-    t.inactive = len < 0;
+    t.len = a.seq_lens[t.b];
     return t;
+}
+// Own tokens that the i-th row of the sequence sees.
+__device__ __forceinline__ int own_seen(const SharedAttnArgs& a, const OwnTile& t, int i) {
+    return t.len < 0 ? 0 : (int)min(max((int64_t)t.len - t.n + i + 1, (int64_t)0), (int64_t)a.max_pages * kPage);
+}
+// The 32 pairs from `first` on, one a lane pair.
+__device__ __forceinline__ RowTile own_rows(const SharedAttnArgs& a, const OwnTile& o, int first, int kh, int ql) {
+    const int g = a.n_head / a.n_kv_head, idx = first + ql, last = min(first + kSaQ, o.n * g) - 1;
+    RowTile t;
+    t.row = idx <= last ? o.row0 + idx / g : -1;
+    t.head = kh * g + idx % g;
+    t.most = last >= first ? own_seen(a, o, last / g) : 0;
+    t.lim = idx <= last ? own_seen(a, o, idx / g) : t.most;  // (a lane without a row asks for no mask)
+    t.inactive = o.len < 0;
+    return t;
+}
+
+// A staged tile's K operands, and its V operands, in one assembly block with the wait: nothing is in flight in a
+// register that the compiler holds for written.
+__device__ __forceinline__ void sa_read_k(const AtAddr& r, uint32_t so, uint4 (&ka)[4], uint4 (&kb)[4]) {
+    at_bf16x8 x[8];
+    asm volatile(
+        "ds_read_b128 %0, %8\n\tds_read_b128 %1, %9\n\tds_read_b128 %2, %10\n\tds_read_b128 %3, %11\n\t"
+        "ds_read_b128 %4, %8 offset:4096\n\tds_read_b128 %5, %9 offset:4096\n\t"
+        "ds_read_b128 %6, %10 offset:4096\n\tds_read_b128 %7, %11 offset:4096\n\ts_waitcnt lgkmcnt(0)"
+        : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7])
+        : "v"(r.kr[0] + so), "v"(r.kr[1] + so), "v"(r.kr[2] + so), "v"(r.kr[3] + so)
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        ka[i] = __builtin_bit_cast(uint4, x[i]);
+        kb[i] = __builtin_bit_cast(uint4, x[4 + i]);
+    }
+}
+__device__ __forceinline__ void sa_read_v(const AtAddr& r, uint32_t so, uint64_t (&v)[2][2][4]) {
+#define SA_TR(O, A) "ds_read_b64_tr_b16 %" #O ", %" #A
+    asm volatile(
+        SA_TR(0, 16) "\n\t" SA_TR(1, 16) " offset:2048\n\t" SA_TR(2, 16) " offset:4096\n\t" SA_TR(3, 16) " offset:6144\n\t"
+        SA_TR(4, 17) "\n\t" SA_TR(5, 17) " offset:2048\n\t" SA_TR(6, 17) " offset:4096\n\t" SA_TR(7, 17) " offset:6144\n\t"
+        SA_TR(8, 18) "\n\t" SA_TR(9, 18) " offset:2048\n\t" SA_TR(10, 18) " offset:4096\n\t" SA_TR(11, 18) " offset:6144\n\t"
+        SA_TR(12, 19) "\n\t" SA_TR(13, 19) " offset:2048\n\t" SA_TR(14, 19) " offset:4096\n\t" SA_TR(15, 19) " offset:6144\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(v[0][0][0]), "=&v"(v[0][0][1]), "=&v"(v[0][0][2]), "=&v"(v[0][0][3]), "=&v"(v[0][1][0]), "=&v"(v[0][1][1]),
+          "=&v"(v[0][1][2]), "=&v"(v[0][1][3]), "=&v"(v[1][0][0]), "=&v"(v[1][0][1]), "=&v"(v[1][0][2]), "=&v"(v[1][0][3]),
+          "=&v"(v[1][1][0]), "=&v"(v[1][1][1]), "=&v"(v[1][1][2]), "=&v"(v[1][1][3])
+        : "v"(r.vr[0][0] + so), "v"(r.vr[1][0] + so), "v"(r.vr[0][1] + so), "v"(r.vr[1][1] + so)
+        : "memory");
+#undef SA_TR
 }
 
 // A wave's running attention of 32 rows: O^T as in AtState, the maximum (exp2 domain; -inf: nothing seen
 // yet) and the sum over this lane's half of the keys.
+typedef __bf16 sa_bf16x2 __attribute__((ext_vector_type(2)));
 struct SaState {
     at_f32x16 o0, o1;
     float m, l;
 };
 
-// Masks tokens at or past lim (k0: the tile's first token), moves the maximum where a tile exceeds it by
-// more than 2^8, and gives the weights as bf16 pairs and (LO) what their rounding left, in bf16 too.
-template <bool LO>
-__device__ __forceinline__ void sa_softmax(SaState& a, at_f32x16 (&s)[2], int k0, int lim, int hh, uint32_t (&pw)[16],
-                                           uint32_t (&pl)[LO ? 16 : 1]) {
-    const float kScale = 0.125f * 1.44269504088896340736f;  // 1/sqrt(64) * log2(e)
-    if (__any(lim < k0 + kAtK)) {
+__device__ __forceinline__ void sa_init(SaState& a) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+    for (int i = 0; i < 16; ++i) a.o0[i] = a.o1[i] = 0.f;
+    a.m = -INFINITY;
+    a.l = 0.f;
+}
+
+// Masks tokens at or past lim (k0: the tile's first token).
+__device__ __forceinline__ void sa_mask(at_f32x16 (&s)[2], int k0, int lim, int hh) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (k0 + 32 * b + (i >> 2) * 8 + hh * 4 + (i & 3) >= lim) s[b][i] = -INFINITY;
-    }
-    float tmax = fmaxf(s[0][0], s[1][0]);
+    for (int b = 0; b < 2; ++b)
 #pragma unroll
-    for (int i = 1; i < 16; ++i) tmax = fmaxf(tmax, fmaxf(s[0][i], s[1][i]));
+        for (int i = 0; i < 16; ++i)
+            if (k0 + 32 * b + (i >> 2) * 8 + hh * 4 + (i & 3) >= lim) s[b][i] = -INFINITY;
+}
+constexpr float kSaScale = 0.125f * 1.44269504088896340736f;  // 1/sqrt(64) * log2(e)
+// Moves the maximum where a tile exceeds it by more than 2^8.
+template <int N>
+__device__ __forceinline__ void sa_maximum(SaState& a, const at_f32x16 (&s)[N]) {
+    // (the maximum that passes NaN on: one instruction for three operands, and none to quieten them)
+    float tmax = s[0][0];
+#pragma unroll
+    for (int i = 1; i < 16 * N; ++i) tmax = __builtin_elementwise_maximum(tmax, s[i >> 4][i & 15]);
     {
         const RowPair pr = swap32(tmax);
-        tmax = fmaxf(pr.a, pr.b) * kScale;
+        tmax = __builtin_elementwise_maximum(pr.a, pr.b) * kSaScale;
     }
     if (__any(tmax > a.m + 8.f)) {
         const float mn = fmaxf(a.m, tmax), alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(a.m - mn);
@@ -119,18 +171,28 @@ __device__ __forceinline__ void sa_softmax(SaState& a, at_f32x16 (&s)[2], int k0
             a.o1[i] *= alpha;
         }
     }
+}
+// The weights as bf16 pairs, their sum over this lane's half of the keys and (LO) what their rounding left, in bf16 too.
+template <bool LO>
+__device__ __forceinline__ float sa_weights(const SaState& a, const at_f32x16 (&s)[2], uint32_t (&pw)[16], uint32_t (&pl)[LO ? 16 : 1]) {
     const float ref = a.m == -INFINITY ? 0.f : a.m;  // nothing seen: every score is -inf and every weight 0
+    float l = 0.f;
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int i = 0; i < 16; i += 2) {
-            const float x = __builtin_amdgcn_exp2f(fmaf(s[b][i], kScale, -ref));
-            const float y = __builtin_amdgcn_exp2f(fmaf(s[b][i + 1], kScale, -ref));
+            const float x = __builtin_amdgcn_exp2f(fmaf(s[b][i], kSaScale, -ref));
+            const float y = __builtin_amdgcn_exp2f(fmaf(s[b][i + 1], kSaScale, -ref));
             const uint32_t w = bf16x2_rne(x, y);
             pw[b * 8 + i / 2] = w;
-            a.l += x + y;
-            if constexpr (LO) pl[b * 8 + i / 2] = bf16x2_rne(x - bf16lo(w), y - bf16hi(w));
+            if constexpr (LO) {
+                l += x + y;
+                pl[b * 8 + i / 2] = bf16x2_rne(x - bf16lo(w), y - bf16hi(w));
+            } else {
+                l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(sa_bf16x2, w), __builtin_bit_cast(sa_bf16x2, 0x3F803F80u), l, false);
+            }
         }
+    return l;
 }
 // O^T += V^T P^T over a tile's 64 keys (k slots as at_read_v gives them).
 __device__ __forceinline__ void sa_pv(SaState& a, const uint64_t (&v)[2][2][4], const uint32_t (&pw)[16]) {
@@ -146,9 +208,27 @@ __device__ __forceinline__ void sa_pv(SaState& a, const uint64_t (&v)[2][2][4], 
     }
 }
 // Values that are not finite, in a tile that some row sees in part: in one product with the rest their 0 x inf = NaN
-// would reach the rows that do not see them.  They become 0 in the operands (returns whether there were any) ...
-__device__ __forceinline__ bool sa_take_out(uint64_t (&v)[2][2][4]) {
-    uint32_t bad = 0;
+// would reach the rows that do not see them.  Whether there are any: the sums of all values by dimension, a product
+// with ones, tell (finite ones that overflow fp32 only send the tile the slow way).  x: registers for it.
+__device__ __forceinline__ bool sa_not_finite(const uint64_t (&v)[2][2][4], at_f32x16 (&x)[2]) {
+    const at_bf16x8 ones = at_op(make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u));
+    float z = 0.f;
+#pragma unroll
+    for (int d = 0; d < 2; ++d) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[d][i] = 0.f;
+#pragma unroll
+        for (int st = 0; st < 4; ++st)
+            x[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                at_op(make_uint4((uint32_t)v[d][0][st], (uint32_t)(v[d][0][st] >> 32), (uint32_t)v[d][1][st], (uint32_t)(v[d][1][st] >> 32))),
+                ones, x[d], 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) z = fmaf(x[d][i], 0.f, z);
+    }
+    return __any(z != 0.f);  // (NaN)
+}
+// Then they become 0 in the operands ...
+__device__ __forceinline__ void sa_take_out(uint64_t (&v)[2][2][4]) {
 #pragma unroll
     for (int d = 0; d < 2; ++d)
 #pragma unroll
@@ -158,163 +238,91 @@ __device__ __forceinline__ bool sa_take_out(uint64_t (&v)[2][2][4]) {
                 uint32_t x[2] = {(uint32_t)v[d][e][st], (uint32_t)(v[d][e][st] >> 32)};
 #pragma unroll
                 for (int w = 0; w < 2; ++w) {
-                    const uint32_t lo = (x[w] & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u;
-                    const uint32_t hi = (x[w] & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u;
-                    bad |= lo | hi;
-                    x[w] &= ~(lo | hi);
+                    if ((x[w] & 0x7F80u) == 0x7F80u) x[w] &= 0xFFFF0000u;
+                    if ((x[w] & 0x7F800000u) == 0x7F800000u) x[w] &= 0xFFFFu;
                 }
                 v[d][e][st] = (uint64_t)x[1] << 32 | x[0];
             }
-    return __any(bad != 0);
 }
-// ... and are added here where the weight is not 0.  vt: the tile in LDS; the weights go through 4 KB of it (wl, rows
-// of 64 keys).
-__device__ __forceinline__ void sa_add_not_finite(SaState& a, const char* vt, char* wl, const uint32_t (&pw)[16], int lane) {
-    const int ql = lane & 31, hh = lane >> 5;
+// ... and are added here where the weight is not 0.  vt: the tile in LDS.
+__device__ __forceinline__ void sa_add_not_finite(SaState& a, const char* vt, const uint32_t (&pw)[16], int hh) {
+    uint32_t p[16];
 #pragma unroll
-    for (int j = 0; j < 16; ++j)
-        *reinterpret_cast<uint32_t*>(wl + ql * 128 + 2 * (32 * (j >> 3) + ((j >> 1) & 3) * 8 + hh * 4 + 2 * (j & 1))) = pw[j];
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    for (int key = 0; key < kAtK; ++key) {
-        const float p = bf16_to_f32(*reinterpret_cast<const uint16_t*>(wl + ql * 128 + 2 * key));
-        const char* row = vt + key * 128 + hh * 8;
+    for (int j = 0; j < 16; ++j) p[j] = pw[j];
+#pragma unroll 1
+    for (int j = 0; j < 16; ++j) {  // pair j of both halves of the wave: 4 keys
+        const auto w = __builtin_amdgcn_permlane32_swap(p[0], p[0], false, false);
+#pragma unroll 1
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t x = k < 2 ? w[0] : w[1];
+            const float pk = k & 1 ? bf16hi(x) : bf16lo(x);
+            const int key = 32 * (j >> 3) + ((j >> 1) & 3) * 8 + (k >> 1) * 4 + 2 * (j & 1) + (k & 1);
+            const char* row = vt + key * 128 + hh * 8;
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
-            const uint2 x = *reinterpret_cast<const uint2*>(row + ((c ^ ((key >> 1) & 7)) << 4));
-            const float f[4] = {bf16lo(x.x), bf16hi(x.x), bf16lo(x.y), bf16hi(x.y)};
+            for (int c = 0; c < 8; ++c) {
+                const uint2 v = *reinterpret_cast<const uint2*>(row + ((c ^ ((key >> 1) & 7)) << 4));
+                const float f[4] = {bf16lo(v.x), bf16hi(v.x), bf16lo(v.y), bf16hi(v.y)};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float y = p != 0.f && !(fabsf(f[i]) < INFINITY) ? p * f[i] : 0.f;
-                if (c < 4) a.o0[4 * (c & 3) + i] += y;
-                else a.o1[4 * (c & 3) + i] += y;
+                for (int i = 0; i < 4; ++i) {
+                    const float y = pk != 0.f && !(fabsf(f[i]) < INFINITY) ? pk * f[i] : 0.f;
+                    if (c < 4) a.o0[4 * (c & 3) + i] += y;
+                    else a.o1[4 * (c & 3) + i] += y;
+                }
             }
         }
+#pragma unroll
+        for (int i = 0; i < 15; ++i) p[i] = p[i + 1];
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 }
 
-// One workgroup per key head, 32 rows and run of pages: the 4 waves take its pages in turn (wave w: w, w + 4, ...)
-// by direct-to-LDS loads into a stage of their own, the next page's K (V) on its way once this one's is in
-// registers, no barrier in the loop; their (m, l, o) are joined through LDS.  PROMPT: several rows a sequence, so a
-// tile's rows may see different tokens.
-template <bool PROMPT>
-__global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_kernel(const SharedAttnArgs a, const SharedPlan pl) {
-    constexpr int kWeights = PROMPT ? kSaQ * 128 : 0;
-    __shared__ __attribute__((aligned(1024))) char smem[kSaWaves * (kAtStage + kWeights)];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int ql = lane & 31, hh = lane >> 5;
-    int id = blockIdx.x, kh, slot, page0, pages;
+// What a workgroup of the cut call does: 32 rows, one key head, a run of pages.
+struct PartWork {
     RowTile t;
-    const int32_t* ids;
-    // Prefix work first: the row tiles of one (key head, run of pages) are 8 workgroups apart, so that one XCD
-    // (workgroups are dealt to the 8 in turn) reads the run through its L2.
+    const int32_t* ids;  // its pages
+    int kh, page0, pages;
+    int64_t part;        // where this lane's row leaves its partial
+};
+// Prefix work comes first: the row tiles of one (key head, run of pages) are 8 workgroups apart, so that one XCD
+// (workgroups are dealt to the 8 in turn) reads the run through its L2.  False: nothing to do (what has no pages
+// says so in its slot).
+__device__ __forceinline__ bool part_work(const SharedAttnArgs& a, const SharedPlan& pl, int tid, PartWork& w) {
+    const int lane = tid & 63, ql = lane & 31;
+    int id = blockIdx.x, slot;
     const int n_pre = (a.n_kv_head * pl.s_pre + 7) / 8 * 8 * pl.row_tiles;
     if (id < n_pre) {
         const int pair = id / (8 * pl.row_tiles) * 8 + id % 8, tile = id / 8 % pl.row_tiles;
-        if (pair >= a.n_kv_head * pl.s_pre) return;
-        kh = pair % a.n_kv_head;
+        if (pair >= a.n_kv_head * pl.s_pre) return false;
+        w.kh = pair % a.n_kv_head;
         slot = pair / a.n_kv_head;
-        t = prefix_rows(a, tile, kh, ql);
-        page0 = slot * pl.c_pre;
-        pages = min(pl.c_pre, (a.prefix_len + kPage - 1) / kPage - page0);
-        ids = a.prefix_pages + page0;
+        w.t = prefix_rows(a, tile, w.kh, ql);
+        w.page0 = slot * pl.c_pre;
+        w.pages = min(pl.c_pre, (a.prefix_len + kPage - 1) / kPage - w.page0);
+        w.ids = a.prefix_pages + w.page0;
     } else {
         id -= n_pre;
-        kh = id % a.n_kv_head;
+        w.kh = id % a.n_kv_head;
         const int sp = id / a.n_kv_head % pl.s_own, tile = id / a.n_kv_head / pl.s_own;
-        int b;
-        t = own_rows(a, tile, kh, lane, ql, b);
-        if (b >= a.B) return;
+        const OwnTile o = own_tile(a, tile, kSaQ, lane);
+        if (o.b >= a.B) return false;
+        w.t = own_rows(a, o, o.first, w.kh, ql);
         slot = pl.s_pre + sp;
-        page0 = sp * pl.c_own;
-        pages = min(pl.c_own, (t.most + kPage - 1) / kPage - page0);
-        ids = a.block_table + (size_t)b * a.max_pages + page0;
+        w.page0 = sp * pl.c_own;
+        w.pages = min(pl.c_own, (w.t.most + kPage - 1) / kPage - w.page0);
+        w.ids = a.block_table + (size_t)o.b * a.max_pages + w.page0;
     }
-    const int64_t rows_heads = (int64_t)a.rows * a.n_head;
-    const int64_t part = slot * rows_heads + (int64_t)t.row * a.n_head + t.head;
-    if (pages <= 0) {  // (an inactive sequence is marked by a negative sum)
-        if (t.row >= 0 && tid < kSaQ) pl.ml[part] = make_float2(-INFINITY, t.inactive ? -1.f : 0.f);
-        return;
-    }
-    char* own = smem + wave * kAtStage;
-    char* wl = smem + kSaWaves * kAtStage + wave * kWeights;
-    const int n = pages > wave ? (pages - wave + kSaWaves - 1) / kSaWaves : 0;  // this wave's pages
-    int phys_l = 0;
-    // the wave's page ids, 64 at a time (lane j: page j of the round)
-    auto fetch_ids = [&](int j0) { phys_l = j0 + lane < n ? ids[wave + kSaWaves * (j0 + lane)] : -1; };
-    auto load = [&](int j, int kv) {  // the wave's page j, K (kv 0) or V; nothing of an invalid page
-        int phys = __builtin_amdgcn_readlane(phys_l, j & 63);
-        const bool ok = phys >= 0 && phys < a.n_pages;
-        const int left = t.most - (page0 + wave + kSaWaves * j) * kPage;
-        const int bytes = ok ? min(left, kPage) * (kHeadDim * 2) : 0;
-        const uint16_t* src = reinterpret_cast<const uint16_t*>(a.kv_base) +
-                              kv_offset(a.layer, a.n_pages, ok ? phys : 0, kv, a.n_kv_head, kh, 0);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int row = i * 8 + (lane >> 3);
-            buffer_to_lds16(src, bytes, own + kv * kAtTile + i * 1024, row * 128 + (((lane & 7) ^ ((row >> 1) & 7)) << 4), 0);
-        }
-        return ok;
-    };
-    uint4 qr[4];
-    {
-        const uint16_t* qp = reinterpret_cast<const uint16_t*>(a.q) + (size_t)max(t.row, 0) * a.q_ld + t.head * kHeadDim;
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk) qr[kk] = *reinterpret_cast<const uint4*>(qp + kk * 16 + hh * 8);
-    }
-    const AtAddr ad = at_addresses(lds_address(own), lane);
-    SaState st;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) st.o0[i] = st.o1[i] = 0.f;
-    st.m = -INFINITY;
-    st.l = 0.f;
-    bool ok = false;
-    if (n > 0) {
-        fetch_ids(0);
-        ok = load(0, 0);
-        __builtin_amdgcn_sched_barrier(0);
-        load(0, 1);
-    }
-    for (int j = 0; j < n; ++j) {
-        const bool more = j + 1 < n, seen = ok;
-        const int k0 = (page0 + wave + kSaWaves * j) * kPage;
-        asm volatile("s_waitcnt vmcnt(8)" ::: "memory");  // K is in (this wave's own loads), V's 8 loads may be out
-        __builtin_amdgcn_sched_barrier(0);
-        uint4 ka[4], kb[4];
-        at_read_k(ad, 0, ka, kb);
-        at_wait_lds();
-        at_tie4(ka);
-        at_tie4(kb);
-        __builtin_amdgcn_sched_barrier(0);
-        if (more) {
-            if (((j + 1) & 63) == 0) fetch_ids(j + 1);
-            ok = load(j + 1, 0);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        at_f32x16 s[2];
-        at_scores(ka, kb, qr, s);
-        uint32_t pw[16], plo[16];
-        sa_softmax<true>(st, s, k0, seen ? t.lim : 0, hh, pw, plo);
-        __builtin_amdgcn_sched_barrier(0);
-        if (more) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");  // V is in, the next K may be out
-        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __builtin_amdgcn_sched_barrier(0);
-        uint64_t v[2][2][4];
-        at_read_v(ad, 0, v);
-        at_wait_lds();
-        at_tie_v(v);
-        __builtin_amdgcn_sched_barrier(0);
-        // (rows without a token in the tile have weights of 0, those past a tile's end zeros for values)
-        if (PROMPT && __any(t.lim < min(t.most, k0 + kAtK)) && sa_take_out(v)) sa_add_not_finite(st, own + kAtTile, wl, pw, lane);
-        if (more) load(j + 1, 1);
-        __builtin_amdgcn_sched_barrier(0);
-        sa_pv(st, v, pw);
-        sa_pv(st, v, plo);
-    }
-    __syncthreads();  // every wave has read its stage: the partials of waves 1 .. 3 go there, lane for lane
-    float* mrg = reinterpret_cast<float*>(smem);  // [3][34][64]
+    w.part = slot * ((int64_t)a.rows * a.n_head) + (int64_t)w.t.row * a.n_head + w.t.head;
+    if (w.pages > 0) return true;
+    // (an inactive sequence is marked by a negative sum)
+    if (w.t.row >= 0 && tid < kSaQ) pl.ml[w.part] = make_float2(-INFINITY, w.t.inactive ? -1.f : 0.f);
+    return false;
+}
+// Joins the waves' results through LDS (every wave is done with smem) and leaves the partial.
+__device__ __forceinline__ void part_finish(const SharedPlan& pl, const PartWork& w, SaState& st, char* smem, int wave, int lane) {
+    static_assert(kSaWaves == 2, "one wave hands over to the other");
+    __syncthreads();
+    float* mw = reinterpret_cast<float*>(smem);  // [34][64], lane for lane
     if (wave > 0) {
-        float* mw = mrg + (wave - 1) * 34 * 64;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             mw[i * 64 + lane] = st.o0[i];
@@ -325,68 +333,434 @@ __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_kernel(const Sha
     }
     __syncthreads();
     if (wave > 0) return;
-    float mm = st.m;
-#pragma unroll
-    for (int w = 0; w < kSaWaves - 1; ++w) mm = fmaxf(mm, mrg[(w * 34 + 32) * 64 + lane]);
-    const float ref = mm == -INFINITY ? 0.f : mm;
-    const float f0 = exp2f(st.m - ref);
-    st.l *= f0;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        st.o0[i] *= f0;
-        st.o1[i] *= f0;
-    }
-#pragma unroll
-    for (int w = 0; w < kSaWaves - 1; ++w) {
-        const float* mw = mrg + w * 34 * 64;
-        const float f = exp2f(mw[32 * 64 + lane] - ref);
-        st.l += mw[33 * 64 + lane] * f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            st.o0[i] += mw[i * 64 + lane] * f;
-            st.o1[i] += mw[(16 + i) * 64 + lane] * f;
-        }
-    }
-    const RowPair ls = swap32(st.l);
-    if (t.row < 0) return;
-    if (hh == 0) pl.ml[part] = make_float2(mm, ls.a + ls.b);
-    float4* out = reinterpret_cast<float4*>(pl.o + part * kHeadDim) + hh;
+    const float m1 = mw[32 * 64 + lane], mm = fmaxf(st.m, m1), ref = mm == -INFINITY ? 0.f : mm;
+    const float f0 = exp2f(st.m - ref), f1 = exp2f(m1 - ref);
+    const RowPair ls = swap32(st.l * f0 + mw[33 * 64 + lane] * f1);
+    if (w.t.row < 0) return;
+    const int hh = lane >> 5;
+    if (hh == 0) pl.ml[w.part] = make_float2(mm, ls.a + ls.b);
+    float4* out = reinterpret_cast<float4*>(pl.o + w.part * kHeadDim) + hh;
+    auto sum = [&](const at_f32x16& o, int at, int i) { return o[i] * f0 + mw[(at + i) * 64 + lane] * f1; };
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-        out[2 * g] = make_float4(st.o0[4 * g], st.o0[4 * g + 1], st.o0[4 * g + 2], st.o0[4 * g + 3]);
-        out[8 + 2 * g] = make_float4(st.o1[4 * g], st.o1[4 * g + 1], st.o1[4 * g + 2], st.o1[4 * g + 3]);
+        out[2 * g] = make_float4(sum(st.o0, 0, 4 * g), sum(st.o0, 0, 4 * g + 1), sum(st.o0, 0, 4 * g + 2), sum(st.o0, 0, 4 * g + 3));
+        out[8 + 2 * g] = make_float4(sum(st.o1, 16, 4 * g), sum(st.o1, 16, 4 * g + 1), sum(st.o1, 16, 4 * g + 2), sum(st.o1, 16, 4 * g + 3));
     }
 }
 
-// Joins the partials: 16 lanes per (row, head), 4 dims each.
+// bf16: the waves take a run's pages in turn (wave w: w, w + 2, ...) by direct-to-LDS loads into a stage of their own,
+// the next page's K (V) on its way once this one's is in registers; no barrier in the loop.  The weights go into the
+// products as bf16 and what their rounding left, so that only the output is rounded.  PROMPT: several rows a
+// sequence, so a tile's rows may see different tokens.
+template <bool PROMPT>
+__global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_kernel(const SharedAttnArgs a, const SharedPlan pl) {
+    __shared__ __attribute__((aligned(1024))) char smem[kSaWaves * kAtStage];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hh = lane >> 5;
+    PartWork w;
+    if (!part_work(a, pl, tid, w)) return;
+    const RowTile& t = w.t;
+    char* own = smem + wave * kAtStage;
+    const int n = w.pages > wave ? (w.pages - wave + kSaWaves - 1) / kSaWaves : 0;  // this wave's pages
+    int phys_l = 0;
+    // the wave's page ids, 64 at a time (lane j: page j of the round)
+    auto fetch_ids = [&](int j0) { phys_l = j0 + lane < n ? w.ids[wave + kSaWaves * (j0 + lane)] : -1; };
+    auto load = [&](int j, int kv) {  // the wave's page j, K (kv 0) or V; nothing of an invalid page
+        int phys = __builtin_amdgcn_readlane(phys_l, j & 63);
+        const bool ok = phys >= 0 && phys < a.n_pages;
+        const int left = t.most - (w.page0 + wave + kSaWaves * j) * kPage;
+        const int bytes = ok ? min(left, kPage) * (kHeadDim * 2) : 0;
+        const uint16_t* src = reinterpret_cast<const uint16_t*>(a.kv_base) +
+                              kv_offset(a.layer, a.n_pages, ok ? phys : 0, kv, a.n_kv_head, w.kh, 0);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int row = i * 8 + (lane >> 3);
+            buffer_to_lds16(src, bytes, own + kv * kAtTile + i * 1024, row * 128 + (((lane & 7) ^ ((row >> 1) & 7)) << 4), 0);
+        }
+        return ok;
+    };
+    uint4 qr[4];
+    at_load_q(reinterpret_cast<const uint16_t*>(a.q) + (size_t)max(t.row, 0) * a.q_ld + t.head * kHeadDim, hh, qr);
+    const AtAddr ad = at_addresses(lds_address(own), lane);
+    SaState st;
+    sa_init(st);
+    bool ok = false;
+    if (n > 0) {
+        fetch_ids(0);
+        ok = load(0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        load(0, 1);
+    }
+    for (int j = 0; j < n; ++j) {
+        const bool more = j + 1 < n, seen = ok;
+        const int k0 = (w.page0 + wave + kSaWaves * j) * kPage;
+        asm volatile("s_waitcnt vmcnt(8)" ::: "memory");  // K is in (this wave's own loads), V's 8 loads may be out
+        __builtin_amdgcn_sched_barrier(0);
+        uint4 ka[4], kb[4];
+        sa_read_k(ad, 0, ka, kb);
+        __builtin_amdgcn_sched_barrier(0);
+        if (more) {
+            if (((j + 1) & 63) == 0) fetch_ids(j + 1);
+            ok = load(j + 1, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        at_f32x16 s[2];
+        at_scores(ka, kb, qr, s);
+        uint32_t pw[16], plo[16];
+        const int lim = seen ? t.lim : 0;
+        if (__any(lim < k0 + kAtK)) sa_mask(s, k0, lim, hh);
+        sa_maximum(st, s);
+        st.l += sa_weights<true>(st, s, pw, plo);
+        __builtin_amdgcn_sched_barrier(0);
+        if (more) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");  // V is in, the next K may be out
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        uint64_t v[2][2][4];
+        sa_read_v(ad, 0, v);
+        __builtin_amdgcn_sched_barrier(0);
+        // (rows without a token in the tile have weights of 0, those past a tile's end zeros for values)
+        if (PROMPT && __any(t.lim < min(t.most, k0 + kAtK)) && sa_not_finite(v, s)) {
+            sa_add_not_finite(st, own + kAtTile, pw, hh);
+            sa_read_v(ad, 0, v);
+            sa_take_out(v);
+        }
+        if (more) load(j + 1, 1);
+        __builtin_amdgcn_sched_barrier(0);
+        sa_pv(st, v, pw);
+        sa_pv(st, v, plo);
+    }
+    part_finish(pl, w, st, smem, wave, lane);
+}
+
+// fp32: the same on 32-token halves of pages (the same 16 KB a stage) with fp32 matrix products, all sums in fp32.  A
+// 16-byte piece c of row r lies at c ^ (r % 16).  K as the first operand: lane (key, hh) holds dims 32 hh .. + 31, one
+// a step; V: lane (dim, hh) holds the key that element i of the scores is for.
+constexpr int kSfK = 32;
+__device__ __forceinline__ void sf_read_k(const uint32_t (&kr)[8], float4 (&k)[8]) {
+    at_bf16x8 x[8];  // (any 16-byte register type)
+    asm volatile(
+        "ds_read_b128 %0, %8\n\tds_read_b128 %1, %9\n\tds_read_b128 %2, %10\n\tds_read_b128 %3, %11\n\t"
+        "ds_read_b128 %4, %12\n\tds_read_b128 %5, %13\n\tds_read_b128 %6, %14\n\tds_read_b128 %7, %15\n\ts_waitcnt lgkmcnt(0)"
+        : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7])
+        : "v"(kr[0]), "v"(kr[1]), "v"(kr[2]), "v"(kr[3]), "v"(kr[4]), "v"(kr[5]), "v"(kr[6]), "v"(kr[7])
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 8; ++i) k[i] = __builtin_bit_cast(float4, x[i]);
+}
+// v[i] = value of key (i/4)*8 + hh*4 + i%4 in dim lane % 32 (+ 32: the addresses of the other half of a row).
+__device__ __forceinline__ void sf_read_v(const uint32_t (&a)[8], int flip, float (&v)[16]) {
+#define SF_R(O, A, OFF) "ds_read_b32 %" #O ", %" #A " offset:" #OFF "\n\t"
+    asm volatile(
+        SF_R(0, 16, 0) SF_R(1, 17, 256) SF_R(2, 18, 512) SF_R(3, 19, 768)
+        SF_R(4, 20, 2048) SF_R(5, 21, 2304) SF_R(6, 22, 2560) SF_R(7, 23, 2816)
+        SF_R(8, 16, 4096) SF_R(9, 17, 4352) SF_R(10, 18, 4608) SF_R(11, 19, 4864)
+        SF_R(12, 20, 6144) SF_R(13, 21, 6400) SF_R(14, 22, 6656) SF_R(15, 23, 6912)
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]), "=&v"(v[4]), "=&v"(v[5]), "=&v"(v[6]), "=&v"(v[7]),
+          "=&v"(v[8]), "=&v"(v[9]), "=&v"(v[10]), "=&v"(v[11]), "=&v"(v[12]), "=&v"(v[13]), "=&v"(v[14]), "=&v"(v[15])
+        : "v"(a[0 ^ flip]), "v"(a[1 ^ flip]), "v"(a[2 ^ flip]), "v"(a[3 ^ flip]), "v"(a[4 ^ flip]), "v"(a[5 ^ flip]),
+          "v"(a[6 ^ flip]), "v"(a[7 ^ flip])
+        : "memory");
+#undef SF_R
+}
+// As sa_add_not_finite.
+__device__ __forceinline__ void sf_add_not_finite(SaState& a, const char* vt, const at_f32x16& pw, int hh) {
+    at_f32x16 p = pw;
+#pragma unroll 1
+    for (int j = 0; j < 16; ++j) {
+        const RowPair w = swap32(p[0]);
+#pragma unroll 1
+        for (int k = 0; k < 2; ++k) {
+            const float pk = k ? w.b : w.a;
+            const int key = (j >> 2) * 8 + k * 4 + (j & 3);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+                const float4 v = *reinterpret_cast<const float4*>(vt + key * 256 + (((2 * c + hh) ^ (key & 15)) << 4));
+                const float f[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float y = pk != 0.f && !(fabsf(f[i]) < INFINITY) ? pk * f[i] : 0.f;
+                    if (c < 4) a.o0[4 * (c & 3) + i] += y;
+                    else a.o1[4 * (c & 3) + i] += y;
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 15; ++i) p[i] = p[i + 1];
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+}
+
+template <bool PROMPT>
+__global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_f32_kernel(const SharedAttnArgs a, const SharedPlan pl) {
+    __shared__ __attribute__((aligned(1024))) char smem[kSaWaves * kAtStage];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int ql = lane & 31, hh = lane >> 5;
+    PartWork w;
+    if (!part_work(a, pl, tid, w)) return;
+    const RowTile& t = w.t;
+    char* own = smem + wave * kAtStage;
+    const int n = w.pages > wave ? 2 * ((w.pages - wave + kSaWaves - 1) / kSaWaves) : 0;  // this wave's half pages
+    int phys_l = 0;
+    auto fetch_ids = [&](int j0) { phys_l = 2 * (j0 + lane) < n ? w.ids[wave + kSaWaves * (j0 + lane)] : -1; };  // (64 pages)
+    auto first = [&](int u) { return (w.page0 + wave + kSaWaves * (u >> 1)) * kPage + (u & 1) * kSfK; };
+    auto load = [&](int u, int kv) {  // half page u, K (kv 0) or V; nothing of an invalid page
+        const int phys = __builtin_amdgcn_readlane(phys_l, (u >> 1) & 63);
+        const bool ok = phys >= 0 && phys < a.n_pages;
+        const int bytes = ok ? max(min(t.most - first(u), kSfK), 0) * (kHeadDim * 4) : 0;
+        const float* src = reinterpret_cast<const float*>(a.kv_base) +
+                           kv_offset(a.layer, a.n_pages, ok ? phys : 0, kv, a.n_kv_head, w.kh, (u & 1) * kSfK);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int row = i * 4 + (lane >> 4);
+            buffer_to_lds16(src, bytes, own + kv * kAtTile + i * 1024, row * 256 + (((lane & 15) ^ (row & 15)) << 4), 0);
+        }
+        return ok;
+    };
+    float4 q[8];
+    {
+        const float* qp = reinterpret_cast<const float*>(a.q) + (size_t)max(t.row, 0) * a.q_ld + t.head * kHeadDim + hh * 32;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = *reinterpret_cast<const float4*>(qp + 4 * i);
+    }
+    uint32_t kr[8], vr[8];
+    {
+        const uint32_t s0 = lds_address(own);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            kr[c] = s0 + ql * 256 + (((hh * 8 + c) ^ (ql & 15)) << 4);
+            // c = 4 (i / 4 % 2) + i % 4 for element i
+            vr[c] = s0 + kAtTile + hh * 1024 + (((ql >> 2) ^ ((c >> 2) * 8 + hh * 4 + (c & 3))) << 4) + (ql & 3) * 4;
+        }
+    }
+    SaState st;
+    sa_init(st);
+    bool ok = false;
+    if (n > 0) {
+        fetch_ids(0);
+        ok = load(0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        load(0, 1);
+    }
+    for (int u = 0; u < n; ++u) {
+        const bool more = u + 1 < n, seen = ok;
+        const int k0 = first(u);
+        asm volatile("s_waitcnt vmcnt(8)" ::: "memory");  // K is in (this wave's own loads), V's 8 loads may be out
+        __builtin_amdgcn_sched_barrier(0);
+        float4 k[8];
+        sf_read_k(kr, k);
+        __builtin_amdgcn_sched_barrier(0);
+        if (more) {
+            if (((u + 1) & 127) == 0) fetch_ids((u + 1) >> 1);
+            ok = load(u + 1, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        at_f32x16 s[1];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[0][i] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            s[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(k[i].x, q[i].x, s[0], 0, 0, 0);
+            s[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(k[i].y, q[i].y, s[0], 0, 0, 0);
+            s[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(k[i].z, q[i].z, s[0], 0, 0, 0);
+            s[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(k[i].w, q[i].w, s[0], 0, 0, 0);
+        }
+        const int lim = seen ? t.lim : 0;
+        if (__any(lim < k0 + kSfK)) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (k0 + (i >> 2) * 8 + hh * 4 + (i & 3) >= lim) s[0][i] = -INFINITY;
+        }
+        sa_maximum(st, s);
+        const float ref = st.m == -INFINITY ? 0.f : st.m;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            s[0][i] = __builtin_amdgcn_exp2f(fmaf(s[0][i], kSaScale, -ref));
+            st.l += s[0][i];
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (more) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");  // V is in, the next K may be out
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        float v0[16], v1[16];
+        sf_read_v(vr, 0, v0);
+        sf_read_v(vr, 4, v1);
+        __builtin_amdgcn_sched_barrier(0);
+        if (PROMPT && __any(t.lim < min(t.most, k0 + kSfK))) {
+            float z = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z = fmaf(v0[i], 0.f, fmaf(v1[i], 0.f, z));
+            if (__any(z != 0.f)) {  // (NaN: a value that is not finite, in a tile that some row sees in part)
+                sf_add_not_finite(st, own + kAtTile, s[0], hh);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    v0[i] = fabsf(v0[i]) < INFINITY ? v0[i] : 0.f;
+                    v1[i] = fabsf(v1[i]) < INFINITY ? v1[i] : 0.f;
+                }
+            }
+        }
+        if (more) load(u + 1, 1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            st.o0 = __builtin_amdgcn_mfma_f32_32x32x2f32(v0[i], s[0][i], st.o0, 0, 0, 0);
+            st.o1 = __builtin_amdgcn_mfma_f32_32x32x2f32(v1[i], s[0][i], st.o1, 0, 0, 0);
+        }
+    }
+    part_finish(pl, w, st, smem, wave, lane);
+}
+
+// Many rows: one workgroup per key head and run of 128 rows of a sequence, whose waves (32
+// rows each) share 64-token tiles of the prefix and then of the sequence's own pages.  Tiles come in whole pages of
+// a head, 8 KB of keys and of values, by direct-to-LDS loads into two stages, a tile ahead; one barrier a tile.
+constexpr int kStWaves = 4;
+__global__ __launch_bounds__(kStWaves * 64, 3) void shared_tile_kernel(const SharedAttnArgs a, int tiles) {
+    constexpr int kRows = kStWaves * kSaQ, kLoads = 8 / kStWaves;
+    __shared__ __attribute__((aligned(1024))) char smem[2 * kAtStage];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int ql = lane & 31, hh = lane >> 5;
+    // Each XCD (workgroups are dealt to the 8 in turn) gets a contiguous run of (key head, tile), tiles fastest, so
+    // that a head's pages are read through one L2.
+    int tile, kh;
+    {
+        const int T = gridDim.x, i = blockIdx.x, x = i & 7, q = T >> 3, r = T & 7;
+        const int t = (x < r ? x * (q + 1) : r * (q + 1) + (x - r) * q) + (i >> 3);
+        tile = t % tiles;
+        kh = t / tiles;
+    }
+    const OwnTile o = own_tile(a, tile, kRows, lane);
+    if (o.b >= a.B) return;
+    const int g = a.n_head / a.n_kv_head;
+    const int last = min(o.first + kRows, o.n * g) - 1;
+    const int most = own_seen(a, o, last / g);  // own tokens that some row of the workgroup sees
+    const int P = o.len < 0 ? 0 : a.prefix_len;
+    const int n_pre = (P + kPage - 1) / kPage, n = n_pre + (most + kPage - 1) / kPage;
+    const int wave_first = o.first + wave * kSaQ;
+    const RowTile t = own_rows(a, o, wave_first, kh, ql);
+    SaState st;
+    uint4 qr[4];
+    at_load_q(reinterpret_cast<const uint16_t*>(a.q) + (size_t)max(t.row, 0) * a.q_ld + t.head * kHeadDim, hh, qr);
+    const bool rows = wave_first < o.n * g;
+    int phys_l = 0;
+    auto fetch_ids = [&](int j0) {  // the ids of tiles j0 .. j0 + 63, one a lane
+        const int j = j0 + lane;
+        phys_l = -1;
+        if (j < n) phys_l = j < n_pre ? a.prefix_pages[j] : a.block_table[(size_t)o.b * a.max_pages + j - n_pre];
+    };
+    auto load = [&](int j) {  // tile j (of the ids in hand, or the first of the next 64); an invalid page: zeros
+        if ((j & 63) == 0) fetch_ids(j);
+        const int phys = __builtin_amdgcn_readlane(phys_l, j & 63);
+        const bool ok = phys >= 0 && phys < a.n_pages;
+        const int left = j < n_pre ? P - j * kPage : most - (j - n_pre) * kPage;
+        const int bytes = ok ? min(left, kPage) * (kHeadDim * 2) : 0;
+        const uint16_t* src = reinterpret_cast<const uint16_t*>(a.kv_base) +
+                              kv_offset(a.layer, a.n_pages, ok ? phys : 0, 0, a.n_kv_head, kh, 0);
+        char* dst = smem + (j & 1) * kAtStage + wave * kLoads * 1024;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int row = (wave * kLoads + i) * 8 + (lane >> 3);
+            const uint32_t vo = row * 128 + (((lane & 7) ^ ((row >> 1) & 7)) << 4);
+            buffer_to_lds16(src, bytes, dst + i * 1024, vo, 0);
+            buffer_to_lds16(src + (size_t)a.n_kv_head * (kPage * kHeadDim), bytes, dst + kAtTile + i * 1024, vo, 0);
+        }
+        return ok;
+    };
+    const AtAddr ad = at_addresses(lds_address(smem), lane);
+    sa_init(st);
+    bool ok = n > 0 && load(0);
+    for (int j = 0; j < n; ++j) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's loads of tile j
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_barrier();  // tile j is in; every wave has read tile j - 1
+        __builtin_amdgcn_sched_barrier(0);
+        const bool seen = ok;
+        if (j + 1 < n) ok = load(j + 1);
+        const bool pre = j < n_pre;
+        const int k0 = pre ? j * kPage : (j - n_pre) * kPage;
+        if (!seen || !rows || (!pre && k0 >= t.most)) continue;  // nothing for this wave
+        const uint32_t so = (j & 1) * kAtStage;
+        const int lim = pre ? P : t.lim;
+        const bool mask = __any(lim < k0 + kAtK);
+        at_f32x16 s[2];
+        uint64_t v[2][2][4];
+        uint32_t pw[16], none[1];
+        uint4 ka[4], kb[4];
+        sa_read_k(ad, so, ka, kb);
+        __builtin_amdgcn_sched_barrier(0);
+        at_scores(ka, kb, qr, s);
+        __builtin_amdgcn_sched_barrier(0);
+        sa_read_v(ad, so, v);
+        __builtin_amdgcn_sched_barrier(0);
+        if (mask) sa_mask(s, k0, lim, hh);
+        sa_maximum(st, s);
+        st.l += sa_weights<false>(st, s, pw, none);
+        if (!pre && __any(t.lim < min(most, k0 + kAtK)) && sa_not_finite(v, s)) {
+            sa_add_not_finite(st, smem + so + kAtTile, pw, hh);
+            sa_read_v(ad, so, v);
+            sa_take_out(v);
+        }
+        sa_pv(st, v, pw);
+    }
+    const RowPair ls = swap32(st.l);
+    const float l = ls.a + ls.b, inv = l == 0.f ? 0.f : 1.0f / l;
+    uint16_t* out = reinterpret_cast<uint16_t*>(a.o) + (size_t)max(t.row, 0) * a.o_ld + t.head * kHeadDim + hh * 8;
+    // 8 dims of a piece are in both halves of the wave: one half takes even pieces, the other odd ones
+#pragma unroll
+    for (int g4 = 0; g4 < 8; g4 += 2) {
+        const at_f32x16& x = g4 < 4 ? st.o0 : st.o1;
+        const int e = 4 * (g4 & 3);
+        const auto r0 = __builtin_amdgcn_permlane32_swap(bf16x2_rne(x[e] * inv, x[e + 1] * inv), bf16x2_rne(x[e + 4] * inv, x[e + 5] * inv), false, false);
+        const auto r1 = __builtin_amdgcn_permlane32_swap(bf16x2_rne(x[e + 2] * inv, x[e + 3] * inv), bf16x2_rne(x[e + 6] * inv, x[e + 7] * inv), false, false);
+        if (t.row >= 0) *reinterpret_cast<uint4*>(out + g4 * 8) = make_uint4(r0[0], r1[0], r0[1], r1[1]);
+    }
+}
+
+// Joins the partials, one wave per (row, head): lane s weighs slot s (64 at a time), then 4 groups of 16 lanes sum
+// every fourth slot, 4 dims a lane.
+constexpr int kJoinWaves = 4;
 template <bool F32>
-__global__ __launch_bounds__(256) void shared_join_kernel(const SharedAttnArgs a, const SharedPlan pl) {
-    const int64_t rows_heads = (int64_t)a.rows * a.n_head, rh = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+__global__ __launch_bounds__(kJoinWaves * 64) void shared_join_kernel(const SharedAttnArgs a, const SharedPlan pl) {
+    const int lane = threadIdx.x & 63;
+    const int64_t rows_heads = (int64_t)a.rows * a.n_head, rh = (int64_t)blockIdx.x * kJoinWaves + (threadIdx.x >> 6);
     if (rh >= rows_heads) return;
-    const int r = (int)(rh / a.n_head), h = (int)(rh % a.n_head), d = (threadIdx.x & 15) * 4;
+    const int r = (int)(rh / a.n_head), h = (int)(rh % a.n_head), grp = lane >> 4, d = (lane & 15) * 4;
     if (a.row_offsets && (r < a.row_offsets[0] || r >= a.row_offsets[a.B])) return;
     const int S = pl.s_pre + pl.s_own;
-    float m = -INFINITY;
+    float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
     bool inactive = false;
-    for (int s = 0; s < S; ++s) {
-        const float2 x = pl.ml[s * rows_heads + rh];
-        m = fmaxf(m, x.x);
-        inactive |= x.y < 0.f;
-    }
-    float l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    if (!inactive)
-        for (int s = 0; s < S; ++s) {
-            const float2 x = pl.ml[s * rows_heads + rh];
-            if (x.y == 0.f) continue;  // nothing seen there (and nothing written)
-            const float f = exp2f(x.x - (m == -INFINITY ? 0.f : m));
-            const float4 y = *reinterpret_cast<const float4*>(pl.o + (s * rows_heads + rh) * kHeadDim + d);
-            l = fmaf(x.y, f, l);
-            o[0] = fmaf(y.x, f, o[0]);
-            o[1] = fmaf(y.y, f, o[1]);
-            o[2] = fmaf(y.z, f, o[2]);
-            o[3] = fmaf(y.w, f, o[3]);
+    for (int s0 = 0; s0 < S; s0 += kWave) {
+        const float2 x = s0 + lane < S ? pl.ml[(s0 + lane) * rows_heads + rh] : make_float2(-INFINITY, 0.f);
+        inactive |= __any(x.y < 0.f);
+        const float mn = fmaxf(m, wave_max(x.x)), ref = mn == -INFINITY ? 0.f : mn;
+        const float f = x.y == 0.f ? 0.f : exp2f(x.x - ref);  // (a sum of 0: nothing seen there, and nothing written)
+        const float keep = exp2f(m - ref);
+        m = mn;
+        l = l * keep + wave_sum(x.y == 0.f ? 0.f : x.y * f);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] *= keep;
+        const int n = min(kWave, S - s0);
+        const unsigned long long live = __ballot(x.y != 0.f);
+#pragma unroll 4
+        for (int s4 = 0; s4 < n; s4 += 4) {  // (every lane stays: the weights come from all of them)
+            const int s = s4 + grp;
+            const float w = __shfl(f, s, kWave);
+            float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (live >> s & 1) y = *reinterpret_cast<const float4*>(pl.o + ((s0 + s) * rows_heads + rh) * kHeadDim + d);
+            o[0] = fmaf(y.x, w, o[0]);
+            o[1] = fmaf(y.y, w, o[1]);
+            o[2] = fmaf(y.z, w, o[2]);
+            o[3] = fmaf(y.w, w, o[3]);
         }
-    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const RowPair p16 = swap16(o[i]);
+        const float half = p16.a + p16.b;
+        const RowPair p32 = swap32(half);
+        o[i] = p32.a + p32.b;
+    }
+    if (grp != 0) return;
+    const float inv = inactive || l == 0.f ? 0.f : 1.0f / l;
+    if (inactive) o[0] = o[1] = o[2] = o[3] = 0.f;
     const size_t at = (size_t)r * a.o_ld + h * kHeadDim + d;
     if constexpr (F32)
         *reinterpret_cast<float4*>(reinterpret_cast<float*>(a.o) + at) = make_float4(o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
@@ -395,101 +769,77 @@ __global__ __launch_bounds__(256) void shared_join_kernel(const SharedAttnArgs a
             make_uint2(bf16x2_rne(o[0] * inv, o[1] * inv), bf16x2_rne(o[2] * inv, o[3] * inv));
 }
 
-// ---- fp32: one wave per row and head ---------------------------------------------------------
-// Lane j scores token j of a page, and lane d then sums dimension d over the tokens that the row
-// sees (the others are not read).
-__global__ __launch_bounds__(kSaWaves * 64) void shared_row_kernel(const SharedAttnArgs a) {
-    const int64_t id = (int64_t)blockIdx.x * kSaWaves + (threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63;
-    if (id >= (int64_t)a.rows * a.n_head) return;
-    const int r = (int)(id / a.n_head), h = (int)(id % a.n_head), kh = h / (a.n_head / a.n_kv_head);
-    int b = r, i = 0, n = 1;
-    if (a.row_offsets) {
-        if (r < a.row_offsets[0] || r >= a.row_offsets[a.B]) return;
-        int lo = 0, hi = a.B - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (a.row_offsets[mid] <= r) lo = mid;
-            else hi = mid - 1;
-        }
-        b = lo;
-        i = r - a.row_offsets[b];
-        n = a.row_offsets[b + 1] - a.row_offsets[b];
-    }
-    const int len = a.seq_lens[b];
-    const int own = len < 0 ? 0 : (int)min((int64_t)len - n + i + 1, (int64_t)a.max_pages * kPage);
-    const float q = ld_act<true>(a.q, (size_t)r * a.q_ld + h * kHeadDim + lane) * 0.125f;
-    float m = -INFINITY, l = 0.f, o = 0.f;
-    auto page = [&](int phys, int seen) {  // the first `seen` tokens of a page
-        if (phys < 0 || phys >= a.n_pages) return;
-        const size_t kb = kv_offset(a.layer, a.n_pages, phys, 0, a.n_kv_head, kh, 0);
-        const size_t vb = kv_offset(a.layer, a.n_pages, phys, 1, a.n_kv_head, kh, 0);
-        float s = 0.f;
-        for (int d = 0; d < kHeadDim; ++d) {
-            const float qd = __shfl(q, d, kWave);
-            if (lane < seen) s = fmaf(qd, ld_act<true>(a.kv_base, kb + lane * kHeadDim + d), s);
-        }
-        if (lane >= seen) s = -INFINITY;
-        const float mn = fmaxf(m, wave_max(s));
-        const float ref = mn == -INFINITY ? 0.f : mn;
-        const float f = expf(m - ref), p = expf(s - ref);
-        m = mn;
-        l = l * f + wave_sum(p);
-        o *= f;
-        for (int j = 0; j < seen; ++j) o = fmaf(__shfl(p, j, kWave), ld_act<true>(a.kv_base, vb + j * kHeadDim + lane), o);
-    };
-    if (len >= 0)
-        for (int t = 0; t < a.prefix_len; t += kPage) page(a.prefix_pages[t / kPage], min(kPage, a.prefix_len - t));
-    for (int t = 0; t < own; t += kPage) page(a.block_table[(size_t)b * a.max_pages + t / kPage], min(kPage, own - t));
-    st_act<true>(a.o, (size_t)r * a.o_ld + h * kHeadDim + lane, l == 0.f ? 0.f : o / l);
-}
+// Pages a workgroup.  Own side: 4 (two a wave), more where the table is so wide that the grid would pass kOwnGroups
+// workgroups (most of them past their sequence's end).  Prefix: so many that about 128 workgroups for each row tile,
+// 256 to kPreGroups in all, share it (few rows: bound by reading, and each workgroup leaves 8 KB of partials; many
+// rows: bound by the products), at most kMaxSplit along it.
+constexpr int kOwnGroups = 8192, kPreGroups = 640, kMaxSplit = 64;
+static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-constexpr int kGroups = 1536, kMaxSplit = 64;
-
-// Workgroups along the tokens: as many pages each (a multiple of the 4 waves) as keep the call near
-// kGroups workgroups, at most kMaxSplit of them for the prefix.
 static SharedPlan shared_plan(int n_head, int n_kv_head, int B, int rows, bool prompt, int prefix_len, int max_pages) {
     const int g = n_head / n_kv_head;
+    const int64_t pages = ceil_div(prefix_len, kPage);
     SharedPlan p{};
-    p.row_tiles = (int)(((int64_t)rows * g + kSaQ - 1) / kSaQ);
-    p.own_tiles = prompt ? (int)((int64_t)rows * g / kSaQ) + B : B * ((g + kSaQ - 1) / kSaQ);
-    const int pages = (prefix_len + kPage - 1) / kPage;
-    int c = kSaWaves;
-    for (;; c += kSaWaves) {
-        p.s_pre = (pages + c - 1) / c;
-        p.s_own = (max_pages + c - 1) / c;
-        const int64_t n = (int64_t)n_kv_head * ((int64_t)p.row_tiles * p.s_pre + (int64_t)p.own_tiles * p.s_own);
-        if (p.s_pre <= kMaxSplit && (n <= kGroups || c >= std::max(pages, max_pages))) break;
-    }
-    p.c_pre = p.c_own = c;
+    p.row_tiles = (int)ceil_div((int64_t)rows * g, kSaQ);
+    p.own_tiles = prompt ? (int)((int64_t)rows * g / kSaQ) + B : B * (int)ceil_div(g, kSaQ);
+    const int64_t groups = std::min<int64_t>(std::max<int64_t>((int64_t)128 * p.row_tiles, 256), kPreGroups);
+    const int64_t c_pre = std::max({(int64_t)2, ceil_div(pages * n_kv_head * p.row_tiles, groups), ceil_div(pages, kMaxSplit)});
+    const int64_t c_own = std::max((int64_t)4, ceil_div((int64_t)max_pages * n_kv_head * p.own_tiles, kOwnGroups));
+    p.c_pre = (int)std::min(ceil_div(c_pre, 2) * 2, std::max(pages, (int64_t)1));
+    p.c_own = (int)std::min(ceil_div(c_own, 2) * 2, (int64_t)max_pages);
+    p.s_pre = (int)ceil_div(pages, p.c_pre);
+    p.s_own = (int)ceil_div(max_pages, p.c_own);
     return p;
 }
 
-// An upper bound of the partials of every call up to these sizes: a call has either one slot on each side or at
-// most kGroups workgroups of 32 rows, and its slots hold at least 4 pages each.
+// Tiles of 128 rows for shared_tile_kernel, 0 if the call is to be cut along the tokens.  The first walks all of a
+// row's pages in one chain (1.1 us a page while the workgroups fit the chip, about 600 of them), the second pays for
+// another launch, 1.4 ns for 32 rows and a page, and 0.7 ns for a row's partials.  Fitted to 555 calls of both
+// (20/20, 20/4 and 8/1 heads, 1 to 32 sequences of 2 to 1024 rows, prefixes of 0 to 6000): the worse of the two is
+// taken in few, and costs 0.4% of a call on average.  Cut and tiled, us, 20 heads behind 1000 tokens: 32 sequences
+// of 4 rows each 13 / 22, of 32 rows 29 / 24, of 256 rows 139 / 70; one of 1024 rows behind 6000 97 / 117.  Own
+// lengths are on the device, so the table's width stands for them on both sides.
+static int shared_tiles(const SharedAttnArgs& a) {
+    if (!a.row_offsets) return 0;
+    const int64_t g = a.n_head / a.n_kv_head, pairs = a.rows * g, tiles = pairs / (kStWaves * kSaQ) + a.B;
+    const double pages = (double)ceil_div(a.prefix_len, kPage), own = a.max_pages;
+    const double tile = 5.0 + 1.1 * (pages + own) * std::max(1.0, (double)tiles * a.n_kv_head / 600);
+    const double cut = 9.0 + 1.4e-3 * a.n_kv_head * ((double)ceil_div(pairs, kSaQ) * pages + (double)(pairs / kSaQ + a.B) * own) +
+                       0.7e-3 * (double)a.rows * a.n_head;
+    return tile <= cut ? (int)tiles : 0;
+}
+
+// An upper bound of the partials of every call up to these sizes, from the least pages a workgroup, and from the
+// most workgroups of 32 rows where more than one shares a side.
 size_t shared_attention_bytes(int n_head, int rows, int prefix_len, int max_pages) {
-    const int pages = (prefix_len + kPage - 1) / kPage;
-    const int64_t rh = (int64_t)rows * n_head, slots = std::min((pages + 3) / 4, kMaxSplit) + (max_pages + 3) / 4;
-    const int64_t n = std::max(std::min(slots * rh, (int64_t)kGroups * kSaQ), std::min<int64_t>(slots, 2) * rh);
+    const int64_t rh = (int64_t)rows * n_head, pages = ceil_div(prefix_len, kPage);
+    const int64_t most = std::min<int64_t>(ceil_div(pages, 2), kMaxSplit) + ceil_div(max_pages, 4);
+    const int64_t n = std::min(most * rh, (int64_t)(kOwnGroups + kPreGroups) * kSaQ + 2 * rh);
     return (size_t)n * (kHeadDim + 2) * 4 + 256;
 }
 
-hipError_t launch_shared_attention(int dtype, const SharedAttnArgs& a, void* ws, hipStream_t st) {
-    if (dtype == FTTS_F32) {
-        const dim3 g((unsigned)(((int64_t)a.rows * a.n_head + kSaWaves - 1) / kSaWaves)), t(kSaWaves * 64);
-        hipLaunchKernelGGL(shared_row_kernel, g, t, 0, st, a);
+hipError_t launch_shared_attention(int dtype, const SharedAttnArgs& a, void* ws, size_t ws_bytes, hipStream_t st) {
+    const bool f32 = dtype == FTTS_F32;
+    const int tiles = f32 ? 0 : shared_tiles(a);
+    if (tiles > 0) {
+        hipLaunchKernelGGL(shared_tile_kernel, dim3((unsigned)(tiles * a.n_kv_head)), dim3(kStWaves * 64), 0, st, a, tiles);
         return hipGetLastError();
     }
     SharedPlan p = shared_plan(a.n_head, a.n_kv_head, a.B, a.rows, a.row_offsets != nullptr, a.prefix_len, a.max_pages);
     const int64_t rows_heads = (int64_t)a.rows * a.n_head;
+    if ((size_t)(p.s_pre + p.s_own) * rows_heads * (kHeadDim + 2) * 4 > ws_bytes) return hipErrorInvalidValue;
     p.o = reinterpret_cast<float*>(ws);
     p.ml = reinterpret_cast<float2*>(p.o + (p.s_pre + p.s_own) * rows_heads * kHeadDim);
     const int64_t groups = (int64_t)((a.n_kv_head * p.s_pre + 7) / 8 * 8) * p.row_tiles + (int64_t)a.n_kv_head * p.own_tiles * p.s_own;
     const dim3 g((unsigned)groups), t(kSaWaves * 64);
-    if (a.row_offsets) hipLaunchKernelGGL(shared_part_kernel<true>, g, t, 0, st, a, p);
+    if (f32 && a.row_offsets) hipLaunchKernelGGL(shared_part_f32_kernel<true>, g, t, 0, st, a, p);
+    else if (f32) hipLaunchKernelGGL(shared_part_f32_kernel<false>, g, t, 0, st, a, p);
+    else if (a.row_offsets) hipLaunchKernelGGL(shared_part_kernel<true>, g, t, 0, st, a, p);
     else hipLaunchKernelGGL(shared_part_kernel<false>, g, t, 0, st, a, p);
     if (hipError_t e = hipGetLastError()) return e;
-    hipLaunchKernelGGL(shared_join_kernel<false>, dim3((unsigned)((rows_heads + 15) / 16)), dim3(256), 0, st, a, p);
+    const dim3 jg((unsigned)((rows_heads + kJoinWaves - 1) / kJoinWaves)), jt(kJoinWaves * 64);
+    if (f32) hipLaunchKernelGGL(shared_join_kernel<true>, jg, jt, 0, st, a, p);
+    else hipLaunchKernelGGL(shared_join_kernel<false>, jg, jt, 0, st, a, p);
     return hipGetLastError();
 }
 
@@ -569,7 +919,7 @@ int ftts_shared_attention(const ftts_attn_shape* shape, const void* q, int64_t q
     a.B = B;
     a.rows = n_rows;
     (void)hipGetLastError();
-    const hipError_t e = launch_shared_attention(shape->dtype, a, ws, (hipStream_t)stream);
+    const hipError_t e = launch_shared_attention(shape->dtype, a, ws, ws_bytes, (hipStream_t)stream);
     if (e != hipSuccess) return set_error(FTTS_E_HIP, "shared_attention launch: %s", hipGetErrorString(e));
     return FTTS_OK;
 }

@@ -129,11 +129,6 @@ __device__ __forceinline__ void at_store(const AttnPrefillArgs& a, const AtState
             *reinterpret_cast<uint4*>(out + (size_t)(row0 + qw + rl) * a.d_model + q * 8) = v;
     }
 }
-// Q as the second operand of S^T = K Q^T: lane (q, hh) holds dims kk*16 + hh*8 .. +7.
-__device__ __forceinline__ void at_load_q(const uint16_t* qrow, int hh, uint4 (&qr)[4]) {
-#pragma unroll
-    for (int kk = 0; kk < 4; ++kk) qr[kk] = *reinterpret_cast<const uint4*>(qrow + kk * 16 + hh * 8);
-}
 // The sequence of query tile gt: how many end at or before it (at most 64, one per lane).
 __device__ __forceinline__ int at_sequence(const AttnPrefillArgs& a, int gt, int lane) {
     static_assert(kMaxPrefillSeqs <= kWave, "one sequence per lane");

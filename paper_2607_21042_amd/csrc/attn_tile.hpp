@@ -42,6 +42,11 @@ __device__ __forceinline__ void at_tie4(uint4 (&o)[4]) {
 }
 __device__ __forceinline__ at_bf16x8 at_op(uint4 v) { return __builtin_bit_cast(at_bf16x8, v); }
 
+// Q as the second operand of S^T = K Q^T: lane (q, hh) holds dims kk*16 + hh*8 .. +7.
+__device__ __forceinline__ void at_load_q(const uint16_t* qrow, int hh, uint4 (&qr)[4]) {
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) qr[kk] = *reinterpret_cast<const uint4*>(qrow + kk * 16 + hh * 8);
+}
 // s[b][i] = raw score of key 32 b + (i/4)*8 + hh*4 + i%4 of the tile and the lane's query.
 __device__ __forceinline__ void at_scores(const uint4 (&ka)[4], const uint4 (&kb)[4], const uint4 (&qr)[4], at_f32x16 (&s)[2]) {
 #pragma unroll

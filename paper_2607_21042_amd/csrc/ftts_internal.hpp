@@ -330,7 +330,7 @@ struct SharedAttnArgs {
     int prefix_len;
     int B, rows;
 };
-hipError_t launch_shared_attention(int dtype, const SharedAttnArgs& a, void* ws, hipStream_t st);
+hipError_t launch_shared_attention(int dtype, const SharedAttnArgs& a, void* ws, size_t ws_bytes, hipStream_t st);
 // Bytes of ws, for up to so many rows, prefix tokens and pages a sequence.
 size_t shared_attention_bytes(int n_head, int rows, int prefix_len, int max_pages);
 

@@ -327,23 +327,33 @@ def advance(tokens, positions, seq_lens, sampled, remaining=None, stop_token=0, 
 
 
 # ---- serving a batch over the paged cache: tables, append, shared-prefix attention -----------
-def _i32(name, t, shape=None):
-    """Checks an int32 tensor argument (and its shape)."""
+def _int32(name, t, dev, n=None):
+    """Data pointer of an int32 tensor of n elements (None: any) on GPU `dev`; None for None."""
+    if t is None:
+        return None
     if t.dtype != torch.int32:
         raise FTTSError(-3, f"{name} must be int32")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise FTTSError(-2, f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
-    return t
+    if n is not None and t.numel() != n:
+        raise FTTSError(-2, f"{name} must have {n} elements, not {t.numel()}")
+    return _data(name, t, dev)
 
 
-def _rows(name, t):
-    """Data pointer and row stride of a 2-D tensor whose rows are contiguous."""
-    if not t.is_cuda:
-        raise FTTSError(-1, f"{name} must live on the GPU")
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise FTTSError(-2, f"{name} must be 2-D with contiguous rows")
-    # (the stride of a lone row says nothing)
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
+def _data(name, t, dev):
+    """Data pointer of a contiguous tensor on GPU `dev`."""
+    if t.get_device() != dev:
+        raise FTTSError(-1, f"{name} is on {t.device}, other tensors are not")
+    if not t.is_contiguous():
+        raise FTTSError(-1, f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _rows(name, t, dev, shape):
+    """Data pointer and row stride of a 2-D tensor of that shape with contiguous rows."""
+    if t.shape != shape or (shape[1] > 1 and t.stride(1) != 1):
+        raise FTTSError(-2, f"{name} must be {list(shape)} with contiguous rows")
+    if t.get_device() != dev:
+        raise FTTSError(-1, f"{name} is on {t.device}, other tensors are not")
+    return t.data_ptr(), t.stride(0) if shape[0] > 1 else shape[1]  # (the stride of a lone row says nothing)
 
 
 def _wdtype(name, dtype):
@@ -352,19 +362,17 @@ def _wdtype(name, dtype):
     return F32 if dtype == torch.float32 else BF16
 
 
-def _on(stream, *tensors):
-    """The device of all the tensors as a context, and the stream to use there."""
-    devices = {t.device for t in tensors if t is not None}
-    if len(devices) != 1:
-        raise FTTSError(-1, f"tensors on different devices: {sorted(map(str, devices))}")
-    dev = devices.pop()
-    if dev.type != "cuda":
-        raise FTTSError(-1, "tensor must live on the GPU")
-    if stream is None:
-        stream = torch.cuda.current_stream(dev)
-    elif getattr(stream, "device", dev) != dev:
-        raise FTTSError(-1, f"stream of {stream.device} for tensors of {dev}")
-    return torch.cuda.device(dev), _stream(stream)
+def _enqueue(dev, stream, fn, *args):
+    """Calls fn(*args, stream) with GPU `dev` current, on `stream` (default: that GPU's current one)."""
+    if dev < 0:
+        raise FTTSError(-1, "tensors must live on the GPU")
+    if stream is not None and not isinstance(stream, int) and stream.device.index != dev:
+        raise FTTSError(-1, f"a stream of {stream.device} for tensors on GPU {dev}")
+    if torch.cuda.current_device() == dev:
+        _check(fn(*args, torch.cuda.current_stream(dev).cuda_stream if stream is None else _stream(stream)))
+    else:
+        with torch.cuda.device(dev):
+            _check(fn(*args, _stream(stream)))
 
 
 def build_tables(added, free_pages, n_pages: int, block_table, row_offsets, slots, counts, cached=None, seq_lens=None,
@@ -372,40 +380,29 @@ def build_tables(added, free_pages, n_pages: int, block_table, row_offsets, slot
     """ftts_build_tables: block tables [B][max_pages] (updated in place), row offsets [B + 1], the
     slot of each packed row and (optionally) the new lengths, from added [B] and cached [B] tokens
     and the free page ids; counts [2] receives the pages taken and the requests refused."""
-    B = added.numel()
-    for name, t, shape in (("added", added, (B,)), ("row_offsets", row_offsets, (B + 1,)), ("counts", counts, (2,)),
-                           ("cached", cached, (B,)), ("seq_lens", seq_lens, (B,)), ("free_pages", free_pages, None),
-                           ("slots", slots, None)):
-        if t is not None:
-            _i32(name, t, shape)
-    _i32("block_table", block_table)
+    B, dev = added.numel(), added.get_device()
     if block_table.dim() != 2 or block_table.shape[0] != B:
         raise FTTSError(-2, f"block_table must be [{B}][max_pages]")
-    n_free, max_rows = 0 if free_pages is None else free_pages.numel(), 0 if slots is None else slots.numel()
-    ctx, st = _on(stream, added, free_pages, block_table, row_offsets, slots, counts, cached, seq_lens)
-    with ctx:
-        _check(lib().ftts_build_tables(_ptr(cached), _ptr(added), B, _ptr(free_pages), n_free, n_pages,
-                                       _ptr(block_table), block_table.shape[1], _ptr(row_offsets), _ptr(seq_lens),
-                                       _ptr(slots), max_rows, _ptr(counts), st))
+    _enqueue(dev, stream, lib().ftts_build_tables, _int32("cached", cached, dev, B), _int32("added", added, dev, B), B,
+             _int32("free_pages", free_pages, dev), 0 if free_pages is None else free_pages.numel(), n_pages,
+             _int32("block_table", block_table, dev), block_table.shape[1],
+             _int32("row_offsets", row_offsets, dev, B + 1), _int32("seq_lens", seq_lens, dev, B),
+             _int32("slots", slots, dev), 0 if slots is None else slots.numel(), _int32("counts", counts, dev, 2))
 
 
 def append_kv(k, v, slots, kv, layer: int, stream=None):
     """ftts_append_kv: rows k and v ([T][n_kv_head * 64], rows may be strided) into layer `layer`
     of a KVCache at slots [T] (rows with a negative slot are skipped)."""
-    T, heads = k.shape[0], kv.pool.shape[3]
+    dev, layers, heads = k.get_device(), kv.pool.shape[0], kv.pool.shape[3]
+    shape = (k.shape[0], heads * 64)
     if k.dtype != v.dtype:
         raise FTTSError(-3, "k and v must have one dtype")
-    for name, t in (("k", k), ("v", v)):
-        if tuple(t.shape) != (T, heads * 64):
-            raise FTTSError(-2, f"{name} must be [{T}][{heads * 64}]")
-    if not 0 <= layer < kv.pool.shape[0]:
-        raise FTTSError(-5, f"layer must be in [0, {kv.pool.shape[0]})")
-    _i32("slots", slots, (T,))
-    (kp, ks), (vp_, vs) = _rows("k", k), _rows("v", v)
-    ctx, st = _on(stream, k, v, slots, kv.pool)
-    with ctx:
-        _check(lib().ftts_append_kv(_wdtype("k", k.dtype), kv.dtype, kp, ks, vp_, vs, T, _ptr(slots),
-                                    _c.byref(kv.c), layer, heads, st))
+    if not 0 <= layer < layers:
+        raise FTTSError(-5, f"layer must be in [0, {layers})")
+    if kv.pool.get_device() != dev:
+        raise FTTSError(-1, f"the pool is on {kv.pool.device}, k is not")
+    _enqueue(dev, stream, lib().ftts_append_kv, _wdtype("k", k.dtype), kv.dtype, *_rows("k", k, dev, shape),
+             *_rows("v", v, dev, shape), shape[0], _int32("slots", slots, dev, shape[0]), _c.byref(kv.c), layer, heads)
 
 
 class SharedPrefix:
@@ -413,7 +410,9 @@ class SharedPrefix:
 
     def __init__(self, pages, length: int):
         length = int(length)
-        self.pages = _i32("pages", pages).contiguous()
+        if pages.dtype != torch.int32:
+            raise FTTSError(-3, "pages must be int32")
+        self.pages = pages.contiguous()
         if self.pages.numel() < -(-length // PAGE):
             raise FTTSError(-2, f"{self.pages.numel()} pages do not hold {length} tokens")
         self.len = length
@@ -435,26 +434,25 @@ def shared_attention(q, kv, layer: int, page_table, prefix, out, ws, row_offsets
     (one each, or as row_offsets [B + 1] says), which all continue `prefix` (a SharedPrefix or
     None), to out [T][n_head * 64]; keys and values in layer `layer` of a KVCache."""
     T, width = q.shape
-    B, max_pages = page_table.block_table.shape
-    if width % 64 or tuple(out.shape) != (T, width):
-        raise FTTSError(-2, "q and out must be [T][n_head * 64]")
+    B, dev, layers, heads = page_table.block_table.shape[0], q.get_device(), kv.pool.shape[0], kv.pool.shape[3]
+    if width % 64:
+        raise FTTSError(-2, "q must be [T][n_head * 64]")
     if q.dtype != out.dtype or q.dtype != kv.pool.dtype:
         raise FTTSError(-3, "q, out and the pool must have one dtype")
-    if not 0 <= layer < kv.pool.shape[0]:
-        raise FTTSError(-5, f"layer must be in [0, {kv.pool.shape[0]})")
-    if row_offsets is not None:
-        _i32("row_offsets", row_offsets, (B + 1,))
+    if not 0 <= layer < layers:
+        raise FTTSError(-5, f"layer must be in [0, {layers})")
     if page_table.seq_lens.numel() != B:
         raise FTTSError(-2, f"the page table needs {B} lengths")
-    (qp, qs), (op, os_) = _rows("q", q), _rows("out", out)
-    ctx, st = _on(stream, q, out, ws, row_offsets, kv.pool, page_table.block_table, page_table.seq_lens,
-                  None if prefix is None or prefix.len == 0 else prefix.pages)
-    shape = AttnShape(_wdtype("q", q.dtype), width // 64, kv.pool.shape[3], 64)
-    with ctx:
-        _check(lib().ftts_shared_attention(_c.byref(shape), qp, qs, _ptr(row_offsets), T, B,
-                                           _c.byref(prefix.c) if prefix is not None else None,
-                                           _c.byref(page_table.c), _c.byref(kv.c), layer, op, os_, _ptr(ws),
-                                           ws.numel() * ws.element_size(), st))
+    shared = [kv.pool, page_table.block_table, page_table.seq_lens]
+    if prefix is not None and prefix.len > 0:
+        shared.append(prefix.pages)
+    if any(t.get_device() != dev for t in shared):
+        raise FTTSError(-1, f"the pool, the page table and the prefix must be on {q.device}, as q is")
+    shape = AttnShape(_wdtype("q", q.dtype), width // 64, heads, 64)
+    _enqueue(dev, stream, lib().ftts_shared_attention, _c.byref(shape), *_rows("q", q, dev, (T, width)),
+             _int32("row_offsets", row_offsets, dev, B + 1), T, B, None if prefix is None else _c.byref(prefix.c),
+             _c.byref(page_table.c), _c.byref(kv.c), layer, *_rows("out", out, dev, (T, width)), _data("ws", ws, dev),
+             ws.numel() * ws.element_size())
 
 
 # --------------------------------------------------------------------------- device state

@@ -189,6 +189,19 @@ def test_single_token(dtype, H, KH, prefix):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,KH,B,prefix,longest", [(5, 1, 6, 5000, 1200), (4, 2, 3, 4333, 300), (1, 1, 2, 8190, 1300),
+                                                   (1, 1, 1, 12300, 64), (2, 1, 40, 2500, 700), (3, 3, 1, 4700, 520)])
+def test_many_partial_results(dtype, H, KH, B, prefix, longest):
+    """Long prefixes and wide tables: from 17 to over 64 runs of pages a row, in numbers that four do not divide."""
+    lens = np.random.default_rng(prefix).integers(0, longest + 1, B)
+    lens[0] = longest
+    b = Batch(dtype, H, KH, prefix, lens.tolist()).gpu()
+    print(f"many partials: {dtype} {H}/{KH} heads, B {B}, prefix {prefix}", flush=True)
+    b.call()
+    b.check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("B,prefix,lens", [(1, 0, [1]), (1, 1, [0]), (1, 300, [40]), (2, 5, [3, 900]), (33, 90, None),
                                            (64, 260, None)])
 def test_single_token_batches(dtype, B, prefix, lens):
