@@ -62,6 +62,7 @@ hipError_t launch_gemv(int wdtype, int epi, bool ln, const GemvArgs& in, hipStre
         a.B = in.B - b0 < group ? in.B - b0 : group;
         a.act = in.act + (size_t)b0 * in.K;
         a.out = in.out + (size_t)b0 * in.out_stride;
+        if (in.hidden) a.hidden = in.hidden + (size_t)b0 * in.K;
         if (epi == EPI_QKV) {
             a.kv.seq_lens = in.kv.seq_lens + b0;
             a.kv.active = in.kv.active + b0;
