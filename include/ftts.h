@@ -476,6 +476,35 @@ int ftts_shared_attention(const ftts_attn_shape* shape, const void* q, int64_t q
                           int32_t layer, void* out, int64_t out_stride, void* ws, size_t ws_bytes,
                           void* stream);
 
+/* ---- the model behind a shared prefix --------------------------------------------------------
+ *
+ * One voice prompt, many sentences: the prompt's rows are prefilled once, as a sequence of its
+ * own (ftts_prefill with a block table of the prefix's pages), and every sequence continues it.
+ * Own tokens keep their own pages and slots from 0 on; pt and seq_lens count them alone.
+ */
+
+/* Bytes of workspace for ftts_prefill_shared / ftts_decode_step_shared (and, as it covers
+ * ftts_workspace_bytes, for the other calls on the same workspace).  Returns 0 for invalid
+ * arguments. */
+size_t ftts_shared_workspace_bytes(const ftts_config* cfg, int32_t max_batch, int32_t max_rows, int32_t prefix_len,
+                                   int32_t max_pages);
+
+/* ftts_prefill_ids for sequences that continue `prefix` (not NULL; len 0: none): their rows also
+ * see all of it.  Rows given as embeddings alone have text_lens of 0.  A row whose token has no
+ * valid page is not seen by later rows. */
+int ftts_prefill_shared(const ftts_weights* w, const ftts_shared_prefix* prefix, const void* cond_emb,
+                        const int32_t* cond_lens, const int32_t* text_ids, const int32_t* text_lens,
+                        int32_t text_vocab, int32_t text_pos0, int32_t B, const ftts_page_table* pt,
+                        const ftts_kv_pool* kv, float* last_logits, void* ws, size_t ws_bytes, void* stream);
+
+/* ftts_decode_step_hidden (hidden_out may be NULL) for sequences that continue `prefix`; an own
+ * length of 0 is a sequence's first token right behind it.  One kernel per phase: FTTS_E_UNSUPPORTED
+ * where the persistent step is forced. */
+int ftts_decode_step_shared(const ftts_weights* w, const ftts_shared_prefix* prefix, const int32_t* tokens,
+                            const int32_t* positions, const ftts_page_table* pt, const ftts_kv_pool* kv,
+                            float* logits_out, float* hidden_out, int32_t* sampled_out, const float* uniforms,
+                            const ftts_sampling* samp, int32_t B, void* ws, size_t ws_bytes, void* stream);
+
 /* ---- Semantic-to-Mel flow-matching DiT: one guided Euler step ------------------------
  *
  * Sec. II-A: the Semantic-to-Mel module is conditional flow matching with a

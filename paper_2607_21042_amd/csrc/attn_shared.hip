@@ -74,7 +74,8 @@ __device__ __forceinline__ OwnTile own_tile(const SharedAttnArgs& a, int tile, i
         t.n = __builtin_amdgcn_readlane(rows, t.b);
         t.first = (tile - (t.b ? __builtin_amdgcn_readlane(end, t.b - 1) : 0)) * size;
     }
-    t.len = a.seq_lens[t.b];
+    t.len = a.seq_lens[t.b] + a.len_add;
+    if (a.active && !a.active[t.b]) t.len = -1;
     return t;
 }
 // Own tokens that the i-th row of the sequence sees.
@@ -352,7 +353,7 @@ __device__ __forceinline__ void part_finish(const SharedPlan& pl, const PartWork
 // the next page's K (V) on its way once this one's is in registers; no barrier in the loop.  The weights go into the
 // products as bf16 and what their rounding left, so that only the output is rounded.  PROMPT: several rows a
 // sequence, so a tile's rows may see different tokens.
-template <bool PROMPT>
+template <bool PROMPT, bool Q32>
 __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_kernel(const SharedAttnArgs a, const SharedPlan pl) {
     __shared__ __attribute__((aligned(1024))) char smem[kSaWaves * kAtStage];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hh = lane >> 5;
@@ -379,7 +380,17 @@ __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_kernel(const Sha
         return ok;
     };
     uint4 qr[4];
-    at_load_q(reinterpret_cast<const uint16_t*>(a.q) + (size_t)max(t.row, 0) * a.q_ld + t.head * kHeadDim, hh, qr);
+    const size_t q0 = (size_t)max(t.row, 0) * a.q_ld + t.head * kHeadDim;
+    if constexpr (Q32) {  // (rounded to bf16, as the prefill's queries are)
+        const float* qp = reinterpret_cast<const float*>(a.q) + q0 + hh * 8;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+            const float4 x = *reinterpret_cast<const float4*>(qp + kk * 16), y = *reinterpret_cast<const float4*>(qp + kk * 16 + 4);
+            qr[kk] = make_uint4(bf16x2_rne(x.x, x.y), bf16x2_rne(x.z, x.w), bf16x2_rne(y.x, y.y), bf16x2_rne(y.z, y.w));
+        }
+    } else {
+        at_load_q(reinterpret_cast<const uint16_t*>(a.q) + q0, hh, qr);
+    }
     const AtAddr ad = at_addresses(lds_address(own), lane);
     SaState st;
     sa_init(st);
@@ -820,6 +831,7 @@ size_t shared_attention_bytes(int n_head, int rows, int prefix_len, int max_page
 
 hipError_t launch_shared_attention(int dtype, const SharedAttnArgs& a, void* ws, size_t ws_bytes, hipStream_t st) {
     const bool f32 = dtype == FTTS_F32;
+    if (a.row_offsets && (a.q_f32 || a.o_f32)) return hipErrorInvalidValue;  // (the decode step's forms)
     const int tiles = f32 ? 0 : shared_tiles(a);
     if (tiles > 0) {
         hipLaunchKernelGGL(shared_tile_kernel, dim3((unsigned)(tiles * a.n_kv_head)), dim3(kStWaves * 64), 0, st, a, tiles);
@@ -834,11 +846,12 @@ hipError_t launch_shared_attention(int dtype, const SharedAttnArgs& a, void* ws,
     const dim3 g((unsigned)groups), t(kSaWaves * 64);
     if (f32 && a.row_offsets) hipLaunchKernelGGL(shared_part_f32_kernel<true>, g, t, 0, st, a, p);
     else if (f32) hipLaunchKernelGGL(shared_part_f32_kernel<false>, g, t, 0, st, a, p);
-    else if (a.row_offsets) hipLaunchKernelGGL(shared_part_kernel<true>, g, t, 0, st, a, p);
-    else hipLaunchKernelGGL(shared_part_kernel<false>, g, t, 0, st, a, p);
+    else if (a.row_offsets) hipLaunchKernelGGL((shared_part_kernel<true, false>), g, t, 0, st, a, p);
+    else if (a.q_f32) hipLaunchKernelGGL((shared_part_kernel<false, true>), g, t, 0, st, a, p);
+    else hipLaunchKernelGGL((shared_part_kernel<false, false>), g, t, 0, st, a, p);
     if (hipError_t e = hipGetLastError()) return e;
     const dim3 jg((unsigned)((rows_heads + kJoinWaves - 1) / kJoinWaves)), jt(kJoinWaves * 64);
-    if (f32) hipLaunchKernelGGL(shared_join_kernel<true>, jg, jt, 0, st, a, p);
+    if (f32 || a.o_f32) hipLaunchKernelGGL(shared_join_kernel<true>, jg, jt, 0, st, a, p);
     else hipLaunchKernelGGL(shared_join_kernel<false>, jg, jt, 0, st, a, p);
     return hipGetLastError();
 }

@@ -121,6 +121,14 @@ int check_kv(const ftts_page_table* pt, const ftts_kv_pool* kv, bool need_seq_le
     return FTTS_OK;
 }
 
+int check_prefix(const ftts_shared_prefix* p) {
+    if (!p) return fail(FTTS_E_INVALID_ARG, "shared prefix is NULL");
+    if (p->len < 0 || p->len > FTTS_MAX_SHARED_PREFIX)
+        return fail(FTTS_E_RANGE, "shared prefix length must be in [0, %d]", FTTS_MAX_SHARED_PREFIX);
+    if (p->len > 0 && !p->pages) return fail(FTTS_E_INVALID_ARG, "shared prefix pages is NULL");
+    return FTTS_OK;
+}
+
 int check_sampling(const ftts_sampling* s, int V, const float* uniforms) {
     if (!s) return fail(FTTS_E_INVALID_ARG, "sampling is NULL");
     if (s->top_k < 1 || s->top_k > FTTS_MAX_TOP_K || s->top_k > V)
@@ -260,6 +268,38 @@ size_t prefill_bytes(const ftts_config& c, int B, int M, PrefillWs* out, char* b
     return off;
 }
 
+// What a call behind a shared prefix needs after its own regions: its sequences' offsets and lengths on the device
+// (prefill), and the attention's partials.
+struct SharedWs {
+    int32_t *row_offsets, *lens;
+    void* attn;
+    size_t attn_bytes;
+};
+size_t shared_bytes(const ftts_config& c, size_t off, int rows, int prefix_len, int max_pages, SharedWs* out, char* base) {
+    auto take = [&](size_t n) { size_t o = off; off += round256(n); return base ? base + o : nullptr; };
+    char* cu = take((FTTS_MAX_BATCH + 1) * 4);
+    char* lens = take(FTTS_MAX_BATCH * 4);
+    const size_t n = shared_attention_bytes(c.n_head, rows, prefix_len, max_pages);
+    char* attn = take(n);
+    if (out) *out = SharedWs{(int32_t*)cu, (int32_t*)lens, attn, n};
+    return off;
+}
+SharedAttnArgs shared_args(const ftts_config& c, const ftts_shared_prefix* prefix, const ftts_page_table* pt,
+                           const ftts_kv_pool* kv, int B, int rows) {
+    SharedAttnArgs a{};
+    a.kv_base = kv->base;
+    a.n_pages = kv->n_pages;
+    a.n_head = a.n_kv_head = c.n_head;
+    a.max_pages = pt->max_pages;
+    a.block_table = pt->block_table;
+    a.prefix_pages = prefix->len > 0 ? prefix->pages : nullptr;
+    a.prefix_len = prefix->len;
+    a.B = B;
+    a.rows = rows;
+    return a;
+}
+int shared_dtype(const ftts_config& c) { return c.wdtype == FTTS_F32 ? FTTS_F32 : FTTS_BF16; }
+
 int g_decode_path = 0;  // 0 automatic, 1 kernel per phase, 2 persistent step
 
 // Per-layer pointers of one kind, if they sit at a fixed stride.
@@ -349,7 +389,8 @@ GemvArgs gemv_args(const ftts_linear& L, int N, int K, int B, const float* act, 
 // the MFMA linears, with each LayerNorm folded into the linear that reads it (the
 // residual updates leave per-tile row statistics behind).  Attention writes bf16
 // for the out-projection and FC1's GELU output is bf16 for FC2.
-int decode_batched(const ftts_weights* w, int B, const DecodeWs& W, const KvAppend& kva, AttnDecodeArgs at,
+template <typename Attend>
+int decode_batched(const ftts_weights* w, int B, const DecodeWs& W, const KvAppend& kva, const Attend& attend,
                    float* logits_out, float* hidden_out, int32_t* sampled_out, const float* uniforms,
                    const ftts_sampling* samp, hipStream_t st) {
     const ftts_config& c = w->cfg;
@@ -381,15 +422,13 @@ int decode_batched(const ftts_weights* w, int B, const DecodeWs& W, const KvAppe
         g.ln_stats = W.stats;
         return g;
     };
-    at.o_bf16 = W.o16;
     for (int l = 0; l < c.n_layer; ++l) {
         const ftts_layer& L = w->layers[l];
         BgemmArgs g = normed(lin(L.qkv, 3 * d, d, nullptr, W.qkv, nullptr, 3 * d), L.ln1_g, L.ln1_b);
         g.kv = kva;
         g.kv.layer = l;
         if ((e = launch_bgemm(c.wdtype, EPI_QKV, g, st)) != hipSuccess) return hip_fail(e, "ln1 + qkv");
-        at.layer = l;
-        if ((e = launch_attn_decode(c.wdtype, at, B, st)) != hipSuccess) return hip_fail(e, "attention");
+        if ((e = attend(l)) != hipSuccess) return hip_fail(e, "attention");
         g = lin(L.out, d, d, W.o16, W.x, nullptr, d);
         g.stats_out = W.stats;
         if ((e = launch_bgemm(c.wdtype, EPI_RESID, g, st)) != hipSuccess) return hip_fail(e, "out-proj");
@@ -521,7 +560,7 @@ int set_error(int code, const char* fmt, ...) {
 int decode_step(const ftts_weights* w, const int32_t* tokens, const int32_t* positions, const ftts_page_table* pt,
                 const ftts_kv_pool* kv, float* logits_out, float* hidden_out, int32_t* sampled_out,
                 const float* uniforms, const ftts_sampling* samp, int32_t B, void* ws, size_t ws_bytes, void* stream,
-                int (*prepare)(void* ws, hipStream_t st)) {
+                int (*prepare)(void* ws, hipStream_t st), const ftts_shared_prefix* prefix) {
     TRY(check_weights(w));
     if (reinterpret_cast<uintptr_t>(hidden_out) % 16) return fail(FTTS_E_ALIGN, "hidden_out must be 16-byte aligned");
     const ftts_config& c = w->cfg;
@@ -531,7 +570,12 @@ int decode_step(const ftts_weights* w, const int32_t* tokens, const int32_t* pos
     TRY(check_kv(pt, kv, true));
     TRY(check_sampling(samp, c.vocab, uniforms));
     TRY(check_ptr(ws, "workspace"));
-    const size_t need = decode_bytes(c, B, nullptr, nullptr);
+    SharedWs S{};
+    size_t need = decode_bytes(c, B, nullptr, nullptr);
+    if (prefix) {
+        TRY(check_prefix(prefix));
+        need = shared_bytes(c, need, B, prefix->len, pt->max_pages, &S, reinterpret_cast<char*>(ws));
+    }
     if (ws_bytes < need) return fail(FTTS_E_WORKSPACE, "workspace too small: %zu < %zu", ws_bytes, need);
 
     hipStream_t st = (hipStream_t)stream;
@@ -541,9 +585,10 @@ int decode_step(const ftts_weights* w, const int32_t* tokens, const int32_t* pos
     const int d = c.d_model, H = c.n_head, F = c.d_ff, V = c.vocab;
 
     mega::Args ma{};
-    const bool mega_ok = g_decode_path != 1 && mega_args(w, B, &ma);
+    const bool mega_ok = g_decode_path != 1 && !prefix && mega_args(w, B, &ma);
     if (g_decode_path == 2 && !mega_ok)
-        return fail(FTTS_E_UNSUPPORTED, "the persistent decode step does not take this model/batch/device");
+        return fail(FTTS_E_UNSUPPORTED, "the persistent decode step does not take this model/batch/device%s",
+                    prefix ? " behind a shared prefix" : "");
     if (mega_ok) {
         MegaWs M;
         mega_bytes(&M, reinterpret_cast<char*>(ws));
@@ -604,7 +649,27 @@ int decode_step(const ftts_weights* w, const int32_t* tokens, const int32_t* pos
     at.active = W.active;
     at.o = W.o;
     at.o_stride = d;
-    if (W.stats) return decode_batched(w, B, W, kva, at, logits_out, hidden_out, sampled_out, uniforms, samp, st);
+    if (W.stats) at.o_bf16 = W.o16;
+
+    SharedAttnArgs sa{};
+    if (prefix) {
+        sa = shared_args(c, prefix, pt, kv, B, B);
+        sa.q = W.qkv;
+        sa.q_ld = 3 * d;
+        sa.o = W.stats ? (void*)W.o16 : (void*)W.o;
+        sa.o_ld = d;
+        sa.seq_lens = pt->seq_lens;
+        sa.len_add = 1;
+        sa.active = W.active;
+        sa.q_f32 = true;
+        sa.o_f32 = !W.stats;
+    }
+    auto attend = [&](int l) {
+        at.layer = sa.layer = l;
+        return prefix ? launch_shared_attention(shared_dtype(c), sa, S.attn, S.attn_bytes, st)
+                      : launch_attn_decode(c.wdtype, at, B, st);
+    };
+    if (W.stats) return decode_batched(w, B, W, kva, attend, logits_out, hidden_out, sampled_out, uniforms, samp, st);
 
     for (int l = 0; l < c.n_layer; ++l) {
         const ftts_layer& L = w->layers[l];
@@ -615,8 +680,7 @@ int decode_step(const ftts_weights* w, const int32_t* tokens, const int32_t* pos
         g.kv = kva;
         g.kv.layer = l;
         if ((e = launch_gemv(c.wdtype, EPI_QKV, true, g, st)) != hipSuccess) return hip_fail(e, "qkv");
-        at.layer = l;
-        if ((e = launch_attn_decode(c.wdtype, at, B, st)) != hipSuccess) return hip_fail(e, "attention");
+        if ((e = attend(l)) != hipSuccess) return hip_fail(e, "attention");
         g = gemv_args(L.out, d, d, B, W.o, W.x, d);
         if ((e = launch_gemv(c.wdtype, EPI_RESID, false, g, st)) != hipSuccess) return hip_fail(e, "out-proj");
         g = gemv_args(L.fc1, F, d, B, W.x, W.h, F);
@@ -647,7 +711,7 @@ int ftts_decode_step(const ftts_weights* w, const int32_t* tokens, const int32_t
                      const float* uniforms, const ftts_sampling* samp, int32_t B, void* ws, size_t ws_bytes,
                      void* stream) {
     return decode_step(w, tokens, positions, pt, kv, logits_out, nullptr, sampled_out, uniforms, samp, B, ws,
-                       ws_bytes, stream, nullptr);
+                       ws_bytes, stream, nullptr, nullptr);
 }
 
 int ftts_decode_step_hidden(const ftts_weights* w, const int32_t* tokens, const int32_t* positions,
@@ -655,7 +719,29 @@ int ftts_decode_step_hidden(const ftts_weights* w, const int32_t* tokens, const 
                             int32_t* sampled_out, const float* uniforms, const ftts_sampling* samp, int32_t B,
                             void* ws, size_t ws_bytes, void* stream) {
     return decode_step(w, tokens, positions, pt, kv, logits_out, hidden_out, sampled_out, uniforms, samp, B, ws,
-                       ws_bytes, stream, nullptr);
+                       ws_bytes, stream, nullptr, nullptr);
+}
+
+int ftts_decode_step_shared(const ftts_weights* w, const ftts_shared_prefix* prefix, const int32_t* tokens,
+                            const int32_t* positions, const ftts_page_table* pt, const ftts_kv_pool* kv,
+                            float* logits_out, float* hidden_out, int32_t* sampled_out, const float* uniforms,
+                            const ftts_sampling* samp, int32_t B, void* ws, size_t ws_bytes, void* stream) {
+    TRY(check_prefix(prefix));
+    return decode_step(w, tokens, positions, pt, kv, logits_out, hidden_out, sampled_out, uniforms, samp, B, ws,
+                       ws_bytes, stream, nullptr, prefix);
+}
+
+size_t ftts_shared_workspace_bytes(const ftts_config* cfg, int32_t max_batch, int32_t max_rows, int32_t prefix_len,
+                                   int32_t max_pages) {
+    const size_t n = ftts_workspace_bytes(cfg, max_batch, max_rows);
+    if (n == 0) return 0;
+    if (prefix_len < 0 || prefix_len > FTTS_MAX_SHARED_PREFIX || max_pages < 1 || max_pages > kMaxPages ||
+        max_rows > (1 << 24)) {
+        fail(FTTS_E_RANGE, "prefix_len must be in [0, %d], max_pages in [1, %d], max_rows at most 2^24",
+             FTTS_MAX_SHARED_PREFIX, kMaxPages);
+        return 0;
+    }
+    return shared_bytes(*cfg, n, std::max(max_batch, max_rows), prefix_len, max_pages, nullptr, nullptr);
 }
 
 // Where the prefill's input rows come from: ready embeddings, or the model's
@@ -670,7 +756,7 @@ struct PrefixSource {
 
 static int prefill(const ftts_weights* w, const PrefixSource& src, const int32_t* lens, int32_t B,
                    const ftts_page_table* pt, const ftts_kv_pool* kv, float* last_logits, void* ws, size_t ws_bytes,
-                   void* stream) {
+                   void* stream, const ftts_shared_prefix* prefix) {
     const ftts_config& c = w->cfg;
     TRY(check_kv(pt, kv, false));
     TRY(check_ptr(ws, "workspace"));
@@ -688,7 +774,9 @@ static int prefill(const ftts_weights* w, const PrefixSource& src, const int32_t
         seqs.cu[b + 1] = (int)M;
     }
     PrefillWs P;
-    const size_t need = prefill_bytes(c, B, (int)M, &P, reinterpret_cast<char*>(ws));
+    SharedWs S{};
+    size_t need = prefill_bytes(c, B, (int)M, &P, reinterpret_cast<char*>(ws));
+    if (prefix) need = shared_bytes(c, need, (int)M, prefix->len, pt->max_pages, &S, reinterpret_cast<char*>(ws));
     if (ws_bytes < need) return fail(FTTS_E_WORKSPACE, "workspace too small: %zu < %zu", ws_bytes, need);
 
     hipStream_t st = (hipStream_t)stream;
@@ -731,6 +819,17 @@ static int prefill(const ftts_weights* w, const PrefixSource& src, const int32_t
     ap.d_model = d;
     ap.n_head = c.n_head;
     ap.seqs = seqs;
+    SharedAttnArgs sa{};
+    if (prefix) {
+        if ((e = launch_row_offsets(seqs, S.row_offsets, S.lens, st)) != hipSuccess) return hip_fail(e, "row offsets");
+        sa = shared_args(c, prefix, pt, kv, B, Mi);
+        sa.q = P.qkv;
+        sa.q_ld = 3 * d;
+        sa.o = P.a;
+        sa.o_ld = d;
+        sa.seq_lens = S.lens;
+        sa.row_offsets = S.row_offsets;
+    }
 
     const GemmPlan p_qkv = gemm_plan(c.wdtype, Mi, 3 * d, d), p_out = gemm_plan(c.wdtype, Mi, d, d);
     const GemmPlan p_fc1 = gemm_plan(c.wdtype, Mi, F, d), p_fc2 = gemm_plan(c.wdtype, Mi, d, F);
@@ -738,7 +837,7 @@ static int prefill(const ftts_weights* w, const PrefixSource& src, const int32_t
     // (16-bit): after its QKV product it goes on with the B last rows, or ends there without
     // logits.  The kernels after QKV, all rows and last rows, traced: 380 and 54 us for 32
     // prefixes of 10,827 rows in all, 50 and 38 us for one of 256 rows.
-    const bool trim = c.wdtype != FTTS_F32;
+    const bool trim = c.wdtype != FTTS_F32 && !prefix;
     float* x = P.x;
     for (int l = 0; l < c.n_layer; ++l) {
         const ftts_layer& L = w->layers[l];
@@ -762,14 +861,18 @@ static int prefill(const ftts_weights* w, const PrefixSource& src, const int32_t
         g.kv = kva;
         g.kv.layer = l;
         if ((e = launch_gemm(c.wdtype, EPI_QKV, g, p_qkv, st)) != hipSuccess) return hip_fail(e, "qkv gemm");
+        if (prefix && l == c.n_layer - 1 && !last_logits) break;
         if (last) {
             if (!last_logits) break;
             if ((e = launch_attn_last(ap, st)) != hipSuccess) return hip_fail(e, "prefill attention");
             if ((e = launch_gather_rows(P.x, d, seqs, P.xlast, st)) != hipSuccess) return hip_fail(e, "gather");
             x = P.xlast;
             g.M = B;
-        } else if ((e = launch_attn_prefill(c.wdtype, ap, st)) != hipSuccess) {
-            return hip_fail(e, "prefill attention");
+        } else {
+            sa.layer = l;
+            e = prefix ? launch_shared_attention(shared_dtype(c), sa, S.attn, S.attn_bytes, st)
+                       : launch_attn_prefill(c.wdtype, ap, st);
+            if (e != hipSuccess) return hip_fail(e, "prefill attention");
         }
         auto plan = [&](const GemmPlan& p) { return last ? gemm_plan(c.wdtype, B, g.N, g.K) : p; };
         g.w = L.out.w;
@@ -826,13 +929,13 @@ int ftts_prefill(const ftts_weights* w, const void* prefix_emb, const int32_t* l
     if (!lens) return fail(FTTS_E_INVALID_ARG, "lens is NULL");
     PrefixSource src{};
     src.emb = prefix_emb;
-    return prefill(w, src, lens, B, pt, kv, last_logits, ws, ws_bytes, stream);
+    return prefill(w, src, lens, B, pt, kv, last_logits, ws, ws_bytes, stream, nullptr);
 }
 
-int ftts_prefill_ids(const ftts_weights* w, const void* cond_emb, const int32_t* cond_lens, const int32_t* text_ids,
-                     const int32_t* text_lens, int32_t text_vocab, int32_t text_pos0, int32_t B,
-                     const ftts_page_table* pt, const ftts_kv_pool* kv, float* last_logits, void* ws,
-                     size_t ws_bytes, void* stream) {
+static int prefill_ids(const ftts_weights* w, const void* cond_emb, const int32_t* cond_lens, const int32_t* text_ids,
+                       const int32_t* text_lens, int32_t text_vocab, int32_t text_pos0, int32_t B,
+                       const ftts_page_table* pt, const ftts_kv_pool* kv, float* last_logits, void* ws,
+                       size_t ws_bytes, void* stream, const ftts_shared_prefix* prefix) {
     TRY(check_weights(w));
     const ftts_config& c = w->cfg;
     if (B < 1 || B > FTTS_MAX_BATCH) return fail(FTTS_E_SHAPE, "B must be in [1, %d]", FTTS_MAX_BATCH);
@@ -861,7 +964,24 @@ int ftts_prefill_ids(const ftts_weights* w, const void* cond_emb, const int32_t*
     src.text_ids = text_ids;
     src.text_vocab = text_vocab;
     src.text_pos0 = text_pos0;
-    return prefill(w, src, lens, B, pt, kv, last_logits, ws, ws_bytes, stream);
+    return prefill(w, src, lens, B, pt, kv, last_logits, ws, ws_bytes, stream, prefix);
+}
+
+int ftts_prefill_ids(const ftts_weights* w, const void* cond_emb, const int32_t* cond_lens, const int32_t* text_ids,
+                     const int32_t* text_lens, int32_t text_vocab, int32_t text_pos0, int32_t B,
+                     const ftts_page_table* pt, const ftts_kv_pool* kv, float* last_logits, void* ws,
+                     size_t ws_bytes, void* stream) {
+    return prefill_ids(w, cond_emb, cond_lens, text_ids, text_lens, text_vocab, text_pos0, B, pt, kv, last_logits, ws,
+                       ws_bytes, stream, nullptr);
+}
+
+int ftts_prefill_shared(const ftts_weights* w, const ftts_shared_prefix* prefix, const void* cond_emb,
+                        const int32_t* cond_lens, const int32_t* text_ids, const int32_t* text_lens,
+                        int32_t text_vocab, int32_t text_pos0, int32_t B, const ftts_page_table* pt,
+                        const ftts_kv_pool* kv, float* last_logits, void* ws, size_t ws_bytes, void* stream) {
+    TRY(check_prefix(prefix));
+    return prefill_ids(w, cond_emb, cond_lens, text_ids, text_lens, text_vocab, text_pos0, B, pt, kv, last_logits, ws,
+                       ws_bytes, stream, prefix);
 }
 
 }  // extern "C"

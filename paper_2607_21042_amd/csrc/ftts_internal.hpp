@@ -309,6 +309,8 @@ hipError_t launch_advance(int32_t* tokens, int32_t* positions, int32_t* seq_lens
 // slots[m] of every packed row (KvAppend::slots), and count[0 .. n_count) = 0.
 hipError_t launch_prefill_setup(const SeqTable& seqs, const int32_t* block_table, int max_pages, int n_pages, int M,
                                 int32_t* slots, uint32_t* count, size_t n_count, hipStream_t st);
+// row_offsets[0 .. n] and lens[0 .. n) of packed sequences.
+hipError_t launch_row_offsets(const SeqTable& seqs, int32_t* row_offsets, int32_t* lens, hipStream_t st);
 hipError_t launch_fill_u32(uint32_t* p, size_t n, uint32_t v, hipStream_t st);
 hipError_t launch_bgemm(int wdtype, int epi, const BgemmArgs& a, hipStream_t st);
 int bgemm_splits(int wdtype, int N, int K, bool ln);
@@ -329,6 +331,10 @@ struct SharedAttnArgs {
     const int32_t* prefix_pages;
     int prefix_len;
     int B, rows;
+    // decode step: own lengths without the new token, its activity flags, fp32 queries over a 16-bit pool and fp32 outputs
+    int len_add;
+    const int32_t* active;        // [B], or null: all
+    bool q_f32, o_f32;            // (16-bit pool; an fp32 pool has both in fp32)
 };
 hipError_t launch_shared_attention(int dtype, const SharedAttnArgs& a, void* ws, size_t ws_bytes, hipStream_t st);
 // Bytes of ws, for up to so many rows, prefix tokens and pages a sequence.

@@ -225,6 +225,18 @@ hipError_t launch_prefill_setup(const SeqTable& seqs, const int32_t* block_table
     return hipGetLastError();
 }
 
+__global__ void row_offsets_kernel(SeqTable seqs, int32_t* row_offsets, int32_t* lens) {
+    const int b = threadIdx.x;
+    if (b <= seqs.n) row_offsets[b] = seqs.cu[b];
+    if (b < seqs.n) lens[b] = seqs.cu[b + 1] - seqs.cu[b];
+}
+
+hipError_t launch_row_offsets(const SeqTable& seqs, int32_t* row_offsets, int32_t* lens, hipStream_t st) {
+    static_assert(kMaxPrefillSeqs < 128, "one thread an offset");
+    hipLaunchKernelGGL(row_offsets_kernel, dim3(1), dim3(128), 0, st, seqs, row_offsets, lens);
+    return hipGetLastError();
+}
+
 // ---- row copies ----------------------------------------------------------------------------
 __global__ void gather_last_kernel(const float* x, int d, SeqTable seqs, float* out) {
     const int b = blockIdx.x;

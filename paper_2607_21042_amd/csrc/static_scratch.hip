@@ -93,5 +93,5 @@ extern "C" int ftts_decode_step_static(const ftts_weights* w, const int32_t* tok
     const int rc = device_scratch(&ptr, &dev);
     if (rc != FTTS_OK) return rc;
     return ftts::decode_step(w, tokens, positions, pt, kv, logits_out, nullptr, sampled_out, uniforms, samp, B, ptr,
-                             kScratchBytes, stream, prepare_static);
+                             kScratchBytes, stream, prepare_static, nullptr);
 }

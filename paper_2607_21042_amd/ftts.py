@@ -150,6 +150,14 @@ def lib():
         L.ftts_shared_attention.restype = _c.c_int
         L.ftts_shared_attention.argtypes = [P(AttnShape), vp, i64, vp, i32, i32, P(SharedPrefixC), P(PageTable),
                                             P(KvPool), i32, vp, i64, vp, _c.c_size_t, vp]
+        L.ftts_shared_workspace_bytes.restype = _c.c_size_t
+        L.ftts_shared_workspace_bytes.argtypes = [P(Config), i32, i32, i32, i32]
+        L.ftts_prefill_shared.restype = _c.c_int
+        L.ftts_prefill_shared.argtypes = [P(Weights), P(SharedPrefixC), vp, P(i32), vp, P(i32), i32, i32, i32,
+                                          P(PageTable), P(KvPool), vp, vp, _c.c_size_t, vp]
+        L.ftts_decode_step_shared.restype = _c.c_int
+        L.ftts_decode_step_shared.argtypes = [P(Weights), P(SharedPrefixC), vp, vp, P(PageTable), P(KvPool), vp, vp, vp,
+                                              vp, P(Sampling), i32, vp, _c.c_size_t, vp]
         _lib = L
     return _lib
 
@@ -453,6 +461,35 @@ def shared_attention(q, kv, layer: int, page_table, prefix, out, ws, row_offsets
              _int32("row_offsets", row_offsets, dev, B + 1), T, B, None if prefix is None else _c.byref(prefix.c),
              _c.byref(page_table.c), _c.byref(kv.c), layer, *_rows("out", out, dev, (T, width)), _data("ws", ws, dev),
              ws.numel() * ws.element_size())
+
+
+def shared_workspace_bytes(cfg: Config, max_batch: int, max_rows: int, prefix_len: int, max_pages: int) -> int:
+    """ftts_shared_workspace_bytes."""
+    n = lib().ftts_shared_workspace_bytes(_c.byref(cfg), max_batch, max_rows, prefix_len, max_pages)
+    if n == 0:
+        raise FTTSError(-1, lib().ftts_last_error().decode())
+    return n
+
+
+def prefill_shared(model, prefix, cond_emb, cond_lens, text_ids, text_lens, text_vocab, text_pos0, page_table, kv,
+                   last_logits, ws, stream=None):
+    """ftts_prefill_shared: ftts_prefill_ids for sequences that continue `prefix` (a SharedPrefix);
+    `cond_lens` and `text_lens` are host sequences."""
+    B = len(cond_lens)
+    cl = (i32 * B)(*[int(x) for x in cond_lens])
+    tl = (i32 * B)(*[int(x) for x in text_lens])
+    _check(lib().ftts_prefill_shared(_c.byref(model.c), _c.byref(prefix.c), _ptr(cond_emb), cl, _ptr(text_ids), tl,
+                                     int(text_vocab), int(text_pos0), B, _c.byref(page_table.c), _c.byref(kv.c),
+                                     _ptr(last_logits), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def decode_step_shared(model, prefix, tokens, positions, page_table, kv, logits_out, sampled_out, uniforms,
+                       sampling: Sampling, ws, stream=None, hidden_out=None):
+    """ftts_decode_step_shared: a decode step of sequences that continue `prefix` (a SharedPrefix)."""
+    _check(lib().ftts_decode_step_shared(_c.byref(model.c), _c.byref(prefix.c), _ptr(tokens), _ptr(positions),
+                                         _c.byref(page_table.c), _c.byref(kv.c), _ptr(logits_out), _ptr(hidden_out),
+                                         _ptr(sampled_out), _ptr(uniforms), _c.byref(sampling), tokens.numel(),
+                                         _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
 
 
 # --------------------------------------------------------------------------- device state

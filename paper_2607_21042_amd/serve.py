@@ -17,9 +17,14 @@ no host round trip.  Between chunks the host
   sampled the stop code (the device freed the slot at that step), and returns
   their pages;
 * admits waiting requests into free slots: their pages (prefix + budget) come
-  from the host page pool, their prefixes are prefilled together in one
+  from the host page pool and become block tables on the device
+  (``ftts_build_tables``), their prefixes are prefilled together in one
   ``ftts_prefill`` call, and their slot state (START token, position 0, KV slot,
   budget) is written by device copies ordered after the running chunk.
+
+With a shared prefix -- the rows of one voice prompt, the same for every request
+-- those rows are prefilled and cached once, and every request continues them
+(``ftts_prefill_shared``, ``ftts_decode_step_shared``).
 
 Nothing here computes model arithmetic: every step of the path runs in the HIP
 library; this module only moves ids, pages and slot bookkeeping.
@@ -27,6 +32,7 @@ library; this module only moves ids, pages and slot bookkeeping.
 from __future__ import annotations
 
 from dataclasses import dataclass, field
+from functools import partial
 
 import numpy as np
 import torch
@@ -67,11 +73,13 @@ class Scheduler:
                instead of launching every kernel from the host.
     stop_on_token  end a request when it samples the stop code (stop_token, default the
                shape's), not only when its budget runs out.
+    shared_prefix  rows [P][d_model] that every request continues (a voice prompt), or None;
+               requests' prefixes and max_ctx count what follows them.
     """
 
     def __init__(self, model, shape, max_slots: int, n_pages: int, max_ctx: int, sampling, chunk: int = 16,
                  overlap: int = 0, hidden: bool = False, max_prefill_rows: int | None = None, graphs: bool = True,
-                 stop_on_token: bool = False, stop_token: int | None = None):
+                 stop_on_token: bool = False, stop_token: int | None = None, shared_prefix: np.ndarray | None = None):
         if chunk < 1 or overlap < 0 or overlap >= chunk:
             raise ValueError("need chunk >= 1 and 0 <= overlap < chunk")
         if graphs:
@@ -98,7 +106,17 @@ class Scheduler:
         self.uni = [torch.zeros((chunk, B), dtype=torch.float32, device=dev) for _ in range(2)]
         self.logits = torch.empty((B, shape.vocab), dtype=torch.float32, device=dev)
         rows = max_prefill_rows if max_prefill_rows is not None else B * max_ctx
-        self.ws = torch.empty(ftts.workspace_bytes(model.cfg, B, rows), dtype=torch.uint8, device=dev)
+        self.shared = None
+        if shared_prefix is None or len(shared_prefix) == 0:
+            self.ws = torch.empty(ftts.workspace_bytes(model.cfg, B, rows), dtype=torch.uint8, device=dev)
+        else:
+            P = len(shared_prefix)
+            self.ws = torch.empty(ftts.shared_workspace_bytes(model.cfg, B, max(rows, P), P, self.max_pages),
+                                  dtype=torch.uint8, device=dev)
+            pages = torch.tensor(self.pool.alloc(-(-P // ftts.PAGE)), **i32)
+            ftts.prefill(model, self._rows([shared_prefix]), [P],
+                         ftts.PageTableView(pages[None], torch.zeros(1, **i32)), self.kv, None, self.ws)
+            self.shared = ftts.SharedPrefix(pages, P)
         self.host_hist = [torch.empty((chunk, B), dtype=torch.int32).pin_memory() for _ in range(2)]
         self.host_hid = ([torch.empty((chunk, B, shape.d_model), dtype=torch.float32).pin_memory()
                           for _ in range(2)] if hidden else None)
@@ -112,6 +130,11 @@ class Scheduler:
         self.next_rid = 0
         self.use_graphs = graphs
         self.graphs = [None, None]
+
+    def _rows(self, parts):
+        """Host row arrays, packed, on the device in the activation dtype."""
+        rows = torch.from_numpy(np.concatenate(parts).astype(np.float32)).cuda()
+        return rows.to(ftts.act_dtype(self.model.wdtype))
 
     # -- requests ----------------------------------------------------------------------------
     def submit(self, req: Request) -> Request:
@@ -146,14 +169,19 @@ class Scheduler:
             return
         slots = [s for s, _ in group]
         lens = [r.prefix.shape[0] for _, r in group]
-        bt = np.full((len(group), self.max_pages), -1, dtype=np.int32)
-        for i, s in enumerate(slots):
-            bt[i, :len(self.slot_pages[s])] = self.slot_pages[s]
-        bt_d = torch.from_numpy(bt).cuda()
-        adt = ftts.act_dtype(self.model.wdtype)
-        prefix = torch.from_numpy(np.concatenate([r.prefix for _, r in group]).astype(np.float32)).cuda().to(adt)
-        pt = ftts.PageTableView(bt_d, torch.zeros(len(group), dtype=torch.int32, device="cuda"))
-        ftts.prefill(self.model, prefix, lens, pt, self.kv, None, self.ws)
+        i32 = dict(dtype=torch.int32, device="cuda")
+        bt_d = torch.full((len(group), self.max_pages), -1, **i32)
+        # the pages just taken, in order, for prefix and budget
+        ftts.build_tables(torch.tensor([n + r.max_new for n, (_, r) in zip(lens, group)], **i32),
+                          torch.tensor([p for s in slots for p in self.slot_pages[s]], **i32), self.kv.n_pages, bt_d,
+                          torch.empty(len(group) + 1, **i32), None, torch.empty(2, **i32))
+        prefix = self._rows([r.prefix for _, r in group])
+        pt = ftts.PageTableView(bt_d, torch.zeros(len(group), **i32))
+        if self.shared is None:
+            ftts.prefill(self.model, prefix, lens, pt, self.kv, None, self.ws)
+        else:
+            ftts.prefill_shared(self.model, self.shared, prefix, lens, None, [0] * len(group), 0, 0, pt, self.kv, None,
+                                self.ws)
         idx = torch.tensor(slots, dtype=torch.int64, device="cuda")
         self.block_table.index_copy_(0, idx, bt_d)
         self.pt.seq_lens.index_copy_(0, idx, torch.tensor(lens, dtype=torch.int32, device="cuda"))
@@ -198,9 +226,10 @@ class Scheduler:
         self.history[buf].fill_(-1)
         self.counter.zero_()
         for t in range(self.chunk):
-            ftts.decode_step(self.model, self.tokens, self.positions, self.pt, self.kv, self.logits, self.sampled,
-                             self.uni[buf][t], self.sampling, self.ws,
-                             hidden_out=self.hidden_buf[buf][t] if self.want_hidden else None)
+            step = ftts.decode_step if self.shared is None else partial(ftts.decode_step_shared, prefix=self.shared)
+            step(self.model, tokens=self.tokens, positions=self.positions, page_table=self.pt, kv=self.kv,
+                 logits_out=self.logits, sampled_out=self.sampled, uniforms=self.uni[buf][t], sampling=self.sampling,
+                 ws=self.ws, hidden_out=self.hidden_buf[buf][t] if self.want_hidden else None)
             ftts.advance(self.tokens, self.positions, self.pt.seq_lens, self.sampled, self.remaining,
                          self.stop_token, self.history[buf], self.counter, retire_on_stop=self.stop_on_token)
 

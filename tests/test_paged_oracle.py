@@ -159,3 +159,51 @@ def test_binding_checks():
         ftts.SharedPrefix(i, 129)
     with pytest.raises(ftts.FTTSError, match="pool"):
         ftts.KVCache.over(torch.zeros(1, 2, 2, 1, 32, 64))
+
+
+# ---- the model behind a shared prefix ----------------------------------------------------------
+def test_shared_model_calls_refuse():
+    from paper_2607_21042_amd import workload
+    from tests.test_abi import _fake_weights
+    cfg = ftts.make_config(workload.TINY, ftts.BF16)
+    w, L = _fake_weights(cfg), ftts.lib()
+    samp, kv = ftts.Sampling(1.0, 1, 1.0), ftts.KvPool(FAKE, 8)
+
+    def step(prefix=(FAKE, 100), B=3, max_pages=4, ws_bytes=1 << 40):
+        p = ctypes.byref(ftts.SharedPrefixC(*prefix)) if prefix else None
+        pt = ftts.PageTable(FAKE, FAKE, max_pages)
+        return L.ftts_decode_step_shared(ctypes.byref(w), p, FAKE, FAKE, ctypes.byref(pt), ctypes.byref(kv), FAKE, None, FAKE,
+                                         None, ctypes.byref(samp), B, FAKE, ws_bytes, None)
+
+    def fill(prefix=(FAKE, 100), lens=(3, 4), max_pages=4, ws_bytes=1 << 40):
+        p = ctypes.byref(ftts.SharedPrefixC(*prefix)) if prefix else None
+        pt, a = ftts.PageTable(FAKE, None, max_pages), (ctypes.c_int32 * len(lens))(*lens)
+        z = (ctypes.c_int32 * len(lens))()
+        return L.ftts_prefill_shared(ctypes.byref(w), p, FAKE, a, None, z, 0, 0, len(lens), ctypes.byref(pt), ctypes.byref(kv),
+                                     FAKE, FAKE, ws_bytes, None)
+
+    for call in (step, fill):
+        assert call(prefix=None) == -1 and call(prefix=(None, 3)) == -1
+        assert call(prefix=(FAKE, -1)) == -5 and call(prefix=(FAKE, (1 << 20) + 1)) == -5
+        assert call(max_pages=0) == -2 and call(ws_bytes=100) == -8
+    assert step(B=0) == -2 and step(B=65) == -2 and fill(lens=(0, 4)) == -5 and fill(lens=(257, 4)) == -5
+    # a workspace that serves the call without a prefix is too small behind one
+    assert step(ws_bytes=ftts.workspace_bytes(cfg, 3, 0)) == -8
+    assert fill(ws_bytes=ftts.workspace_bytes(cfg, 2, 7)) == -8
+    try:
+        ftts.set_decode_path(ftts.PATH_PERSISTENT)
+        assert step() == -7 and b"shared prefix" in L.ftts_last_error()
+    finally:
+        ftts.set_decode_path(ftts.PATH_AUTO)
+
+
+def test_shared_workspace_covers_smaller_calls():
+    from paper_2607_21042_amd import workload
+    cfg = ftts.make_config(workload.TINY, ftts.BF16)
+    a = ftts.shared_workspace_bytes(cfg, 8, 100, 64, 4)
+    assert a > ftts.workspace_bytes(cfg, 8, 100) and a % 256 == 0
+    for more in ((16, 100, 64, 4), (8, 4000, 64, 4), (8, 100, 6400, 4), (8, 100, 64, 90)):
+        assert ftts.shared_workspace_bytes(cfg, *more) >= a
+    for bad in ((0, 1, 1, 1), (65, 1, 1, 1), (1, -1, 1, 1), (1, 1, -1, 1), (1, 1, 1, 0), (1, 1, 1, 513), (1, (1 << 24) + 1, 1, 1)):
+        with pytest.raises(ftts.FTTSError):
+            ftts.shared_workspace_bytes(cfg, *bad)
