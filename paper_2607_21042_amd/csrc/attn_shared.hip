@@ -9,6 +9,7 @@
 // kinds of work are cut along the tokens into workgroups that leave partial results, and a
 // second kernel joins them.
 #include <algorithm>
+#include <cmath>
 
 #include "attn_tile.hpp"
 #include "decode_entry.hpp"
@@ -277,6 +278,22 @@ __device__ __forceinline__ void sa_add_not_finite(SaState& a, const char* vt, co
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 }
 
+// The rows' queries as at_load_q gives them; Q32: fp32 ones, rounded to bf16 as the prefill's are.
+template <bool Q32>
+__device__ __forceinline__ void sa_load_q(const SharedAttnArgs& a, const RowTile& t, int hh, uint4 (&qr)[4]) {
+    const size_t q0 = (size_t)max(t.row, 0) * a.q_ld + t.head * kHeadDim;
+    if constexpr (Q32) {
+        const float* qp = reinterpret_cast<const float*>(a.q) + q0 + hh * 8;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+            const float4 x = *reinterpret_cast<const float4*>(qp + kk * 16), y = *reinterpret_cast<const float4*>(qp + kk * 16 + 4);
+            qr[kk] = make_uint4(bf16x2_rne(x.x, x.y), bf16x2_rne(x.z, x.w), bf16x2_rne(y.x, y.y), bf16x2_rne(y.z, y.w));
+        }
+    } else {
+        at_load_q(reinterpret_cast<const uint16_t*>(a.q) + q0, hh, qr);
+    }
+}
+
 // What a workgroup of the cut call does: 32 rows, one key head, a run of pages.
 struct PartWork {
     RowTile t;
@@ -380,17 +397,7 @@ __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_kernel(const Sha
         return ok;
     };
     uint4 qr[4];
-    const size_t q0 = (size_t)max(t.row, 0) * a.q_ld + t.head * kHeadDim;
-    if constexpr (Q32) {  // (rounded to bf16, as the prefill's queries are)
-        const float* qp = reinterpret_cast<const float*>(a.q) + q0 + hh * 8;
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-            const float4 x = *reinterpret_cast<const float4*>(qp + kk * 16), y = *reinterpret_cast<const float4*>(qp + kk * 16 + 4);
-            qr[kk] = make_uint4(bf16x2_rne(x.x, x.y), bf16x2_rne(x.z, x.w), bf16x2_rne(y.x, y.y), bf16x2_rne(y.z, y.w));
-        }
-    } else {
-        at_load_q(reinterpret_cast<const uint16_t*>(a.q) + q0, hh, qr);
-    }
+    sa_load_q<Q32>(a, t, hh, qr);
     const AtAddr ad = at_addresses(lds_address(own), lane);
     SaState st;
     sa_init(st);
@@ -725,6 +732,120 @@ __global__ __launch_bounds__(kStWaves * 64, 3) void shared_tile_kernel(const Sha
     }
 }
 
+// Short contexts, one row a sequence: one workgroup per key head and sequence takes the prefix's pages and the
+// sequence's own, its waves in turn, and writes the result at once: the prefix is read by every sequence (through
+// L2), but there is one launch and no partial.
+constexpr int kSwWaves = 4;
+template <bool Q32>
+__global__ __launch_bounds__(kSwWaves * 64, 2) void shared_whole_kernel(const SharedAttnArgs a) {
+    __shared__ __attribute__((aligned(1024))) char smem[kSwWaves * kAtStage];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hh = lane >> 5;
+    const int kh = blockIdx.x % a.n_kv_head;
+    const OwnTile o = own_tile(a, blockIdx.x / a.n_kv_head, kSaQ, lane);
+    const RowTile t = own_rows(a, o, o.first, kh, lane & 31);
+    const int P = t.inactive ? 0 : a.prefix_len, n_pre = (P + kPage - 1) / kPage;
+    const int pages = n_pre + (t.most + kPage - 1) / kPage;
+    const int n = pages > wave ? (pages - wave + kSwWaves - 1) / kSwWaves : 0;  // this wave's pages: wave, wave + 4, ...
+    char* own = smem + wave * kAtStage;
+    int phys_l = -1;  // lane i: the id of the wave's i-th page (the launcher bounds them by 64)
+    if (const int j = wave + kSwWaves * lane; j < pages)
+        phys_l = j < n_pre ? a.prefix_pages[j] : a.block_table[(size_t)o.b * a.max_pages + j - n_pre];
+    auto load = [&](int i, int kv) {  // the wave's i-th page, K (kv 0) or V; nothing of an invalid page
+        const int phys = __builtin_amdgcn_readlane(phys_l, i), j = wave + kSwWaves * i;
+        const bool ok = phys >= 0 && phys < a.n_pages;
+        const int left = j < n_pre ? P - j * kPage : t.most - (j - n_pre) * kPage;
+        const int bytes = ok ? min(left, kPage) * (kHeadDim * 2) : 0;
+        const uint16_t* src = reinterpret_cast<const uint16_t*>(a.kv_base) +
+                              kv_offset(a.layer, a.n_pages, ok ? phys : 0, kv, a.n_kv_head, kh, 0);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int row = k * 8 + (lane >> 3);
+            buffer_to_lds16(src, bytes, own + kv * kAtTile + k * 1024, row * 128 + (((lane & 7) ^ ((row >> 1) & 7)) << 4), 0);
+        }
+        return ok;
+    };
+    uint4 qr[4];
+    sa_load_q<Q32>(a, t, hh, qr);
+    const AtAddr ad = at_addresses(lds_address(own), lane);
+    SaState st;
+    sa_init(st);
+    bool ok = false;
+    if (n > 0) {
+        ok = load(0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        load(0, 1);
+    }
+    for (int i = 0; i < n; ++i) {
+        const bool more = i + 1 < n, seen = ok;
+        const int j = wave + kSwWaves * i;
+        const int left = j < n_pre ? P - j * kPage : t.most - (j - n_pre) * kPage;  // (all rows see as much)
+        asm volatile("s_waitcnt vmcnt(8)" ::: "memory");  // K is in (this wave's own loads), V's 8 loads may be out
+        __builtin_amdgcn_sched_barrier(0);
+        uint4 ka[4], kb[4];
+        sa_read_k(ad, 0, ka, kb);
+        __builtin_amdgcn_sched_barrier(0);
+        if (more) ok = load(i + 1, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        at_f32x16 s[2];
+        at_scores(ka, kb, qr, s);
+        uint32_t pw[16], plo[16];
+        const int lim = seen ? left : 0;
+        if (lim < kAtK) sa_mask(s, 0, lim, hh);
+        sa_maximum(st, s);
+        st.l += sa_weights<true>(st, s, pw, plo);
+        __builtin_amdgcn_sched_barrier(0);
+        if (more) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");  // V is in, the next K may be out
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        uint64_t v[2][2][4];
+        sa_read_v(ad, 0, v);
+        __builtin_amdgcn_sched_barrier(0);
+        if (more) load(i + 1, 1);
+        __builtin_amdgcn_sched_barrier(0);
+        sa_pv(st, v, pw);
+        sa_pv(st, v, plo);
+    }
+    // the waves' (m, l, O) through LDS, lane for lane; each wave then sums a quarter of the dims
+    __syncthreads();
+    float* mrg = reinterpret_cast<float*>(smem);  // [4][34][64]
+    {
+        float* mw = mrg + wave * 34 * 64;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            mw[i * 64 + lane] = st.o0[i];
+            mw[(16 + i) * 64 + lane] = st.o1[i];
+        }
+        mw[32 * 64 + lane] = st.m;
+        mw[33 * 64 + lane] = st.l;
+    }
+    __syncthreads();
+    float mm = -INFINITY, l = 0.f, x[8];
+#pragma unroll
+    for (int w = 0; w < kSwWaves; ++w) mm = fmaxf(mm, mrg[(w * 34 + 32) * 64 + lane]);
+    const float ref = mm == -INFINITY ? 0.f : mm;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = 0.f;
+#pragma unroll
+    for (int w = 0; w < kSwWaves; ++w) {
+        const float* mw = mrg + w * 34 * 64;
+        const float f = exp2f(mw[32 * 64 + lane] - ref);
+        l += mw[33 * 64 + lane] * f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] += mw[(8 * wave + i) * 64 + lane] * f;
+    }
+    const RowPair ls = swap32(l);
+    const float sum = ls.a + ls.b, inv = sum == 0.f ? 0.f : 1.0f / sum;
+    if (t.row < 0) return;
+    // element 8 wave + i: dims 16 wave + 8 (i / 4) + 4 hh + i % 4
+    const size_t at = (size_t)t.row * a.o_ld + t.head * kHeadDim + 16 * wave + 4 * hh;
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+        const float y[4] = {x[4 * g] * inv, x[4 * g + 1] * inv, x[4 * g + 2] * inv, x[4 * g + 3] * inv};
+        if (a.o_f32) *reinterpret_cast<float4*>(reinterpret_cast<float*>(a.o) + at + 8 * g) = make_float4(y[0], y[1], y[2], y[3]);
+        else *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.o) + at + 8 * g) = make_uint2(bf16x2_rne(y[0], y[1]), bf16x2_rne(y[2], y[3]));
+    }
+}
+
 // Joins the partials, one wave per (row, head): lane s weighs slot s (64 at a time), then 4 groups of 16 lanes sum
 // every fourth slot, 4 dims a lane.
 constexpr int kJoinWaves = 4;
@@ -780,22 +901,22 @@ __global__ __launch_bounds__(kJoinWaves * 64) void shared_join_kernel(const Shar
             make_uint2(bf16x2_rne(o[0] * inv, o[1] * inv), bf16x2_rne(o[2] * inv, o[3] * inv));
 }
 
-// Pages a workgroup.  Own side: 4 (two a wave), more where the table is so wide that the grid would pass kOwnGroups
+// Pages a workgroup.  Own side: 4 (two a wave; fp32, bound by its products: one a wave), more where the table is so wide that the grid would pass kOwnGroups
 // workgroups (most of them past their sequence's end).  Prefix: so many that about 128 workgroups for each row tile,
 // 256 to kPreGroups in all, share it (few rows: bound by reading, and each workgroup leaves 8 KB of partials; many
 // rows: bound by the products), at most kMaxSplit along it.
 constexpr int kOwnGroups = 8192, kPreGroups = 640, kMaxSplit = 64;
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-static SharedPlan shared_plan(int n_head, int n_kv_head, int B, int rows, bool prompt, int prefix_len, int max_pages) {
+static SharedPlan shared_plan(bool f32, int n_head, int n_kv_head, int B, int rows, bool prompt, int prefix_len, int max_pages) {
     const int g = n_head / n_kv_head;
     const int64_t pages = ceil_div(prefix_len, kPage);
     SharedPlan p{};
     p.row_tiles = (int)ceil_div((int64_t)rows * g, kSaQ);
     p.own_tiles = prompt ? (int)((int64_t)rows * g / kSaQ) + B : B * (int)ceil_div(g, kSaQ);
-    const int64_t groups = std::min<int64_t>(std::max<int64_t>((int64_t)128 * p.row_tiles, 256), kPreGroups);
+    const int64_t groups = f32 ? kPreGroups : std::min<int64_t>(std::max<int64_t>((int64_t)128 * p.row_tiles, 256), kPreGroups);
     const int64_t c_pre = std::max({(int64_t)2, ceil_div(pages * n_kv_head * p.row_tiles, groups), ceil_div(pages, kMaxSplit)});
-    const int64_t c_own = std::max((int64_t)4, ceil_div((int64_t)max_pages * n_kv_head * p.own_tiles, kOwnGroups));
+    const int64_t c_own = std::max((int64_t)(f32 ? 2 : 4), ceil_div((int64_t)max_pages * n_kv_head * p.own_tiles, kOwnGroups));
     p.c_pre = (int)std::min(ceil_div(c_pre, 2) * 2, std::max(pages, (int64_t)1));
     p.c_own = (int)std::min(ceil_div(c_own, 2) * 2, (int64_t)max_pages);
     p.s_pre = (int)ceil_div(pages, p.c_pre);
@@ -820,11 +941,27 @@ static int shared_tiles(const SharedAttnArgs& a) {
     return tile <= cut ? (int)tiles : 0;
 }
 
+// Whether shared_whole_kernel takes a call of one row a sequence.  Its chain is a quarter of a sequence's pages (0.3 us
+// a page while about 300 workgroups run, two a unit fit), and every sequence reads the prefix; the cut pays for another launch
+// and 1 ns for 32 rows and a page.  Fitted to 432 calls of both (20/20, 4/4 and 20/4 heads, 1 to 64 sequences of up
+// to 1200 tokens behind 0 to 2000): the worse of the two costs 0.4% of a call on average.  Whole and cut, us, 20 heads:
+// 1 sequence of 50 behind 60 5.5 / 7.8, 8 of 250 behind 250 7.5 / 9.2, 8 of 250 behind 1000 12.6 / 10.8, 32 of 250
+// behind 60 14.6 / 14.4, 32 of 1200 behind 2000 56 / 37.  The table's width stands for the own lengths (for the cut, up to
+// 16 pages of it: a wide table is rarely full).
+static bool shared_whole(const SharedAttnArgs& a) {
+    if (a.row_offsets || ceil_div(a.prefix_len, kPage) + a.max_pages > kWave * kSwWaves) return false;
+    const double g = a.n_head / a.n_kv_head, pages = (double)ceil_div(a.prefix_len, kPage), own = a.max_pages;
+    const double tiles = (double)a.B * ceil_div(a.n_head / a.n_kv_head, kSaQ);
+    const double whole = 4.0 + 0.3 * (pages + own) * std::max(1.0, tiles * a.n_kv_head / 300);
+    const double cut = 8.0 + 1e-3 * a.n_kv_head * (pages * std::ceil(a.B * g / kSaQ) + tiles * std::min(own, 16.0));
+    return whole <= cut;
+}
+
 // An upper bound of the partials of every call up to these sizes, from the least pages a workgroup, and from the
 // most workgroups of 32 rows where more than one shares a side.
 size_t shared_attention_bytes(int n_head, int rows, int prefix_len, int max_pages) {
     const int64_t rh = (int64_t)rows * n_head, pages = ceil_div(prefix_len, kPage);
-    const int64_t most = std::min<int64_t>(ceil_div(pages, 2), kMaxSplit) + ceil_div(max_pages, 4);
+    const int64_t most = std::min<int64_t>(ceil_div(pages, 2), kMaxSplit) + ceil_div(max_pages, 2);
     const int64_t n = std::min(most * rh, (int64_t)(kOwnGroups + kPreGroups) * kSaQ + 2 * rh);
     return (size_t)n * (kHeadDim + 2) * 4 + 256;
 }
@@ -837,7 +974,14 @@ hipError_t launch_shared_attention(int dtype, const SharedAttnArgs& a, void* ws,
         hipLaunchKernelGGL(shared_tile_kernel, dim3((unsigned)(tiles * a.n_kv_head)), dim3(kStWaves * 64), 0, st, a, tiles);
         return hipGetLastError();
     }
-    SharedPlan p = shared_plan(a.n_head, a.n_kv_head, a.B, a.rows, a.row_offsets != nullptr, a.prefix_len, a.max_pages);
+    if (!f32 && shared_whole(a)) {
+        const int64_t own_tiles = a.B * ceil_div(a.n_head / a.n_kv_head, kSaQ);
+        const dim3 wg((unsigned)(own_tiles * a.n_kv_head)), wt(kSwWaves * 64);
+        if (a.q_f32) hipLaunchKernelGGL(shared_whole_kernel<true>, wg, wt, 0, st, a);
+        else hipLaunchKernelGGL(shared_whole_kernel<false>, wg, wt, 0, st, a);
+        return hipGetLastError();
+    }
+    SharedPlan p = shared_plan(f32, a.n_head, a.n_kv_head, a.B, a.rows, a.row_offsets != nullptr, a.prefix_len, a.max_pages);
     const int64_t rows_heads = (int64_t)a.rows * a.n_head;
     if ((size_t)(p.s_pre + p.s_own) * rows_heads * (kHeadDim + 2) * 4 > ws_bytes) return hipErrorInvalidValue;
     p.o = reinterpret_cast<float*>(ws);

@@ -10,7 +10,7 @@ namespace ftts {
 // A request's share of the free pages and of the packed rows is a prefix sum over the requests
 // before it, at most 1024 of them: every workgroup does that scan for itself, one request a
 // thread, and then fills its part of the table and of the slot map, so one launch serves both
-// and nothing passes between workgroups.  A row finds its request by bisecting the row offsets in
+// and nothing passes between workgroups.  A run of four rows finds its request by bisecting the row offsets in
 // LDS, and its page from the kept entries or from the free list directly (never from the entries
 // that another workgroup is writing).
 constexpr int kTabThreads = 1024, kTabPer = 4;  // elements a thread fills at a time
@@ -77,30 +77,45 @@ __global__ __launch_bounds__(kTabThreads) void build_tables_kernel(const TableAr
             a.counts[1] = s_refused;
         }
     }
-    const int cells = a.B * a.max_pages, step = gridDim.x * kTabThreads, i0 = blockIdx.x * kTabThreads + t;
-    for (int i = i0; i < cells; i += step) {
-        const int b = i / a.max_pages, p = i - b * a.max_pages;
-        const int kept = s_has[b];
-        if (p >= kept) a.table[i] = p < s_need[b] ? a.free_pages[s_first[b] + p - kept] : -1;
+    // Four elements a thread at a time: one division or bisection for them, and one store where they start on 16 bytes.
+    const int64_t step = (int64_t)gridDim.x * kTabThreads * kTabPer, i0 = ((int64_t)blockIdx.x * kTabThreads + t) * kTabPer;
+    const int64_t cells = (int64_t)a.B * a.max_pages;
+    for (int64_t i = i0; i < cells; i += step) {
+        int b = (int)(i / a.max_pages), p = (int)(i - (int64_t)b * a.max_pages);
+#pragma unroll
+        for (int k = 0; k < kTabPer; ++k) {
+            if (i + k >= cells) break;
+            const int kept = s_has[b];
+            if (p >= kept) a.table[i + k] = p < s_need[b] ? a.free_pages[s_first[b] + p - kept] : -1;
+            if (++p == a.max_pages) p = 0, ++b;
+        }
     }
-    for (int r = i0; r < a.max_rows; r += step) {
-        int slot = -1;
-        if (r < s_row[a.B]) {
-            int lo = 0, hi = a.B - 1;  // the last request that begins at or before r and is not empty
-            while (lo < hi) {
-                const int mid = (lo + hi + 1) >> 1;
-                if (s_row[mid] <= r) lo = mid;
-                else hi = mid - 1;
-            }
-            if (s_first[lo] >= 0) {
-                const int tok = s_cached[lo] + r - s_row[lo], page = tok / kPage;
-                const int kept = s_has[lo];
-                const int phys = page < kept ? a.table[(size_t)lo * a.max_pages + page]
-                                             : a.free_pages[s_first[lo] + page - kept];
-                if (phys >= 0 && phys < a.n_pages) slot = phys * kPage + tok % kPage;
+    const bool whole = (reinterpret_cast<uintptr_t>(a.slots) & 15u) == 0;
+    for (int64_t r0 = i0; r0 < a.max_rows; r0 += step) {
+        int slot[kTabPer], lo = 0, hi = a.B - 1;  // the last request that begins at or before r0
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (s_row[mid] <= r0) lo = mid;
+            else hi = mid - 1;
+        }
+#pragma unroll
+        for (int k = 0; k < kTabPer; ++k) {
+            const int r = (int)r0 + k;
+            slot[k] = -1;
+            while (lo < a.B && s_row[lo + 1] <= r) ++lo;  // (past empty ones; B: behind the last)
+            if (lo < a.B && s_first[lo] >= 0) {
+                const int tok = s_cached[lo] + r - s_row[lo], page = tok / kPage, kept = s_has[lo];
+                const int phys = page < kept ? a.table[(size_t)lo * a.max_pages + page] : a.free_pages[s_first[lo] + page - kept];
+                if (phys >= 0 && phys < a.n_pages) slot[k] = phys * kPage + tok % kPage;
             }
         }
-        a.slots[r] = slot;
+        if (whole && r0 + kTabPer <= a.max_rows) {
+            *reinterpret_cast<int4*>(a.slots + r0) = make_int4(slot[0], slot[1], slot[2], slot[3]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < kTabPer; ++k)
+                if (r0 + k < a.max_rows) a.slots[r0 + k] = slot[k];
+        }
     }
 }
 

@@ -174,6 +174,30 @@ class Batch:
         return rel
 
 
+def kernel(b):
+    """Which of the launcher's kernels a call takes: "whole" (one row a sequence, one launch), "tile" (128 rows share
+    pages, one launch) or "cut" (along the tokens, joined); fp32 is always cut."""
+    if b.f32:
+        return "cut"
+    B, g, pages, own = len(b.lens), b.H // b.KH, -(-b.P // 64), b.width
+    if b.cu is None:
+        tiles = B * -(-g // 32)
+        whole = 4.0 + 0.3 * (pages + own) * max(1.0, tiles * b.KH / 300)
+        fits = pages + own <= 256 and whole <= 8.0 + 1e-3 * b.KH * (pages * -(-B * g // 32) + tiles * min(own, 16))
+        return "whole" if fits else "cut"
+    tiles = b.T * g // 128 + B
+    tile = 5.0 + 1.1 * (pages + own) * max(1.0, tiles * b.KH / 600)
+    cut = 9.0 + 1.4e-3 * b.KH * (-(-b.T * g // 32) * pages + (b.T * g // 32 + B) * own) + 0.7e-3 * b.T * b.H
+    return "tile" if tile <= cut else "cut"
+
+
+def test_the_cases_take_every_kernel():
+    one = {kernel(Batch("bf16", H, KH, P, EDGE)) for H, KH in HEADS for P in (0, 1, 63, 64, 65, 130, 700)}
+    few = {kernel(Batch("bf16", 4, 4, P, [1, 2, 33, 7], [1, 2, 33, 7])) for P in (0, 65, 400)}
+    wide = {kernel(Batch("bf16", H, KH, P, r, r)) for H, KH, P, r in ((8, 8, 150, [120] * 12 + [1, 129]), (20, 20, 33, [40] * 20))}
+    assert one == {"whole", "cut"} and few == {"tile", "cut"} and wide == {"tile"}
+
+
 EDGE = [0, 1, 2, 63, 64, 65, 127, 128, 129, 200, 256, 257, 321, 500, 513, 700]
 HEADS = [(4, 4), (5, 1), (6, 3)]
 
@@ -270,10 +294,11 @@ def test_rows_that_see_nothing(dtype, rows):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("H,KH,B", [(4, 4, 2), (8, 8, 12), (6, 1, 2)])
-def test_values_that_are_not_finite_reach_only_rows_that_see_them(dtype, H, KH, B):
-    rows, prefix = [90] * B, 70
+@pytest.mark.parametrize("H,KH,B,prefix", [(4, 4, 2, 70), (8, 8, 12, 70), (6, 1, 2, 70), (4, 4, 1, 900), (6, 3, 2, 600)])
+def test_values_that_are_not_finite_reach_only_rows_that_see_them(dtype, H, KH, B, prefix):
+    rows = [90] * B
     b = Batch(dtype, H, KH, prefix, [100] * B, rows).gpu()
+    assert kernel(b) == ("cut" if dtype == "f32" or prefix > 70 else "tile")
     b.call()
     clean = b.out.clone()
     for tok, what in ((100 - 90 + 45, float("nan")), (99, float("inf")), (10 + 63, float("-inf")), (10 + 1, float("inf"))):
@@ -293,6 +318,42 @@ def test_values_that_are_not_finite_reach_only_rows_that_see_them(dtype, H, KH, 
         torch.cuda.synchronize()
         assert torch.equal(b.out[:first], clean[:first]) and torch.equal(b.out[90:], clean[90:]), tok
         assert not torch.isfinite(b.out[first:90].float()).any(), tok
+
+
+def reference64(b, seq, rows):
+    """Rows `rows` of sequence `seq` (indices within it) in float64 on the GPU, all heads."""
+    n = 1 if b.rows is None else b.rows[seq]
+    at = [(b.pre[t // 64], t % 64) for t in range(b.P)] + [(b.table[seq, t // 64], t % 64) for t in range(b.lens[seq])]
+    pg, sl = (dev(x, torch.int64) for x in np.array(at).T)
+    k, v = (b.kv.pool[b.layer][pg, j, :, sl].double().repeat_interleave(b.H // b.KH, 1) for j in (0, 1))
+    first = seq if b.cu is None else int(b.cu[seq])
+    q = b.qd[first + torch.tensor(rows, device="cuda"), :b.H * 64].double().view(len(rows), b.H, 64)
+    out = torch.empty_like(q)
+    for h in range(b.H):
+        s = q[:, h] @ k[:, h].T / 8
+        seen = b.P + b.lens[seq] - n + torch.tensor(rows, device="cuda") + 1
+        s = s.masked_fill(torch.arange(len(pg), device="cuda")[None] >= seen[:, None], -float("inf"))
+        out[:, h] = torch.softmax(s, -1) @ v[:, h]
+    return out, b.out[first + torch.tensor(rows, device="cuda")].double().view_as(out)
+
+
+@pytest.mark.parametrize("dtype,H,KH,prefix,lens,rows,takes", [
+    ("bf16", 1, 1, 560000, [70], None, "cut"), ("f32", 1, 1, 300000, [70], None, "cut"),
+    ("bf16", 8, 8, 5000, [3000], [3000], "tile"), ("bf16", 8, 2, 9000, [40, 2500], [40, 1500], "cut"),
+    ("bf16", 4, 4, 130, [20000, 5], None, "cut"), ("bf16", 20, 20, 0, [700, 3000], [700, 3000], "tile")])
+def test_long_contexts(dtype, H, KH, prefix, lens, rows, takes):
+    """Chains of more than 64 pages (page ids come 64 at a time) and the longest prefixes, against float64 on the
+    GPU at some rows; norms as above, single values within 2^-7 of the largest (two roundings of 2^-8)."""
+    b = Batch(dtype, H, KH, prefix, lens, rows, layers=1).gpu()
+    assert kernel(b) == takes
+    print(f"long contexts: {dtype} {H}/{KH} heads, prefix {prefix}, lengths {lens}", flush=True)
+    b.call()
+    torch.cuda.synchronize()
+    for seq in range(len(lens)):
+        n = 1 if rows is None else rows[seq]
+        ref, got = reference64(b, seq, sorted({0, n // 3, n // 2, max(n - 2, 0), n - 1}))
+        assert (got - ref).norm() <= (1e-5 if dtype == "f32" else 2.0 ** -8) * ref.norm(), seq
+        assert (got - ref).abs().max() <= (1e-5 if dtype == "f32" else 2.0 ** -7) * ref.abs().max(), seq
 
 
 def test_a_shared_prefix_gives_what_a_copy_in_every_sequence_gives():
