@@ -10,6 +10,7 @@
 // second kernel joins them.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "attn_tile.hpp"
 #include "decode_entry.hpp"
@@ -95,16 +96,18 @@ __device__ __forceinline__ RowTile own_rows(const SharedAttnArgs& a, const OwnTi
     return t;
 }
 
-// A staged tile's K operands, and its V operands, in one assembly block with the wait: nothing is in flight in a
-// register that the compiler holds for written.
-__device__ __forceinline__ void sa_read_k(const AtAddr& r, uint32_t so, uint4 (&ka)[4], uint4 (&kb)[4]) {
+// A staged tile's K operands, and its V operands (SO: byte offset of the stage), in one assembly block with the wait:
+// nothing is in flight in a register that the compiler holds for written.
+template <int SO>
+__device__ __forceinline__ void sa_read_k(const AtAddr& r, uint4 (&ka)[4], uint4 (&kb)[4]) {
     at_bf16x8 x[8];
     asm volatile(
-        "ds_read_b128 %0, %8\n\tds_read_b128 %1, %9\n\tds_read_b128 %2, %10\n\tds_read_b128 %3, %11\n\t"
-        "ds_read_b128 %4, %8 offset:4096\n\tds_read_b128 %5, %9 offset:4096\n\t"
-        "ds_read_b128 %6, %10 offset:4096\n\tds_read_b128 %7, %11 offset:4096\n\ts_waitcnt lgkmcnt(0)"
+        "ds_read_b128 %0, %8 offset:%12\n\tds_read_b128 %1, %9 offset:%12\n\t"
+        "ds_read_b128 %2, %10 offset:%12\n\tds_read_b128 %3, %11 offset:%12\n\t"
+        "ds_read_b128 %4, %8 offset:%13\n\tds_read_b128 %5, %9 offset:%13\n\t"
+        "ds_read_b128 %6, %10 offset:%13\n\tds_read_b128 %7, %11 offset:%13\n\ts_waitcnt lgkmcnt(0)"
         : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7])
-        : "v"(r.kr[0] + so), "v"(r.kr[1] + so), "v"(r.kr[2] + so), "v"(r.kr[3] + so)
+        : "v"(r.kr[0]), "v"(r.kr[1]), "v"(r.kr[2]), "v"(r.kr[3]), "n"(SO), "n"(SO + 4096)
         : "memory");
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -112,20 +115,38 @@ __device__ __forceinline__ void sa_read_k(const AtAddr& r, uint32_t so, uint4 (&
         kb[i] = __builtin_bit_cast(uint4, x[4 + i]);
     }
 }
-__device__ __forceinline__ void sa_read_v(const AtAddr& r, uint32_t so, uint64_t (&v)[2][2][4]) {
-#define SA_TR(O, A) "ds_read_b64_tr_b16 %" #O ", %" #A
+template <int SO>
+__device__ __forceinline__ void sa_read_v(const AtAddr& r, uint64_t (&v)[2][2][4]) {
+#define SA_TR(O, A, S) "ds_read_b64_tr_b16 %" #O ", %" #A " offset:%" #S "\n\t"
     asm volatile(
-        SA_TR(0, 16) "\n\t" SA_TR(1, 16) " offset:2048\n\t" SA_TR(2, 16) " offset:4096\n\t" SA_TR(3, 16) " offset:6144\n\t"
-        SA_TR(4, 17) "\n\t" SA_TR(5, 17) " offset:2048\n\t" SA_TR(6, 17) " offset:4096\n\t" SA_TR(7, 17) " offset:6144\n\t"
-        SA_TR(8, 18) "\n\t" SA_TR(9, 18) " offset:2048\n\t" SA_TR(10, 18) " offset:4096\n\t" SA_TR(11, 18) " offset:6144\n\t"
-        SA_TR(12, 19) "\n\t" SA_TR(13, 19) " offset:2048\n\t" SA_TR(14, 19) " offset:4096\n\t" SA_TR(15, 19) " offset:6144\n\t"
+        SA_TR(0, 16, 20) SA_TR(1, 16, 21) SA_TR(2, 16, 22) SA_TR(3, 16, 23)
+        SA_TR(4, 17, 20) SA_TR(5, 17, 21) SA_TR(6, 17, 22) SA_TR(7, 17, 23)
+        SA_TR(8, 18, 20) SA_TR(9, 18, 21) SA_TR(10, 18, 22) SA_TR(11, 18, 23)
+        SA_TR(12, 19, 20) SA_TR(13, 19, 21) SA_TR(14, 19, 22) SA_TR(15, 19, 23)
         "s_waitcnt lgkmcnt(0)"
         : "=&v"(v[0][0][0]), "=&v"(v[0][0][1]), "=&v"(v[0][0][2]), "=&v"(v[0][0][3]), "=&v"(v[0][1][0]), "=&v"(v[0][1][1]),
           "=&v"(v[0][1][2]), "=&v"(v[0][1][3]), "=&v"(v[1][0][0]), "=&v"(v[1][0][1]), "=&v"(v[1][0][2]), "=&v"(v[1][0][3]),
           "=&v"(v[1][1][0]), "=&v"(v[1][1][1]), "=&v"(v[1][1][2]), "=&v"(v[1][1][3])
-        : "v"(r.vr[0][0] + so), "v"(r.vr[1][0] + so), "v"(r.vr[0][1] + so), "v"(r.vr[1][1] + so)
+        : "v"(r.vr[0][0]), "v"(r.vr[1][0]), "v"(r.vr[0][1]), "v"(r.vr[1][1]), "n"(SO), "n"(SO + 2048), "n"(SO + 4096), "n"(SO + 6144)
         : "memory");
 #undef SA_TR
+}
+
+// A page of one key head as its loads see it: where its keys (its values: n_kv_head blocks on) begin, and how many
+// tokens of it are seen, 0 for a page outside the pool.  One a lane, computed 64 at a time: a loop's scalar work per page is
+// what the vector units wait for.
+struct PageRef {
+    uint32_t lo, hi;
+    int tokens;
+};
+__device__ __forceinline__ PageRef page_ref(const SharedAttnArgs& a, int kh, int esize, int phys, int left) {
+    const bool ok = phys >= 0 && phys < a.n_pages;
+    const uint64_t off = kv_offset(a.layer, a.n_pages, ok ? phys : 0, 0, a.n_kv_head, kh, 0) * esize;
+    return {(uint32_t)off, (uint32_t)(off >> 32), ok ? max(min(left, kPage), 0) : 0};
+}
+__device__ __forceinline__ const char* page_at(const SharedAttnArgs& a, const PageRef& r, int lane) {
+    return reinterpret_cast<const char*>(a.kv_base) +
+           ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)r.hi, lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)r.lo, lane));
 }
 
 // A wave's running attention of 32 rows: O^T as in AtState, the maximum (exp2 domain; -inf: nothing seen
@@ -379,22 +400,21 @@ __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_kernel(const Sha
     const RowTile& t = w.t;
     char* own = smem + wave * kAtStage;
     const int n = w.pages > wave ? (w.pages - wave + kSaWaves - 1) / kSaWaves : 0;  // this wave's pages
-    int phys_l = 0;
-    // the wave's page ids, 64 at a time (lane j: page j of the round)
-    auto fetch_ids = [&](int j0) { phys_l = j0 + lane < n ? w.ids[wave + kSaWaves * (j0 + lane)] : -1; };
-    auto load = [&](int j, int kv) {  // the wave's page j, K (kv 0) or V; nothing of an invalid page
-        int phys = __builtin_amdgcn_readlane(phys_l, j & 63);
-        const bool ok = phys >= 0 && phys < a.n_pages;
-        const int left = t.most - (w.page0 + wave + kSaWaves * j) * kPage;
-        const int bytes = ok ? min(left, kPage) * (kHeadDim * 2) : 0;
-        const uint16_t* src = reinterpret_cast<const uint16_t*>(a.kv_base) +
-                              kv_offset(a.layer, a.n_pages, ok ? phys : 0, kv, a.n_kv_head, w.kh, 0);
+    const size_t to_v = (size_t)a.n_kv_head * kAtTile;  // from a page's keys to its values
+    PageRef page{};
+    auto fetch = [&](int j0) {  // the wave's pages j0 .. j0 + 63, one a lane
+        const int j = w.page0 + wave + kSaWaves * (j0 + lane);
+        page = page_ref(a, w.kh, 2, j0 + lane < n ? w.ids[j - w.page0] : -1, t.most - j * kPage);
+    };
+    auto load = [&](int j, int kv) {  // the wave's page j, K (kv 0) or V; zeros for what is not seen
+        const int tokens = __builtin_amdgcn_readlane(page.tokens, j & 63);
+        const char* src = page_at(a, page, j & 63) + kv * to_v;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int row = i * 8 + (lane >> 3);
-            buffer_to_lds16(src, bytes, own + kv * kAtTile + i * 1024, row * 128 + (((lane & 7) ^ ((row >> 1) & 7)) << 4), 0);
+            buffer_to_lds16(src, tokens * 128, own + kv * kAtTile + i * 1024, row * 128 + (((lane & 7) ^ ((row >> 1) & 7)) << 4), 0);
         }
-        return ok;
+        return tokens > 0;
     };
     uint4 qr[4];
     sa_load_q<Q32>(a, t, hh, qr);
@@ -403,7 +423,7 @@ __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_kernel(const Sha
     sa_init(st);
     bool ok = false;
     if (n > 0) {
-        fetch_ids(0);
+        fetch(0);
         ok = load(0, 0);
         __builtin_amdgcn_sched_barrier(0);
         load(0, 1);
@@ -414,10 +434,10 @@ __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_kernel(const Sha
         asm volatile("s_waitcnt vmcnt(8)" ::: "memory");  // K is in (this wave's own loads), V's 8 loads may be out
         __builtin_amdgcn_sched_barrier(0);
         uint4 ka[4], kb[4];
-        sa_read_k(ad, 0, ka, kb);
+        sa_read_k<0>(ad, ka, kb);
         __builtin_amdgcn_sched_barrier(0);
         if (more) {
-            if (((j + 1) & 63) == 0) fetch_ids(j + 1);
+            if (((j + 1) & 63) == 0) fetch(j + 1);
             ok = load(j + 1, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -433,12 +453,12 @@ __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_kernel(const Sha
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
         uint64_t v[2][2][4];
-        sa_read_v(ad, 0, v);
+        sa_read_v<0>(ad, v);
         __builtin_amdgcn_sched_barrier(0);
         // (rows without a token in the tile have weights of 0, those past a tile's end zeros for values)
         if (PROMPT && __any(t.lim < min(t.most, k0 + kAtK)) && sa_not_finite(v, s)) {
             sa_add_not_finite(st, own + kAtTile, pw, hh);
-            sa_read_v(ad, 0, v);
+            sa_read_v<0>(ad, v);
             sa_take_out(v);
         }
         if (more) load(j + 1, 1);
@@ -518,21 +538,23 @@ __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_f32_kernel(const
     const RowTile& t = w.t;
     char* own = smem + wave * kAtStage;
     const int n = w.pages > wave ? 2 * ((w.pages - wave + kSaWaves - 1) / kSaWaves) : 0;  // this wave's half pages
-    int phys_l = 0;
-    auto fetch_ids = [&](int j0) { phys_l = 2 * (j0 + lane) < n ? w.ids[wave + kSaWaves * (j0 + lane)] : -1; };  // (64 pages)
+    const size_t to_v = (size_t)a.n_kv_head * (kPage * kHeadDim * 4);  // from a page's keys to its values
+    PageRef page{};
+    auto fetch = [&](int j0) {  // the wave's pages j0 .. j0 + 63, one a lane
+        const int j = w.page0 + wave + kSaWaves * (j0 + lane);
+        page = page_ref(a, w.kh, 4, 2 * (j0 + lane) < n ? w.ids[j - w.page0] : -1, t.most - j * kPage);
+    };
     auto first = [&](int u) { return (w.page0 + wave + kSaWaves * (u >> 1)) * kPage + (u & 1) * kSfK; };
-    auto load = [&](int u, int kv) {  // half page u, K (kv 0) or V; nothing of an invalid page
-        const int phys = __builtin_amdgcn_readlane(phys_l, (u >> 1) & 63);
-        const bool ok = phys >= 0 && phys < a.n_pages;
-        const int bytes = ok ? max(min(t.most - first(u), kSfK), 0) * (kHeadDim * 4) : 0;
-        const float* src = reinterpret_cast<const float*>(a.kv_base) +
-                           kv_offset(a.layer, a.n_pages, ok ? phys : 0, kv, a.n_kv_head, w.kh, (u & 1) * kSfK);
+    auto load = [&](int u, int kv) {  // half page u, K (kv 0) or V; zeros for what is not seen
+        const int j = (u >> 1) & 63, tokens = __builtin_amdgcn_readlane(page.tokens, j);
+        const char* src = page_at(a, page, j) + kv * to_v + (u & 1) * kAtTile;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int row = i * 4 + (lane >> 4);
-            buffer_to_lds16(src, bytes, own + kv * kAtTile + i * 1024, row * 256 + (((lane & 15) ^ (row & 15)) << 4), 0);
+            buffer_to_lds16(src, max(min(tokens - (u & 1) * kSfK, kSfK), 0) * 256, own + kv * kAtTile + i * 1024,
+                            row * 256 + (((lane & 15) ^ (row & 15)) << 4), 0);
         }
-        return ok;
+        return tokens > 0;
     };
     float4 q[8];
     {
@@ -554,7 +576,7 @@ __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_f32_kernel(const
     sa_init(st);
     bool ok = false;
     if (n > 0) {
-        fetch_ids(0);
+        fetch(0);
         ok = load(0, 0);
         __builtin_amdgcn_sched_barrier(0);
         load(0, 1);
@@ -568,7 +590,7 @@ __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_f32_kernel(const
         sf_read_k(kr, k);
         __builtin_amdgcn_sched_barrier(0);
         if (more) {
-            if (((u + 1) & 127) == 0) fetch_ids((u + 1) >> 1);
+            if (((u + 1) & 127) == 0) fetch((u + 1) >> 1);
             ok = load(u + 1, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -655,68 +677,74 @@ __global__ __launch_bounds__(kStWaves * 64, 3) void shared_tile_kernel(const Sha
     const int wave_first = o.first + wave * kSaQ;
     const RowTile t = own_rows(a, o, wave_first, kh, ql);
     SaState st;
+    sa_init(st);
     uint4 qr[4];
     at_load_q(reinterpret_cast<const uint16_t*>(a.q) + (size_t)max(t.row, 0) * a.q_ld + t.head * kHeadDim, hh, qr);
     const bool rows = wave_first < o.n * g;
-    int phys_l = 0;
-    auto fetch_ids = [&](int j0) {  // the ids of tiles j0 .. j0 + 63, one a lane
+    const size_t to_v = (size_t)a.n_kv_head * kAtTile;  // from a page's keys to its values
+    PageRef page{};
+    auto fetch = [&](int j0) {  // tiles j0 .. j0 + 63, one a lane
         const int j = j0 + lane;
-        phys_l = -1;
-        if (j < n) phys_l = j < n_pre ? a.prefix_pages[j] : a.block_table[(size_t)o.b * a.max_pages + j - n_pre];
+        int phys = -1;
+        if (j < n) phys = j < n_pre ? a.prefix_pages[j] : a.block_table[(size_t)o.b * a.max_pages + j - n_pre];
+        page = page_ref(a, kh, 2, phys, j < n_pre ? P - j * kPage : most - (j - n_pre) * kPage);
     };
-    auto load = [&](int j) {  // tile j (of the ids in hand, or the first of the next 64); an invalid page: zeros
-        if ((j & 63) == 0) fetch_ids(j);
-        const int phys = __builtin_amdgcn_readlane(phys_l, j & 63);
-        const bool ok = phys >= 0 && phys < a.n_pages;
-        const int left = j < n_pre ? P - j * kPage : most - (j - n_pre) * kPage;
-        const int bytes = ok ? min(left, kPage) * (kHeadDim * 2) : 0;
-        const uint16_t* src = reinterpret_cast<const uint16_t*>(a.kv_base) +
-                              kv_offset(a.layer, a.n_pages, ok ? phys : 0, 0, a.n_kv_head, kh, 0);
-        char* dst = smem + (j & 1) * kAtStage + wave * kLoads * 1024;
+    uint32_t vo[kLoads];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+        const int row = (wave * kLoads + i) * 8 + (lane >> 3);
+        vo[i] = row * 128 + (((lane & 7) ^ ((row >> 1) & 7)) << 4);
+    }
+    auto load = [&](int j, int so) {  // this wave's part of tile j into the stage at so; zeros for what is not seen
+        if ((j & 63) == 0) fetch(j);
+        const int tokens = __builtin_amdgcn_readlane(page.tokens, j & 63);
+        const char* src = page_at(a, page, j & 63);
+        char* dst = smem + so + wave * kLoads * 1024;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const int row = (wave * kLoads + i) * 8 + (lane >> 3);
-            const uint32_t vo = row * 128 + (((lane & 7) ^ ((row >> 1) & 7)) << 4);
-            buffer_to_lds16(src, bytes, dst + i * 1024, vo, 0);
-            buffer_to_lds16(src + (size_t)a.n_kv_head * (kPage * kHeadDim), bytes, dst + kAtTile + i * 1024, vo, 0);
+            buffer_to_lds16(src, tokens * 128, dst + i * 1024, vo[i], 0);
+            buffer_to_lds16(src + to_v, tokens * 128, dst + kAtTile + i * 1024, vo[i], 0);
         }
-        return ok;
+        return tokens > 0;
     };
     const AtAddr ad = at_addresses(lds_address(smem), lane);
-    sa_init(st);
-    bool ok = n > 0 && load(0);
-    for (int j = 0; j < n; ++j) {
+    bool ok = n > 0 && load(0, 0);
+    auto step = [&](auto stage, int j) {  // tile j, in the stage at SO
+        constexpr int SO = decltype(stage)::value;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's loads of tile j
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_barrier();  // tile j is in; every wave has read tile j - 1
         __builtin_amdgcn_sched_barrier(0);
         const bool seen = ok;
-        if (j + 1 < n) ok = load(j + 1);
+        if (j + 1 < n) ok = load(j + 1, kAtStage - SO);
         const bool pre = j < n_pre;
         const int k0 = pre ? j * kPage : (j - n_pre) * kPage;
-        if (!seen || !rows || (!pre && k0 >= t.most)) continue;  // nothing for this wave
-        const uint32_t so = (j & 1) * kAtStage;
+        if (!seen || !rows || (!pre && k0 >= t.most)) return;  // nothing for this wave
         const int lim = pre ? P : t.lim;
         const bool mask = __any(lim < k0 + kAtK);
+        uint4 ka[4], kb[4];
         at_f32x16 s[2];
         uint64_t v[2][2][4];
         uint32_t pw[16], none[1];
-        uint4 ka[4], kb[4];
-        sa_read_k(ad, so, ka, kb);
+        sa_read_k<SO>(ad, ka, kb);
         __builtin_amdgcn_sched_barrier(0);
         at_scores(ka, kb, qr, s);
         __builtin_amdgcn_sched_barrier(0);
-        sa_read_v(ad, so, v);
+        sa_read_v<SO>(ad, v);
         __builtin_amdgcn_sched_barrier(0);
         if (mask) sa_mask(s, k0, lim, hh);
         sa_maximum(st, s);
         st.l += sa_weights<false>(st, s, pw, none);
         if (!pre && __any(t.lim < min(most, k0 + kAtK)) && sa_not_finite(v, s)) {
-            sa_add_not_finite(st, smem + so + kAtTile, pw, hh);
-            sa_read_v(ad, so, v);
+            sa_add_not_finite(st, smem + SO + kAtTile, pw, hh);
+            sa_read_v<SO>(ad, v);
             sa_take_out(v);
         }
         sa_pv(st, v, pw);
+    };
+    for (int j = 0; j < n; j += 2) {
+        step(std::integral_constant<int, 0>{}, j);
+        if (j + 1 < n) step(std::integral_constant<int, kAtStage>{}, j + 1);
     }
     const RowPair ls = swap32(st.l);
     const float l = ls.a + ls.b, inv = l == 0.f ? 0.f : 1.0f / l;
@@ -747,49 +775,46 @@ __global__ __launch_bounds__(kSwWaves * 64, 2) void shared_whole_kernel(const Sh
     const int pages = n_pre + (t.most + kPage - 1) / kPage;
     const int n = pages > wave ? (pages - wave + kSwWaves - 1) / kSwWaves : 0;  // this wave's pages: wave, wave + 4, ...
     char* own = smem + wave * kAtStage;
-    int phys_l = -1;  // lane i: the id of the wave's i-th page (the launcher bounds them by 64)
-    if (const int j = wave + kSwWaves * lane; j < pages)
-        phys_l = j < n_pre ? a.prefix_pages[j] : a.block_table[(size_t)o.b * a.max_pages + j - n_pre];
-    auto load = [&](int i, int kv) {  // the wave's i-th page, K (kv 0) or V; nothing of an invalid page
-        const int phys = __builtin_amdgcn_readlane(phys_l, i), j = wave + kSwWaves * i;
-        const bool ok = phys >= 0 && phys < a.n_pages;
-        const int left = j < n_pre ? P - j * kPage : t.most - (j - n_pre) * kPage;
-        const int bytes = ok ? min(left, kPage) * (kHeadDim * 2) : 0;
-        const uint16_t* src = reinterpret_cast<const uint16_t*>(a.kv_base) +
-                              kv_offset(a.layer, a.n_pages, ok ? phys : 0, kv, a.n_kv_head, kh, 0);
+    const size_t to_v = (size_t)a.n_kv_head * kAtTile;  // from a page's keys to its values
+    PageRef page;
+    {
+        const int j = wave + kSwWaves * lane;  // lane i: the wave's i-th page (the launcher bounds them by 64)
+        int phys = -1;
+        if (j < pages) phys = j < n_pre ? a.prefix_pages[j] : a.block_table[(size_t)o.b * a.max_pages + j - n_pre];
+        page = page_ref(a, kh, 2, phys, j < n_pre ? P - j * kPage : t.most - (j - n_pre) * kPage);
+    }
+    auto load = [&](int i, int kv) {  // the wave's i-th page, K (kv 0) or V; zeros for what is not seen
+        const int tokens = __builtin_amdgcn_readlane(page.tokens, i);
+        const char* src = page_at(a, page, i) + kv * to_v;
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             const int row = k * 8 + (lane >> 3);
-            buffer_to_lds16(src, bytes, own + kv * kAtTile + k * 1024, row * 128 + (((lane & 7) ^ ((row >> 1) & 7)) << 4), 0);
+            buffer_to_lds16(src, tokens * 128, own + kv * kAtTile + k * 1024, row * 128 + (((lane & 7) ^ ((row >> 1) & 7)) << 4), 0);
         }
-        return ok;
     };
     uint4 qr[4];
     sa_load_q<Q32>(a, t, hh, qr);
     const AtAddr ad = at_addresses(lds_address(own), lane);
     SaState st;
     sa_init(st);
-    bool ok = false;
     if (n > 0) {
-        ok = load(0, 0);
+        load(0, 0);
         __builtin_amdgcn_sched_barrier(0);
         load(0, 1);
     }
     for (int i = 0; i < n; ++i) {
-        const bool more = i + 1 < n, seen = ok;
-        const int j = wave + kSwWaves * i;
-        const int left = j < n_pre ? P - j * kPage : t.most - (j - n_pre) * kPage;  // (all rows see as much)
+        const bool more = i + 1 < n;
         asm volatile("s_waitcnt vmcnt(8)" ::: "memory");  // K is in (this wave's own loads), V's 8 loads may be out
         __builtin_amdgcn_sched_barrier(0);
         uint4 ka[4], kb[4];
-        sa_read_k(ad, 0, ka, kb);
+        sa_read_k<0>(ad, ka, kb);
         __builtin_amdgcn_sched_barrier(0);
-        if (more) ok = load(i + 1, 0);
+        if (more) load(i + 1, 0);
         __builtin_amdgcn_sched_barrier(0);
         at_f32x16 s[2];
         at_scores(ka, kb, qr, s);
         uint32_t pw[16], plo[16];
-        const int lim = seen ? left : 0;
+        const int lim = __builtin_amdgcn_readlane(page.tokens, i);  // (all rows see as much)
         if (lim < kAtK) sa_mask(s, 0, lim, hh);
         sa_maximum(st, s);
         st.l += sa_weights<true>(st, s, pw, plo);
@@ -798,7 +823,7 @@ __global__ __launch_bounds__(kSwWaves * 64, 2) void shared_whole_kernel(const Sh
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
         uint64_t v[2][2][4];
-        sa_read_v(ad, 0, v);
+        sa_read_v<0>(ad, v);
         __builtin_amdgcn_sched_barrier(0);
         if (more) load(i + 1, 1);
         __builtin_amdgcn_sched_barrier(0);
