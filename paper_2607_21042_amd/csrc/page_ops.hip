@@ -13,7 +13,11 @@ namespace ftts {
 // and nothing passes between workgroups.  A run of four rows finds its request by bisecting the row offsets in
 // LDS, and its page from the kept entries or from the free list directly (never from the entries
 // that another workgroup is writing).
-constexpr int kTabThreads = 1024, kTabPer = 4;  // elements a thread fills at a time
+//
+// Small calls are latency, so they take one element a thread and, up to 256 requests, 256 threads a workgroup; from
+// kTabWide elements on a thread fills four, with one division or bisection for them, one page lookup where they
+// share it, and one store where they start on 16 bytes.
+constexpr int kTabThreads = 1024, kTabWide = 1 << 16;
 
 struct TableArgs {
     const int32_t *cached, *added, *free_pages;
@@ -31,6 +35,7 @@ __device__ __forceinline__ T scan_wave(T v, int lane) {  // inclusive
     return v;
 }
 
+template <int PER>
 __global__ __launch_bounds__(kTabThreads) void build_tables_kernel(const TableArgs a) {
     __shared__ int64_t w_rows[kTabThreads / kWave];
     __shared__ int w_take[kTabThreads / kWave], s_refused, s_taken;
@@ -77,43 +82,47 @@ __global__ __launch_bounds__(kTabThreads) void build_tables_kernel(const TableAr
             a.counts[1] = s_refused;
         }
     }
-    // Four elements a thread at a time: one division or bisection for them, and one store where they start on 16 bytes.
-    const int64_t step = (int64_t)gridDim.x * kTabThreads * kTabPer, i0 = ((int64_t)blockIdx.x * kTabThreads + t) * kTabPer;
+    const int64_t step = (int64_t)gridDim.x * blockDim.x * PER, i0 = ((int64_t)blockIdx.x * blockDim.x + t) * PER;
     const int64_t cells = (int64_t)a.B * a.max_pages;
     for (int64_t i = i0; i < cells; i += step) {
         int b = (int)(i / a.max_pages), p = (int)(i - (int64_t)b * a.max_pages);
 #pragma unroll
-        for (int k = 0; k < kTabPer; ++k) {
+        for (int k = 0; k < PER; ++k) {
             if (i + k >= cells) break;
             const int kept = s_has[b];
             if (p >= kept) a.table[i + k] = p < s_need[b] ? a.free_pages[s_first[b] + p - kept] : -1;
             if (++p == a.max_pages) p = 0, ++b;
         }
     }
-    const bool whole = (reinterpret_cast<uintptr_t>(a.slots) & 15u) == 0;
+    const bool whole = PER == 4 && (reinterpret_cast<uintptr_t>(a.slots) & 15u) == 0;
     for (int64_t r0 = i0; r0 < a.max_rows; r0 += step) {
-        int slot[kTabPer], lo = 0, hi = a.B - 1;  // the last request that begins at or before r0
+        int slot[PER], lo = 0, hi = a.B - 1;  // the last request that begins at or before r0
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
             if (s_row[mid] <= r0) lo = mid;
             else hi = mid - 1;
         }
+        int at_lo = -1, at_page = -1, phys = -1;  // the page last looked up
 #pragma unroll
-        for (int k = 0; k < kTabPer; ++k) {
+        for (int k = 0; k < PER; ++k) {
             const int r = (int)r0 + k;
             slot[k] = -1;
             while (lo < a.B && s_row[lo + 1] <= r) ++lo;  // (past empty ones; B: behind the last)
             if (lo < a.B && s_first[lo] >= 0) {
                 const int tok = s_cached[lo] + r - s_row[lo], page = tok / kPage, kept = s_has[lo];
-                const int phys = page < kept ? a.table[(size_t)lo * a.max_pages + page] : a.free_pages[s_first[lo] + page - kept];
+                if (lo != at_lo || page != at_page) {
+                    phys = page < kept ? a.table[(size_t)lo * a.max_pages + page] : a.free_pages[s_first[lo] + page - kept];
+                    at_lo = lo;
+                    at_page = page;
+                }
                 if (phys >= 0 && phys < a.n_pages) slot[k] = phys * kPage + tok % kPage;
             }
         }
-        if (whole && r0 + kTabPer <= a.max_rows) {
-            *reinterpret_cast<int4*>(a.slots + r0) = make_int4(slot[0], slot[1], slot[2], slot[3]);
+        if (whole && r0 + PER <= a.max_rows) {
+            *reinterpret_cast<int4*>(a.slots + r0) = make_int4(slot[0], slot[PER > 1 ? 1 : 0], slot[PER > 2 ? 2 : 0], slot[PER > 3 ? 3 : 0]);
         } else {
 #pragma unroll
-            for (int k = 0; k < kTabPer; ++k)
+            for (int k = 0; k < PER; ++k)
                 if (r0 + k < a.max_rows) a.slots[r0 + k] = slot[k];
         }
     }
@@ -203,9 +212,12 @@ int ftts_build_tables(const int32_t* cached, const int32_t* added, int32_t B, co
         if (reinterpret_cast<uintptr_t>(x.p) & 3u) return set_error(FTTS_E_ALIGN, "build_tables: input not 4-byte aligned");
     TableArgs a{cached, added, free_pages, B, n_free, n_pages, max_pages, max_rows, block_table, row_offsets, seq_lens, slots, counts};
     const int64_t n = std::max<int64_t>((int64_t)B * max_pages, max_rows);
-    const int blocks = (int)std::min<int64_t>((n + kTabThreads * kTabPer - 1) / (kTabThreads * kTabPer), 256);
+    const bool wide = n >= kTabWide;
+    const int threads = B <= 256 && !wide ? 256 : kTabThreads, fill = threads * (wide ? 4 : 1);
+    const dim3 g((unsigned)std::max<int64_t>(std::min<int64_t>((n + fill - 1) / fill, 256), 1));
     (void)hipGetLastError();
-    hipLaunchKernelGGL(build_tables_kernel, dim3(std::max(blocks, 1)), dim3(kTabThreads), 0, (hipStream_t)stream, a);
+    if (wide) hipLaunchKernelGGL(build_tables_kernel<4>, g, dim3(threads), 0, (hipStream_t)stream, a);
+    else hipLaunchKernelGGL(build_tables_kernel<1>, g, dim3(threads), 0, (hipStream_t)stream, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return set_error(FTTS_E_HIP, "build_tables launch: %s", hipGetErrorString(e));
     return FTTS_OK;
