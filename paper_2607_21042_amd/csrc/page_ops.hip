@@ -82,10 +82,11 @@ __global__ __launch_bounds__(kTabThreads) void build_tables_kernel(const TableAr
             a.counts[1] = s_refused;
         }
     }
-    const int64_t step = (int64_t)gridDim.x * blockDim.x * PER, i0 = ((int64_t)blockIdx.x * blockDim.x + t) * PER;
-    const int64_t cells = (int64_t)a.B * a.max_pages;
-    for (int64_t i = i0; i < cells; i += step) {
-        int b = (int)(i / a.max_pages), p = (int)(i - (int64_t)b * a.max_pages);
+    // (cells stay below 2^20, rows at 2^24, a step at 2^20)
+    const uint32_t step = gridDim.x * blockDim.x * PER, i0 = (blockIdx.x * blockDim.x + t) * PER;
+    const uint32_t cells = (uint32_t)a.B * a.max_pages, max_rows = a.max_rows;
+    for (uint32_t i = i0; i < cells; i += step) {
+        int b = i / (uint32_t)a.max_pages, p = i - b * a.max_pages;
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
             if (i + k >= cells) break;
@@ -95,11 +96,11 @@ __global__ __launch_bounds__(kTabThreads) void build_tables_kernel(const TableAr
         }
     }
     const bool whole = PER == 4 && (reinterpret_cast<uintptr_t>(a.slots) & 15u) == 0;
-    for (int64_t r0 = i0; r0 < a.max_rows; r0 += step) {
+    for (uint32_t r0 = i0; r0 < max_rows; r0 += step) {
         int slot[PER], lo = 0, hi = a.B - 1;  // the last request that begins at or before r0
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
-            if (s_row[mid] <= r0) lo = mid;
+            if (s_row[mid] <= (int)r0) lo = mid;
             else hi = mid - 1;
         }
         int at_lo = -1, at_page = -1, phys = -1;  // the page last looked up
@@ -118,12 +119,12 @@ __global__ __launch_bounds__(kTabThreads) void build_tables_kernel(const TableAr
                 if (phys >= 0 && phys < a.n_pages) slot[k] = phys * kPage + tok % kPage;
             }
         }
-        if (whole && r0 + PER <= a.max_rows) {
+        if (whole && r0 + PER <= max_rows) {
             *reinterpret_cast<int4*>(a.slots + r0) = make_int4(slot[0], slot[PER > 1 ? 1 : 0], slot[PER > 2 ? 2 : 0], slot[PER > 3 ? 3 : 0]);
         } else {
 #pragma unroll
             for (int k = 0; k < PER; ++k)
-                if (r0 + k < a.max_rows) a.slots[r0 + k] = slot[k];
+                if (r0 + k < max_rows) a.slots[r0 + k] = slot[k];
         }
     }
 }
