@@ -926,11 +926,11 @@ __global__ __launch_bounds__(kJoinWaves * 64) void shared_join_kernel(const Shar
             make_uint2(bf16x2_rne(o[0] * inv, o[1] * inv), bf16x2_rne(o[2] * inv, o[3] * inv));
 }
 
-// Pages a workgroup.  Own side: 4 (two a wave; fp32, bound by its products: one a wave), more where the table is so wide that the grid would pass kOwnGroups
-// workgroups (most of them past their sequence's end).  Prefix: so many that about 128 workgroups for each row tile,
-// 256 to kPreGroups in all, share it (few rows: bound by reading, and each workgroup leaves 8 KB of partials; many
-// rows: bound by the products), at most kMaxSplit along it.
-constexpr int kOwnGroups = 8192, kPreGroups = 640, kMaxSplit = 64;
+// Pages a workgroup.  Own side: 4 (two a wave; fp32, bound by its products: one a wave), more where the table is so
+// wide that the grid would pass kOwnGroups workgroups (most of them past their sequence's end).  Prefix: so many that
+// about kPreFew workgroups share it (few rows: bound by reading, and each workgroup leaves 8 KB of partials) or
+// kPreMany (many rows, or fp32: bound by the products), at most kMaxSplit along it.
+constexpr int kOwnGroups = 8192, kPreFew = 256, kPreMany = 640, kMaxSplit = 64;
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 static SharedPlan shared_plan(bool f32, int n_head, int n_kv_head, int B, int rows, bool prompt, int prefix_len, int max_pages) {
@@ -939,7 +939,7 @@ static SharedPlan shared_plan(bool f32, int n_head, int n_kv_head, int B, int ro
     SharedPlan p{};
     p.row_tiles = (int)ceil_div((int64_t)rows * g, kSaQ);
     p.own_tiles = prompt ? (int)((int64_t)rows * g / kSaQ) + B : B * (int)ceil_div(g, kSaQ);
-    const int64_t groups = f32 ? kPreGroups : std::min<int64_t>(std::max<int64_t>((int64_t)128 * p.row_tiles, 256), kPreGroups);
+    const int64_t groups = f32 || p.row_tiles > 4 ? kPreMany : kPreFew;
     const int64_t c_pre = std::max({(int64_t)2, ceil_div(pages * n_kv_head * p.row_tiles, groups), ceil_div(pages, kMaxSplit)});
     const int64_t c_own = std::max((int64_t)(f32 ? 2 : 4), ceil_div((int64_t)max_pages * n_kv_head * p.own_tiles, kOwnGroups));
     p.c_pre = (int)std::min(ceil_div(c_pre, 2) * 2, std::max(pages, (int64_t)1));
@@ -987,7 +987,7 @@ static bool shared_whole(const SharedAttnArgs& a) {
 size_t shared_attention_bytes(int n_head, int rows, int prefix_len, int max_pages) {
     const int64_t rh = (int64_t)rows * n_head, pages = ceil_div(prefix_len, kPage);
     const int64_t most = std::min<int64_t>(ceil_div(pages, 2), kMaxSplit) + ceil_div(max_pages, 2);
-    const int64_t n = std::min(most * rh, (int64_t)(kOwnGroups + kPreGroups) * kSaQ + 2 * rh);
+    const int64_t n = std::min(most * rh, (int64_t)(kOwnGroups + kPreMany) * kSaQ + 2 * rh);
     return (size_t)n * (kHeadDim + 2) * 4 + 256;
 }
 
