@@ -10,7 +10,9 @@
  * Linear weights may be bf16 or fp32, or weight-only quantised to W8A16 /
  * W4A16 (Table I caption; Sec. III-B).  It also runs one guided Euler step of
  * the Semantic-to-Mel flow-matching DiT for a batch of utterances
- * (ftts_dit_step, at the end of this file).
+ * (ftts_dit_step, at the end of this file), and serves a batch whose sequences
+ * continue one shared prefix (block tables, KV append, attention, prefill and
+ * decode step: ftts_build_tables and what follows it).
  *
  * Conventions for every entry point
  * ---------------------------------

@@ -4,10 +4,13 @@
 // 0 .. L_b - n_b + i:  o = sum_j p_j v_j / sum_j p_j,  p_j = exp(q . k_j / 8 - m).
 //
 // A softmax over two disjoint sets of tokens is joined from (m, l, o) of each: m = max(m1, m2),
-// l = l1 e^(m1 - m) + l2 e^(m2 - m), o likewise.  So the batch's rows meet the prefix as one
-// matrix, whatever sequence they belong to, and each sequence's rows meet its own pages; both
-// kinds of work are cut along the tokens into workgroups that leave partial results, and a
-// second kernel joins them.
+// l = l1 e^(m1 - m) + l2 e^(m2 - m), o likewise.  Four kernels share that, chosen by rules on sizes
+// (shared_whole, shared_tiles):
+//   cut    (shared_part_*_kernel): the batch's rows meet the prefix as one matrix, whatever sequence they
+//          belong to, and each sequence's rows meet its own pages; both kinds of work are cut along the tokens into
+//          workgroups that leave partial results, and a second kernel joins them.  Bound by reading the pages once.
+//   whole  one row a sequence and few pages: a workgroup a sequence and key head, no partials.
+//   tile   many rows: 128 rows share each page on its way through LDS.  Bound by vector and matrix work.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -389,8 +392,14 @@ __device__ __forceinline__ void part_finish(const SharedPlan& pl, const PartWork
 
 // bf16: the waves take a run's pages in turn (wave w: w, w + 2, ...) by direct-to-LDS loads into a stage of their own,
 // the next page's K (V) on its way once this one's is in registers; no barrier in the loop.  The weights go into the
-// products as bf16 and what their rounding left, so that only the output is rounded.  PROMPT: several rows a
-// sequence, so a tile's rows may see different tokens.
+// products as bf16 and what their rounding left, so that only the output is rounded (the second product is free where
+// reading bounds).  PROMPT: several rows a sequence, so a tile's rows may see different tokens.
+//
+// Two waves a workgroup: one wave each measured 1-2 us better for 32 short sequences and 2 worse behind long prefixes,
+// four 1-3 worse nearly everywhere (more idle waves at a run's end).  Traced with the join: 32 sequences of 64-700 tokens
+// behind 1500, 20 heads, 18.6 + 4.0 us for 76 MB; 64 of 100-900 behind 16,001 54 + 5 us for 255 MB (a read reaches
+// 5.9 TB/s: 12.9 and 43 us); 24 of up to 1200 behind 5000, 20 query and 4 key heads, 10 + 4.5 for 22 MB: there a chain of
+// page ids, keys, products, values and the hand-over, not bytes.
 template <bool PROMPT, bool Q32>
 __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_kernel(const SharedAttnArgs a, const SharedPlan pl) {
     __shared__ __attribute__((aligned(1024))) char smem[kSaWaves * kAtStage];
@@ -471,7 +480,9 @@ __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_kernel(const Sha
 
 // fp32: the same on 32-token halves of pages (the same 16 KB a stage) with fp32 matrix products, all sums in fp32.  A
 // 16-byte piece c of row r lies at c ^ (r % 16).  K as the first operand: lane (key, hh) holds dims 32 hh .. + 31, one
-// a step; V: lane (dim, hh) holds the key that element i of the scores is for.
+// a step; V: lane (dim, hh) holds the key that element i of the scores is for.  Bound by the products: 8192 cycles a
+// wave and page, whatever the rows, so a wave takes one page where there are enough: 8 sequences of 30-500 tokens behind
+// 700, 20 heads, 16.8 + 3.9 us (two pages a wave: 24 + 3); a wave a row on the vector units took 450.
 constexpr int kSfK = 32;
 __device__ __forceinline__ void sf_read_k(const uint32_t (&kr)[8], float4 (&k)[8]) {
     at_bf16x8 x[8];  // (any 16-byte register type)
@@ -651,7 +662,15 @@ __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_f32_kernel(const
 
 // Many rows: one workgroup per key head and run of 128 rows of a sequence, whose waves (32
 // rows each) share 64-token tiles of the prefix and then of the sequence's own pages.  Tiles come in whole pages of
-// a head, 8 KB of keys and of values, by direct-to-LDS loads into two stages, a tile ahead; one barrier a tile.
+// a head, 8 KB of keys and of values, by direct-to-LDS loads into two stages, a tile ahead; one barrier a tile; three
+// workgroups a CU.  The weights go into the products as bf16 (rounded once; their sum takes the rounded ones).
+//
+// Four prompts of 1500-2300 rows behind 8000 tokens, 20 heads: 497 us, 790 TFLOP/s (a library product of 8192^3: 1460).
+// Counted there: matrix units busy 34% of the time, vector units 45% (32 exponentials of 8 cycles and about 114
+// operations of 4 a tile of 32 rows and a page), both at once 10%, and 15% of the units' time at the launch's ends.  Measured and not
+// taken: three stages, 64 rows a wave (spills), two waves a workgroup (more loads), the next tile's scores under this
+// one's exponentials (two waves a SIMD: 637 us), half a tile's weights under the other half's products (spills: 525),
+// the maximum of the first tile alone with a second pass where a sum overflows (488, not worth its second path).
 constexpr int kStWaves = 4;
 __global__ __launch_bounds__(kStWaves * 64, 3) void shared_tile_kernel(const SharedAttnArgs a, int tiles) {
     constexpr int kRows = kStWaves * kSaQ, kLoads = 8 / kStWaves;
@@ -762,7 +781,8 @@ __global__ __launch_bounds__(kStWaves * 64, 3) void shared_tile_kernel(const Sha
 
 // Short contexts, one row a sequence: one workgroup per key head and sequence takes the prefix's pages and the
 // sequence's own, its waves in turn, and writes the result at once: the prefix is read by every sequence (through
-// L2), but there is one launch and no partial.
+// L2), but there is one launch and no partial.  Bound by its chain (ids, keys, products, values, hand-over): 4
+// sequences of up to 90 tokens behind 134, 20 heads, 6.7 us traced (cut: 4.7 + 3.0 and a second launch).
 constexpr int kSwWaves = 4;
 template <bool Q32>
 __global__ __launch_bounds__(kSwWaves * 64, 2) void shared_whole_kernel(const SharedAttnArgs a) {
@@ -872,7 +892,7 @@ __global__ __launch_bounds__(kSwWaves * 64, 2) void shared_whole_kernel(const Sh
 }
 
 // Joins the partials, one wave per (row, head): lane s weighs slot s (64 at a time), then 4 groups of 16 lanes sum
-// every fourth slot, 4 dims a lane.
+// every fourth slot, 4 dims a lane (16 lanes that walk all slots in turn took 20 us for 25 slots of 480 rows; this 5).
 constexpr int kJoinWaves = 4;
 template <bool F32>
 __global__ __launch_bounds__(kJoinWaves * 64) void shared_join_kernel(const SharedAttnArgs a, const SharedPlan pl) {
