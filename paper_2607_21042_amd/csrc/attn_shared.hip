@@ -318,18 +318,25 @@ __device__ __forceinline__ void sa_load_q(const SharedAttnArgs& a, const RowTile
     }
 }
 
+// A page id asked for before it is known whether the page is seen (a plain load could be moved behind that): the ids
+// then come with the lengths instead of a trip to memory after them.
+__device__ __forceinline__ int early_id(const int32_t* p) {
+    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+}
+
 // What a workgroup of the cut call does: 32 rows, one key head, a run of pages.
 struct PartWork {
     RowTile t;
     const int32_t* ids;  // its pages
     int kh, page0, pages;
+    int id0;             // page 2 * lane + wave of the run
     int64_t part;        // where this lane's row leaves its partial
 };
 // Prefix work comes first: the row tiles of one (key head, run of pages) are 8 workgroups apart, so that one XCD
 // (workgroups are dealt to the 8 in turn) reads the run through its L2.  False: nothing to do (what has no pages
 // says so in its slot).
 __device__ __forceinline__ bool part_work(const SharedAttnArgs& a, const SharedPlan& pl, int tid, PartWork& w) {
-    const int lane = tid & 63, ql = lane & 31;
+    const int lane = tid & 63, ql = lane & 31, j0 = (tid >> 6) + kSaWaves * lane;
     int id = blockIdx.x, slot;
     const int n_pre = (a.n_kv_head * pl.s_pre + 7) / 8 * 8 * pl.row_tiles;
     if (id < n_pre) {
@@ -341,17 +348,19 @@ __device__ __forceinline__ bool part_work(const SharedAttnArgs& a, const SharedP
         w.page0 = slot * pl.c_pre;
         w.pages = min(pl.c_pre, (a.prefix_len + kPage - 1) / kPage - w.page0);
         w.ids = a.prefix_pages + w.page0;
+        w.id0 = early_id(w.ids + min(j0, w.pages - 1));
     } else {
         id -= n_pre;
         w.kh = id % a.n_kv_head;
         const int sp = id / a.n_kv_head % pl.s_own, tile = id / a.n_kv_head / pl.s_own;
+        w.page0 = sp * pl.c_own;
         const OwnTile o = own_tile(a, tile, kSaQ, lane);
         if (o.b >= a.B) return false;
+        w.ids = a.block_table + (size_t)o.b * a.max_pages + w.page0;
+        w.id0 = early_id(w.ids + min(j0, a.max_pages - 1 - w.page0));
         w.t = own_rows(a, o, o.first, w.kh, ql);
         slot = pl.s_pre + sp;
-        w.page0 = sp * pl.c_own;
         w.pages = min(pl.c_own, (w.t.most + kPage - 1) / kPage - w.page0);
-        w.ids = a.block_table + (size_t)o.b * a.max_pages + w.page0;
     }
     w.part = slot * ((int64_t)a.rows * a.n_head) + (int64_t)w.t.row * a.n_head + w.t.head;
     if (w.pages > 0) return true;
@@ -413,7 +422,8 @@ __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_kernel(const Sha
     PageRef page{};
     auto fetch = [&](int j0) {  // the wave's pages j0 .. j0 + 63, one a lane
         const int j = w.page0 + wave + kSaWaves * (j0 + lane);
-        page = page_ref(a, w.kh, 2, j0 + lane < n ? w.ids[j - w.page0] : -1, t.most - j * kPage);
+        const int id = j0 == 0 ? w.id0 : j0 + lane < n ? w.ids[j - w.page0] : -1;
+        page = page_ref(a, w.kh, 2, id, j0 + lane < n ? t.most - j * kPage : 0);
     };
     auto load = [&](int j, int kv) {  // the wave's page j, K (kv 0) or V; zeros for what is not seen
         const int tokens = __builtin_amdgcn_readlane(page.tokens, j & 63);
@@ -553,7 +563,8 @@ __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_f32_kernel(const
     PageRef page{};
     auto fetch = [&](int j0) {  // the wave's pages j0 .. j0 + 63, one a lane
         const int j = w.page0 + wave + kSaWaves * (j0 + lane);
-        page = page_ref(a, w.kh, 4, 2 * (j0 + lane) < n ? w.ids[j - w.page0] : -1, t.most - j * kPage);
+        const int id = j0 == 0 ? w.id0 : 2 * (j0 + lane) < n ? w.ids[j - w.page0] : -1;
+        page = page_ref(a, w.kh, 4, id, 2 * (j0 + lane) < n ? t.most - j * kPage : 0);
     };
     auto first = [&](int u) { return (w.page0 + wave + kSaWaves * (u >> 1)) * kPage + (u & 1) * kSfK; };
     auto load = [&](int u, int kv) {  // half page u, K (kv 0) or V; zeros for what is not seen
@@ -789,20 +800,17 @@ __global__ __launch_bounds__(kSwWaves * 64, 2) void shared_whole_kernel(const Sh
     __shared__ __attribute__((aligned(1024))) char smem[kSwWaves * kAtStage];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hh = lane >> 5;
     const int kh = blockIdx.x % a.n_kv_head;
+    const int n_pre = (a.prefix_len + kPage - 1) / kPage, j0 = wave + kSwWaves * lane;
     const OwnTile o = own_tile(a, blockIdx.x / a.n_kv_head, kSaQ, lane);
+    const int id0 = early_id(j0 < n_pre ? a.prefix_pages + j0
+                                        : a.block_table + (size_t)o.b * a.max_pages + min(j0 - n_pre, a.max_pages - 1));
     const RowTile t = own_rows(a, o, o.first, kh, lane & 31);
-    const int P = t.inactive ? 0 : a.prefix_len, n_pre = (P + kPage - 1) / kPage;
-    const int pages = n_pre + (t.most + kPage - 1) / kPage;
+    const int P = a.prefix_len, pages = t.inactive ? 0 : n_pre + (t.most + kPage - 1) / kPage;
     const int n = pages > wave ? (pages - wave + kSwWaves - 1) / kSwWaves : 0;  // this wave's pages: wave, wave + 4, ...
     char* own = smem + wave * kAtStage;
     const size_t to_v = (size_t)a.n_kv_head * kAtTile;  // from a page's keys to its values
-    PageRef page;
-    {
-        const int j = wave + kSwWaves * lane;  // lane i: the wave's i-th page (the launcher bounds them by 64)
-        int phys = -1;
-        if (j < pages) phys = j < n_pre ? a.prefix_pages[j] : a.block_table[(size_t)o.b * a.max_pages + j - n_pre];
-        page = page_ref(a, kh, 2, phys, j < n_pre ? P - j * kPage : t.most - (j - n_pre) * kPage);
-    }
+    // lane i: the wave's i-th page (the launcher bounds them by 64)
+    const PageRef page = page_ref(a, kh, 2, id0, j0 >= pages ? 0 : j0 < n_pre ? P - j0 * kPage : t.most - (j0 - n_pre) * kPage);
     auto load = [&](int i, int kv) {  // the wave's i-th page, K (kv 0) or V; zeros for what is not seen
         const int tokens = __builtin_amdgcn_readlane(page.tokens, i);
         const char* src = page_at(a, page, i) + kv * to_v;
@@ -893,7 +901,7 @@ __global__ __launch_bounds__(kSwWaves * 64, 2) void shared_whole_kernel(const Sh
 
 // Joins the partials, one wave per (row, head): lane s weighs slot s (64 at a time), then 4 groups of 16 lanes sum
 // every fourth slot, 4 dims a lane (16 lanes that walk all slots in turn took 20 us for 25 slots of 480 rows; this 5).
-constexpr int kJoinWaves = 4;
+constexpr int kJoinWaves = 4, kJoinEarly = 4;
 template <bool F32>
 __global__ __launch_bounds__(kJoinWaves * 64) void shared_join_kernel(const SharedAttnArgs a, const SharedPlan pl) {
     const int lane = threadIdx.x & 63;
@@ -906,6 +914,10 @@ __global__ __launch_bounds__(kJoinWaves * 64) void shared_join_kernel(const Shar
     bool inactive = false;
     for (int s0 = 0; s0 < S; s0 += kWave) {
         const float2 x = s0 + lane < S ? pl.ml[(s0 + lane) * rows_heads + rh] : make_float2(-INFINITY, 0.f);
+        auto partial = [&](int s) { return *reinterpret_cast<const float4*>(pl.o + ((s0 + s) * rows_heads + rh) * kHeadDim + d); };
+        float4 early[kJoinEarly];  // asked for with the weights; where nothing was written the weight is 0 and they are dropped
+#pragma unroll
+        for (int i = 0; i < kJoinEarly; ++i) early[i] = partial(min(4 * i + grp, min(kWave, S - s0) - 1));
         inactive |= __any(x.y < 0.f);
         const float mn = fmaxf(m, wave_max(x.x)), ref = mn == -INFINITY ? 0.f : mn;
         const float f = x.y == 0.f ? 0.f : exp2f(x.x - ref);  // (a sum of 0: nothing seen there, and nothing written)
@@ -916,16 +928,22 @@ __global__ __launch_bounds__(kJoinWaves * 64) void shared_join_kernel(const Shar
         for (int i = 0; i < 4; ++i) o[i] *= keep;
         const int n = min(kWave, S - s0);
         const unsigned long long live = __ballot(x.y != 0.f);
-#pragma unroll 4
-        for (int s4 = 0; s4 < n; s4 += 4) {  // (every lane stays: the weights come from all of them)
+        auto add = [&](int s4, const float4& y) {  // (every lane stays: the weights come from all of them)
             const int s = s4 + grp;
-            const float w = __shfl(f, s, kWave);
-            float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (live >> s & 1) y = *reinterpret_cast<const float4*>(pl.o + ((s0 + s) * rows_heads + rh) * kHeadDim + d);
+            const float w = __shfl(f, s & 63, kWave);
+            if (s >= n || !(live >> s & 1)) return;
             o[0] = fmaf(y.x, w, o[0]);
             o[1] = fmaf(y.y, w, o[1]);
             o[2] = fmaf(y.z, w, o[2]);
             o[3] = fmaf(y.w, w, o[3]);
+        };
+#pragma unroll
+        for (int i = 0; i < kJoinEarly; ++i) add(4 * i, early[i]);
+#pragma unroll 4
+        for (int s4 = 4 * kJoinEarly; s4 < n; s4 += 4) {
+            float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (s4 + grp < n) y = partial(s4 + grp);
+            add(s4, y);
         }
     }
 #pragma unroll
