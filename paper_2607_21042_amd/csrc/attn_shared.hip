@@ -84,9 +84,10 @@ __device__ __forceinline__ OwnTile own_tile(const SharedAttnArgs& a, int tile, i
     return t;
 }
 // Own tokens that the i-th row of the sequence sees.
-__device__ __forceinline__ int own_seen(const SharedAttnArgs& a, const OwnTile& t, int i) {
-    return t.len < 0 ? 0 : (int)min(max((int64_t)t.len - t.n + i + 1, (int64_t)0), (int64_t)a.max_pages * kPage);
+__device__ __forceinline__ int own_seen(const SharedAttnArgs& a, int len, int n, int i) {
+    return len < 0 ? 0 : (int)min(max((int64_t)len - n + i + 1, (int64_t)0), (int64_t)a.max_pages * kPage);
 }
+__device__ __forceinline__ int own_seen(const SharedAttnArgs& a, const OwnTile& t, int i) { return own_seen(a, t.len, t.n, i); }
 // The 32 pairs from `first` on, one a lane pair.
 __device__ __forceinline__ RowTile own_rows(const SharedAttnArgs& a, const OwnTile& o, int first, int kh, int ql) {
     const int g = a.n_head / a.n_kv_head, idx = first + ql, last = min(first + kSaQ, o.n * g) - 1;
@@ -671,8 +672,66 @@ __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_f32_kernel(const
     part_finish(pl, w, st, smem, wave, lane);
 }
 
-// Many rows: one workgroup per key head and run of 128 rows of a sequence, whose waves (32
-// rows each) share 64-token tiles of the prefix and then of the sequence's own pages.  Tiles come in whole pages of
+// The rows of a workgroup of shared_tile_kernel, (token, head) pairs first .. end - 1 counted over all rows, and the chain of
+// pages that they see: the prefix's, then their sequences' own, sequence after sequence.  Sequence i is lane i's.
+struct TilePages {
+    int first, end, n_pre, n_own;
+    uint64_t seqs;              // the sequences with rows here
+    int row0, n, len;           // a sequence's first row, rows and length
+    int most, start;            // its own tokens that some row here sees, its first page's place among all own ones
+};
+// PACK: tiles of all rows, whatever sequence they are of; else each sequence's rows begin a tile.
+template <bool PACK>
+__device__ __forceinline__ TilePages tile_pages(const SharedAttnArgs& a, int tile, int size, int lane) {
+    static_assert(FTTS_MAX_BATCH <= kWave, "one sequence per lane");
+    const int g = a.n_head / a.n_kv_head;
+    const bool in = lane < a.B;
+    const int lo = in ? a.row_offsets[lane] : 0, hi = in ? a.row_offsets[lane + 1] : 0;
+    TilePages t;
+    t.len = in ? a.seq_lens[lane] + a.len_add : -1;
+    if (a.active && in && !a.active[lane]) t.len = -1;
+    t.row0 = min(max(lo, 0), a.rows);
+    t.n = min(max(hi, t.row0), a.rows) - t.row0;
+    if constexpr (PACK) {
+        t.first = tile * size;
+        t.end = min(t.first + size, a.rows * g);  // (rows * n_head < 2^31)
+        t.seqs = __ballot(t.n > 0 && t.row0 <= (t.end - 1) / g && t.row0 + t.n > t.first / g);
+    } else {
+        const int own = (t.n * g + size - 1) / size;
+        int upto = own;
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) {
+            const int u = __shfl_up(upto, d, kWave);
+            if (lane >= d) upto += u;
+        }
+        const int b = __popcll(__ballot(in && upto <= tile));
+        if (b >= a.B) {
+            t.first = t.end = 0;
+            return t;
+        }
+        const int r0 = __builtin_amdgcn_readlane(t.row0, b);
+        t.first = r0 * g + (tile - __builtin_amdgcn_readlane(upto - own, b)) * size;
+        t.end = min(t.first + size, (r0 + __builtin_amdgcn_readlane(t.n, b)) * g);
+        t.seqs = 1ull << b;
+    }
+    const bool here = t.seqs >> lane & 1;
+    t.most = here ? own_seen(a, t.len, t.n, min((t.end - 1) / g - t.row0, t.n - 1)) : 0;
+    t.n_pre = __any(here && t.len >= 0) ? (a.prefix_len + kPage - 1) / kPage : 0;
+    const int pages = (t.most + kPage - 1) / kPage;
+    int upto = pages;
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) {
+        const int u = __shfl_up(upto, d, kWave);
+        if (lane >= d) upto += u;
+    }
+    t.start = upto - pages;
+    t.n_own = __builtin_amdgcn_readlane(upto, kWave - 1);
+    return t;
+}
+
+// Many rows: one workgroup per key head and run of 128 rows, whose waves (32 rows each) share 64-token tiles of the
+// prefix and then of the sequences' own pages.  Where many short prompts follow a long prefix a run goes over sequences'
+// ends (packed: a wave passes the own pages of sequences that it has no row of), else each sequence begins one.  Tiles come in whole pages of
 // a head, 8 KB of keys and of values, by direct-to-LDS loads into two stages, a tile ahead; one barrier a tile; three
 // workgroups a CU.  The weights go into the products as bf16 (rounded once; their sum takes the rounded ones).
 //
@@ -683,6 +742,7 @@ __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_f32_kernel(const
 // one's exponentials (two waves a SIMD: 637 us), half a tile's weights under the other half's products (spills: 525),
 // the maximum of the first tile alone with a second pass where a sum overflows (488, not worth its second path).
 constexpr int kStWaves = 4;
+template <bool PACK>
 __global__ __launch_bounds__(kStWaves * 64, 3) void shared_tile_kernel(const SharedAttnArgs a, int tiles) {
     constexpr int kRows = kStWaves * kSaQ, kLoads = 8 / kStWaves;
     __shared__ __attribute__((aligned(1024))) char smem[2 * kAtStage];
@@ -697,27 +757,43 @@ __global__ __launch_bounds__(kStWaves * 64, 3) void shared_tile_kernel(const Sha
         tile = t % tiles;
         kh = t / tiles;
     }
-    const OwnTile o = own_tile(a, tile, kRows, lane);
-    if (o.b >= a.B) return;
     const int g = a.n_head / a.n_kv_head;
-    const int last = min(o.first + kRows, o.n * g) - 1;
-    const int most = own_seen(a, o, last / g);  // own tokens that some row of the workgroup sees
-    const int P = o.len < 0 ? 0 : a.prefix_len;
-    const int n_pre = (P + kPage - 1) / kPage, n = n_pre + (most + kPage - 1) / kPage;
-    const int wave_first = o.first + wave * kSaQ;
-    const RowTile t = own_rows(a, o, wave_first, kh, ql);
+    const TilePages o = tile_pages<PACK>(a, tile, kRows, lane);
+    if (o.first >= o.end) return;
+    const int P = a.prefix_len, n = o.n_pre + o.n_own;
+    // This lane's pair, the tile's last one where it is past it (which is not written twice).
+    const int pair = o.first + wave * kSaQ + ql, row = min(pair, o.end - 1) / g, head = kh * g + min(pair, o.end - 1) % g;
+    int seq = -1, own_lim = 0, pre_lim = 0;  // its sequence, the own tokens and those of the prefix that it sees
+    for (uint64_t m = o.seqs; m; m &= m - 1) {
+        const int b = __builtin_ctzll(m), r0 = __builtin_amdgcn_readlane(o.row0, b), rn = __builtin_amdgcn_readlane(o.n, b);
+        const int len = __builtin_amdgcn_readlane(o.len, b);
+        if (row < r0 || row >= r0 + rn) continue;
+        seq = b;
+        own_lim = own_seen(a, len, rn, row - r0);
+        pre_lim = len < 0 ? 0 : P;
+    }
+    const bool rows = o.first + wave * kSaQ < o.end;
     SaState st;
     sa_init(st);
     uint4 qr[4];
-    at_load_q(reinterpret_cast<const uint16_t*>(a.q) + (size_t)max(t.row, 0) * a.q_ld + t.head * kHeadDim, hh, qr);
-    const bool rows = wave_first < o.n * g;
+    at_load_q(reinterpret_cast<const uint16_t*>(a.q) + (size_t)row * a.q_ld + head * kHeadDim, hh, qr);
     const size_t to_v = (size_t)a.n_kv_head * kAtTile;  // from a page's keys to its values
     PageRef page{};
-    auto fetch = [&](int j0) {  // tiles j0 .. j0 + 63, one a lane
-        const int j = j0 + lane;
-        int phys = -1;
-        if (j < n) phys = j < n_pre ? a.prefix_pages[j] : a.block_table[(size_t)o.b * a.max_pages + j - n_pre];
-        page = page_ref(a, kh, 2, phys, j < n_pre ? P - j * kPage : most - (j - n_pre) * kPage);
+    int whose = 0;  // the page's sequence (kWave: the prefix) and its number there, in the low 24 bits
+    auto fetch = [&](int j0) {  // pages j0 .. j0 + 63 of the chain, one a lane
+        const int j = j0 + lane, own = j - o.n_pre;
+        const int32_t* id = own < 0 ? a.prefix_pages + j : nullptr;
+        int left = P - j * kPage;
+        whose = kWave << 24 | j;
+        for (uint64_t m = o.seqs; m; m &= m - 1) {
+            const int b = __builtin_ctzll(m), k = own - __builtin_amdgcn_readlane(o.start, b);
+            const int most = __builtin_amdgcn_readlane(o.most, b);
+            if (k < 0 || own < 0 || k * kPage >= most) continue;
+            id = a.block_table + (size_t)b * a.max_pages + k;
+            left = most - k * kPage;
+            whose = b << 24 | k;
+        }
+        page = page_ref(a, kh, 2, id && j < n ? *id : -1, left);
     };
     uint32_t vo[kLoads];
 #pragma unroll
@@ -735,22 +811,23 @@ __global__ __launch_bounds__(kStWaves * 64, 3) void shared_tile_kernel(const Sha
             buffer_to_lds16(src, tokens * 128, dst + i * 1024, vo[i], 0);
             buffer_to_lds16(src + to_v, tokens * 128, dst + kAtTile + i * 1024, vo[i], 0);
         }
-        return tokens > 0;
+        return tokens;
     };
     const AtAddr ad = at_addresses(lds_address(smem), lane);
-    bool ok = n > 0 && load(0, 0);
+    int next = n > 0 ? load(0, 0) : 0, next_whose = n > 0 ? __builtin_amdgcn_readlane(whose, 0) : 0;
     auto step = [&](auto stage, int j) {  // tile j, in the stage at SO
         constexpr int SO = decltype(stage)::value;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's loads of tile j
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_barrier();  // tile j is in; every wave has read tile j - 1
         __builtin_amdgcn_sched_barrier(0);
-        const bool seen = ok;
-        if (j + 1 < n) ok = load(j + 1, kAtStage - SO);
-        const bool pre = j < n_pre;
-        const int k0 = pre ? j * kPage : (j - n_pre) * kPage;
-        if (!seen || !rows || (!pre && k0 >= t.most)) return;  // nothing for this wave
-        const int lim = pre ? P : t.lim;
+        const int tokens = next, of = next_whose >> 24, k0 = (next_whose & 0xFFFFFF) * kPage;
+        if (j + 1 < n) {
+            next = load(j + 1, kAtStage - SO);
+            next_whose = __builtin_amdgcn_readlane(whose, (j + 1) & 63);
+        }
+        const int lim = of == kWave ? pre_lim : !PACK || of == seq ? own_lim : 0;
+        if (tokens == 0 || !rows || !__any(lim > k0)) return;  // nothing for this wave
         const bool mask = __any(lim < k0 + kAtK);
         uint4 ka[4], kb[4];
         at_f32x16 s[2];
@@ -765,7 +842,7 @@ __global__ __launch_bounds__(kStWaves * 64, 3) void shared_tile_kernel(const Sha
         if (mask) sa_mask(s, k0, lim, hh);
         sa_maximum(st, s);
         st.l += sa_weights<false>(st, s, pw, none);
-        if (!pre && __any(t.lim < min(most, k0 + kAtK)) && sa_not_finite(v, s)) {
+        if (mask && __any(lim < k0 + tokens) && sa_not_finite(v, s)) {
             sa_add_not_finite(st, smem + SO + kAtTile, pw, hh);
             sa_read_v<SO>(ad, v);
             sa_take_out(v);
@@ -778,7 +855,8 @@ __global__ __launch_bounds__(kStWaves * 64, 3) void shared_tile_kernel(const Sha
     }
     const RowPair ls = swap32(st.l);
     const float l = ls.a + ls.b, inv = l == 0.f ? 0.f : 1.0f / l;
-    uint16_t* out = reinterpret_cast<uint16_t*>(a.o) + (size_t)max(t.row, 0) * a.o_ld + t.head * kHeadDim + hh * 8;
+    uint16_t* out = reinterpret_cast<uint16_t*>(a.o) + (size_t)row * a.o_ld + head * kHeadDim + hh * 8;
+    const bool write = pair < o.end && seq >= 0;
     // 8 dims of a piece are in both halves of the wave: one half takes even pieces, the other odd ones
 #pragma unroll
     for (int g4 = 0; g4 < 8; g4 += 2) {
@@ -786,7 +864,7 @@ __global__ __launch_bounds__(kStWaves * 64, 3) void shared_tile_kernel(const Sha
         const int e = 4 * (g4 & 3);
         const auto r0 = __builtin_amdgcn_permlane32_swap(bf16x2_rne(x[e] * inv, x[e + 1] * inv), bf16x2_rne(x[e + 4] * inv, x[e + 5] * inv), false, false);
         const auto r1 = __builtin_amdgcn_permlane32_swap(bf16x2_rne(x[e + 2] * inv, x[e + 3] * inv), bf16x2_rne(x[e + 6] * inv, x[e + 7] * inv), false, false);
-        if (t.row >= 0) *reinterpret_cast<uint4*>(out + g4 * 8) = make_uint4(r0[0], r1[0], r0[1], r1[1]);
+        if (write) *reinterpret_cast<uint4*>(out + g4 * 8) = make_uint4(r0[0], r1[0], r0[1], r1[1]);
     }
 }
 
@@ -987,21 +1065,27 @@ static SharedPlan shared_plan(bool f32, int n_head, int n_kv_head, int B, int ro
     return p;
 }
 
-// Tiles of 128 rows for shared_tile_kernel, 0 if the call is to be cut along the tokens.  The first walks all of a
-// row's pages in one chain (1.1 us a page while the workgroups fit the chip, about 600 of them), the second pays for
-// another launch, 1.4 ns for 32 rows and a page, and 0.7 ns for a row's partials.  Fitted to 555 calls of both
-// (20/20, 20/4 and 8/1 heads, 1 to 32 sequences of 2 to 1024 rows, prefixes of 0 to 6000): the worse of the two is
-// taken in few, and costs 0.4% of a call on average.  Cut and tiled, us, 20 heads behind 1000 tokens: 32 sequences
-// of 4 rows each 13 / 22, of 32 rows 29 / 24, of 256 rows 139 / 70; one of 1024 rows behind 6000 97 / 117.  Own
-// lengths are on the device, so the table's width stands for them on both sides.
-static int shared_tiles(const SharedAttnArgs& a) {
+// Tiles of 128 rows for shared_tile_kernel, 0 if the call is to be cut along the tokens.  A tile's pages are one chain,
+// 0.8 us a page (packed: 0.88) while a unit has one workgroup, 256 of them, and so many times that where it has more; in
+// its own tiles a sequence has half of one to spare, packed it meets the own pages of 1 + (B - 1) / tiles sequences.
+// The cut pays for another launch, 1.65 ns for 32 rows and a page (own pages, often past a sequence's end: 0.8 of that),
+// and 0.53 ns for a row's partials.  Fitted to 29,004 calls of all three (20/20, 20/4, 32/16, 12/12, 8/8 and 8/1 heads,
+// 1 to 64 sequences of 1 to 1024 rows, prefixes of 0 to 5800 tokens): the least of them missed costs 0.8% of a call on
+// average.  Cut, tiled and packed, us, 20 heads: 32 sequences of 4 rows each behind 1000 tokens 13 / 22 / 37, of 20-220 behind 600
+// 72 / 43 / 36, 64 of 36-58 behind 4000 203 / 174 / 92, 24 of 52-191 with up to 695 tokens behind 563 116 / 43 / 75.  Own lengths
+// are on the device, so the table's width stands for them.
+static int shared_tiles(const SharedAttnArgs& a, bool* pack) {
     if (!a.row_offsets) return 0;
-    const int64_t g = a.n_head / a.n_kv_head, pairs = a.rows * g, tiles = pairs / (kStWaves * kSaQ) + a.B;
-    const double pages = (double)ceil_div(a.prefix_len, kPage), own = a.max_pages;
-    const double tile = 5.0 + 1.1 * (pages + own) * std::max(1.0, (double)tiles * a.n_kv_head / 600);
-    const double cut = 9.0 + 1.4e-3 * a.n_kv_head * ((double)ceil_div(pairs, kSaQ) * pages + (double)(pairs / kSaQ + a.B) * own) +
-                       0.7e-3 * (double)a.rows * a.n_head;
-    return tile <= cut ? (int)tiles : 0;
+    const int64_t pairs = (int64_t)a.rows * (a.n_head / a.n_kv_head), tiles = ceil_div(pairs, kStWaves * kSaQ);
+    const double KH = a.n_kv_head, pages = (double)ceil_div(a.prefix_len, kPage), own = a.max_pages;
+    const double t_own = (double)pairs / (kStWaves * kSaQ) + 0.5 * a.B, with = 1.0 + (double)(a.B - 1) / tiles;
+    const double plain = 5.5 + 0.8 * (pages + 1.1 * own) * std::max(1.0, t_own * KH / 256);
+    const double packed = 5.5 + 0.88 * (pages + 1.1 * own * with) * std::max(1.0, tiles * KH / 256);
+    const double cut = 9.0 + 1.65e-3 * KH * ((double)ceil_div(pairs, kSaQ) * pages + 0.8 * ((double)pairs / kSaQ + a.B) * own) +
+                       0.53e-3 * (double)a.rows * a.n_head;
+    if (std::min(plain, packed) > cut) return 0;
+    *pack = packed < plain;
+    return (int)(*pack ? tiles : pairs / (kStWaves * kSaQ) + a.B);
 }
 
 // Whether shared_whole_kernel takes a call of one row a sequence.  Its chain is a quarter of a sequence's pages (0.3 us
@@ -1032,9 +1116,12 @@ size_t shared_attention_bytes(int n_head, int rows, int prefix_len, int max_page
 hipError_t launch_shared_attention(int dtype, const SharedAttnArgs& a, void* ws, size_t ws_bytes, hipStream_t st) {
     const bool f32 = dtype == FTTS_F32;
     if (a.row_offsets && (a.q_f32 || a.o_f32)) return hipErrorInvalidValue;  // (the decode step's forms)
-    const int tiles = f32 ? 0 : shared_tiles(a);
+    bool pack = false;
+    const int tiles = f32 ? 0 : shared_tiles(a, &pack);
     if (tiles > 0) {
-        hipLaunchKernelGGL(shared_tile_kernel, dim3((unsigned)(tiles * a.n_kv_head)), dim3(kStWaves * 64), 0, st, a, tiles);
+        const dim3 wg((unsigned)(tiles * a.n_kv_head)), wt(kStWaves * 64);
+        if (pack) hipLaunchKernelGGL(shared_tile_kernel<true>, wg, wt, 0, st, a, tiles);
+        else hipLaunchKernelGGL(shared_tile_kernel<false>, wg, wt, 0, st, a, tiles);
         return hipGetLastError();
     }
     if (!f32 && shared_whole(a)) {

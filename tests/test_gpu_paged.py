@@ -175,8 +175,8 @@ class Batch:
 
 
 def kernel(b):
-    """Which of the launcher's kernels a call takes: "whole" (one row a sequence, one launch), "tile" (128 rows share
-    pages, one launch) or "cut" (along the tokens, joined); fp32 is always cut."""
+    """Which of the launcher's kernels a call takes: "whole" (one row a sequence, one launch), "tile" (128 rows of a
+    sequence share pages, one launch), "packed" (128 rows of all) or "cut" (along the tokens, joined); fp32 is always cut."""
     if b.f32:
         return "cut"
     B, g, pages, own = len(b.lens), b.H // b.KH, -(-b.P // 64), b.width
@@ -185,10 +185,11 @@ def kernel(b):
         whole = 4.0 + 0.3 * (pages + own) * max(1.0, tiles * b.KH / 300)
         fits = pages + own <= 256 and whole <= 8.0 + 1e-3 * b.KH * (pages * -(-B * g // 32) + tiles * min(own, 16))
         return "whole" if fits else "cut"
-    tiles = b.T * g // 128 + B
-    tile = 5.0 + 1.1 * (pages + own) * max(1.0, tiles * b.KH / 600)
-    cut = 9.0 + 1.4e-3 * b.KH * (-(-b.T * g // 32) * pages + (b.T * g // 32 + B) * own) + 0.7e-3 * b.T * b.H
-    return "tile" if tile <= cut else "cut"
+    pairs, tiles = b.T * g, -(-b.T * g // 128)
+    tile = 5.5 + 0.8 * (pages + 1.1 * own) * max(1.0, (pairs / 128 + 0.5 * B) * b.KH / 256)
+    packed = 5.5 + 0.88 * (pages + 1.1 * own * (1 + (B - 1) / tiles)) * max(1.0, tiles * b.KH / 256)
+    cut = 9.0 + 1.65e-3 * b.KH * (-(-pairs // 32) * pages + 0.8 * (pairs / 32 + B) * own) + 0.53e-3 * b.T * b.H
+    return "cut" if min(tile, packed) > cut else "packed" if packed < tile else "tile"
 
 
 def test_the_cases_take_every_kernel():
@@ -257,6 +258,73 @@ def test_prompt_rows_of_wider_batches(dtype, H, KH, prefix, rows):
     print(f"wide prompt: {dtype} {H}/{KH} heads, {len(rows)} sequences", flush=True)
     b.call()
     b.check()
+
+
+def packed_batch(H, KH, prefix, B, longest, seed):
+    """Short prompts in tiles of 128 rows that go over sequences' ends: sequences without rows, of one row, with cached
+    tokens, inactive, with fewer tokens than rows, rows before the first sequence and behind the last."""
+    rng = np.random.default_rng(seed)
+    rows = rng.integers(1, longest + 1, B).tolist()
+    rows[0], rows[5], rows[6], rows[7], rows[B - 1] = 1, 0, 0, 130, 2
+    lens = [n + (int(rng.integers(0, 100)) if i % 6 == 1 else 0) for i, n in enumerate(rows)]
+    b = Batch("bf16", H, KH, prefix, lens, rows, extra_rows=7, seed=seed, layers=1)
+    b.lens[3], b.lens[9], b.lens[10] = -1, rows[9] - 1, 0
+    b.cu = b.cu + 3
+    return b
+
+
+@pytest.mark.parametrize("H,KH,prefix,B,longest", [
+    (20, 20, 333, 40, 80), (20, 20, 64, 40, 70), (24, 8, 500, 64, 50), (18, 6, 1000, 64, 60), (32, 16, 1, 64, 70)])
+def test_prompts_that_share_row_tiles(H, KH, prefix, B, longest):
+    b = packed_batch(H, KH, prefix, B, longest, 3).gpu()
+    takes = kernel(b)
+    print(f"packed prompts: {H}/{KH} heads, prefix {prefix}, {B} sequences: {takes}", flush=True)
+    assert takes == ("packed" if prefix > 64 else "tile")
+    b.call()
+    torch.cuda.synchronize()
+    for seq in range(B):
+        if b.rows[seq] and b.lens[seq] >= 0:
+            ref, got = reference64(b, seq, list(range(b.rows[seq])))
+            assert (got - ref).norm() <= 2.0 ** -8 * ref.norm() and (got - ref).abs().max() <= 2.0 ** -7 * ref.abs().max(), seq
+    assert (b.out[b.cu[3]:b.cu[4]] == 0).all()
+    assert (b.out[:3] == -7).all() and (b.out[-4:] == -7).all()
+
+
+def test_prompts_that_share_row_tiles_over_many_pages():
+    """Chains whose 64th page is one of the prefix, or in the middle of the sequences' own ones."""
+    for prefix in (64 * 61 + 5, 64 * 70):
+        b = packed_batch(20, 20, prefix, 40, 60, 8).gpu()
+        assert kernel(b) == "packed"
+        print(f"packed prompts behind {prefix}", flush=True)
+        b.call()
+        torch.cuda.synchronize()
+        for seq in (0, 1, 7, 20, 39):
+            ref, got = reference64(b, seq, sorted({0, b.rows[seq] // 2, b.rows[seq] - 1}))
+            assert (got - ref).norm() <= 2.0 ** -8 * ref.norm(), seq
+
+
+def test_values_that_are_not_finite_stay_with_their_sequence():
+    """A sequence's own page of NaN and infinities changes no row of the others in its row tile, nor of an inactive
+    sequence a prefix's."""
+    b = packed_batch(20, 20, 333, 40, 80, 5).gpu()
+    assert kernel(b) == "packed"
+    b.call()
+    clean = b.out.clone()
+    r = slice(int(b.cu[4]), int(b.cu[5]))
+    for what in (float("nan"), float("inf")):
+        pool = b.pool.copy()
+        pool[0, b.table[4, 0], 1, :, 0] = what
+        b.kv.pool.copy_(torch.from_numpy(pool))
+        b.call()
+        torch.cuda.synchronize()
+        assert torch.equal(b.out[:r.start], clean[:r.start]) and torch.equal(b.out[r.stop:], clean[r.stop:])
+        assert not torch.isfinite(b.out[r].float()).any()
+    pool = b.pool.copy()
+    pool[0, b.pre[1], :, :, 7] = np.nan
+    b.kv.pool.copy_(torch.from_numpy(pool))
+    b.call()
+    torch.cuda.synchronize()
+    assert (b.out[b.cu[3]:b.cu[4]] == 0).all() and torch.isnan(b.out[r].float()).all()
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -331,7 +399,7 @@ def reference64(b, seq, rows):
     out = torch.empty_like(q)
     for h in range(b.H):
         s = q[:, h] @ k[:, h].T / 8
-        seen = b.P + b.lens[seq] - n + torch.tensor(rows, device="cuda") + 1
+        seen = (b.P + b.lens[seq] - n + torch.tensor(rows, device="cuda") + 1).clamp(min=b.P)
         s = s.masked_fill(torch.arange(len(pg), device="cuda")[None] >= seen[:, None], -float("inf"))
         out[:, h] = torch.softmax(s, -1) @ v[:, h]
     return out, b.out[first + torch.tensor(rows, device="cuda")].double().view_as(out)
