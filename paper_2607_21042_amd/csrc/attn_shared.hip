@@ -14,6 +14,7 @@
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
+#include <utility>
 
 #include "attn_tile.hpp"
 #include "decode_entry.hpp"
@@ -22,17 +23,17 @@ namespace ftts {
 
 constexpr int kSaWaves = 2, kSaQ = 32;
 
-// How a call is cut: prefix rows in row_tiles tiles of 32, own rows in own_tiles (an upper bound
+// How a call is cut: prefix rows in row_tiles tiles of q_pre, own rows in own_tiles of q_own (an upper bound
 // where the rows per sequence are on the device); c_pre and c_own pages a workgroup, s_pre and
 // s_own workgroups along the tokens; partials of slot s (prefix slots first) at ml + s * T H and
 // o + s * T H * 64.
 struct SharedPlan {
-    int row_tiles, own_tiles, c_pre, s_pre, c_own, s_own;
+    int q_pre, q_own, row_tiles, own_tiles, c_pre, s_pre, c_own, s_own;
     float2* ml;
     float* o;
 };
 
-// The rows of a workgroup: 32 (token, query head) pairs that read one key head.
+// The rows of a workgroup: up to 32 (token, query head) pairs that read one key head.
 struct RowTile {
     int row, head;   // this lane's pair; row -1: none
     int lim;         // the tokens of the segment that it sees
@@ -40,9 +41,9 @@ struct RowTile {
     bool inactive;   // the sequence has no length
 };
 
-// Tile `tile` of all rows (the prefix's side).
-__device__ __forceinline__ RowTile prefix_rows(const SharedAttnArgs& a, int tile, int kh, int ql) {
-    const int g = a.n_head / a.n_kv_head, idx = tile * kSaQ + ql;
+// Tile `tile` of `size` of all rows (the prefix's side).
+__device__ __forceinline__ RowTile prefix_rows(const SharedAttnArgs& a, int tile, int size, int kh, int ql) {
+    const int g = a.n_head / a.n_kv_head, idx = tile * size + ql;
     RowTile t;
     t.row = idx / g < a.rows ? idx / g : -1;
     t.head = kh * g + idx % g;
@@ -88,9 +89,9 @@ __device__ __forceinline__ int own_seen(const SharedAttnArgs& a, int len, int n,
     return len < 0 ? 0 : (int)min(max((int64_t)len - n + i + 1, (int64_t)0), (int64_t)a.max_pages * kPage);
 }
 __device__ __forceinline__ int own_seen(const SharedAttnArgs& a, const OwnTile& t, int i) { return own_seen(a, t.len, t.n, i); }
-// The 32 pairs from `first` on, one a lane pair.
-__device__ __forceinline__ RowTile own_rows(const SharedAttnArgs& a, const OwnTile& o, int first, int kh, int ql) {
-    const int g = a.n_head / a.n_kv_head, idx = first + ql, last = min(first + kSaQ, o.n * g) - 1;
+// The `size` pairs from `first` on.
+__device__ __forceinline__ RowTile own_rows(const SharedAttnArgs& a, const OwnTile& o, int first, int size, int kh, int ql) {
+    const int g = a.n_head / a.n_kv_head, idx = first + ql, last = min(first + size, o.n * g) - 1;
     RowTile t;
     t.row = idx <= last ? o.row0 + idx / g : -1;
     t.head = kh * g + idx % g;
@@ -325,19 +326,20 @@ __device__ __forceinline__ int early_id(const int32_t* p) {
     return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
 }
 
-// What a workgroup of the cut call does: 32 rows, one key head, a run of pages.
+// What a workgroup of the cut call does: a tile of rows, one key head, a run of pages.
 struct PartWork {
     RowTile t;
     const int32_t* ids;  // its pages
-    int kh, page0, pages;
+    int size, kh, page0, pages;
     int id0;             // page 2 * lane + wave of the run
     int64_t part;        // where this lane's row leaves its partial
 };
 // Prefix work comes first: the row tiles of one (key head, run of pages) are 8 workgroups apart, so that one XCD
 // (workgroups are dealt to the 8 in turn) reads the run through its L2.  False: nothing to do (what has no pages
 // says so in its slot).
+template <bool SIZES>  // tiles as the plan says, else 32 rows
 __device__ __forceinline__ bool part_work(const SharedAttnArgs& a, const SharedPlan& pl, int tid, PartWork& w) {
-    const int lane = tid & 63, ql = lane & 31, j0 = (tid >> 6) + kSaWaves * lane;
+    const int lane = tid & 63, j0 = (tid >> 6) + kSaWaves * lane;
     int id = blockIdx.x, slot;
     const int n_pre = (a.n_kv_head * pl.s_pre + 7) / 8 * 8 * pl.row_tiles;
     if (id < n_pre) {
@@ -345,7 +347,8 @@ __device__ __forceinline__ bool part_work(const SharedAttnArgs& a, const SharedP
         if (pair >= a.n_kv_head * pl.s_pre) return false;
         w.kh = pair % a.n_kv_head;
         slot = pair / a.n_kv_head;
-        w.t = prefix_rows(a, tile, w.kh, ql);
+        w.size = SIZES ? pl.q_pre : kSaQ;
+        w.t = prefix_rows(a, tile, w.size, w.kh, lane & (w.size - 1));
         w.page0 = slot * pl.c_pre;
         w.pages = min(pl.c_pre, (a.prefix_len + kPage - 1) / kPage - w.page0);
         w.ids = a.prefix_pages + w.page0;
@@ -355,18 +358,19 @@ __device__ __forceinline__ bool part_work(const SharedAttnArgs& a, const SharedP
         w.kh = id % a.n_kv_head;
         const int sp = id / a.n_kv_head % pl.s_own, tile = id / a.n_kv_head / pl.s_own;
         w.page0 = sp * pl.c_own;
-        const OwnTile o = own_tile(a, tile, kSaQ, lane);
+        w.size = SIZES ? pl.q_own : kSaQ;
+        const OwnTile o = own_tile(a, tile, w.size, lane);
         if (o.b >= a.B) return false;
         w.ids = a.block_table + (size_t)o.b * a.max_pages + w.page0;
         w.id0 = early_id(w.ids + min(j0, a.max_pages - 1 - w.page0));
-        w.t = own_rows(a, o, o.first, w.kh, ql);
+        w.t = own_rows(a, o, o.first, w.size, w.kh, lane & (w.size - 1));
         slot = pl.s_pre + sp;
         w.pages = min(pl.c_own, (w.t.most + kPage - 1) / kPage - w.page0);
     }
     w.part = slot * ((int64_t)a.rows * a.n_head) + (int64_t)w.t.row * a.n_head + w.t.head;
     if (w.pages > 0) return true;
     // (an inactive sequence is marked by a negative sum)
-    if (w.t.row >= 0 && tid < kSaQ) pl.ml[w.part] = make_float2(-INFINITY, w.t.inactive ? -1.f : 0.f);
+    if (w.t.row >= 0 && tid < w.size) pl.ml[w.part] = make_float2(-INFINITY, w.t.inactive ? -1.f : 0.f);
     return false;
 }
 // Joins the waves' results through LDS (every wave is done with smem) and leaves the partial.
@@ -415,7 +419,7 @@ __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_kernel(const Sha
     __shared__ __attribute__((aligned(1024))) char smem[kSaWaves * kAtStage];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hh = lane >> 5;
     PartWork w;
-    if (!part_work(a, pl, tid, w)) return;
+    if (!part_work<false>(a, pl, tid, w)) return;
     const RowTile& t = w.t;
     char* own = smem + wave * kAtStage;
     const int n = w.pages > wave ? (w.pages - wave + kSaWaves - 1) / kSaWaves : 0;  // this wave's pages
@@ -492,8 +496,7 @@ __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_kernel(const Sha
 // fp32: the same on 32-token halves of pages (the same 16 KB a stage) with fp32 matrix products, all sums in fp32.  A
 // 16-byte piece c of row r lies at c ^ (r % 16).  K as the first operand: lane (key, hh) holds dims 32 hh .. + 31, one
 // a step; V: lane (dim, hh) holds the key that element i of the scores is for.  Bound by the products: 8192 cycles a
-// wave and page, whatever the rows, so a wave takes one page where there are enough: 8 sequences of 30-500 tokens behind
-// 700, 20 heads, 16.8 + 3.9 us (two pages a wave: 24 + 3); a wave a row on the vector units took 450.
+// wave and page, whatever the rows, so a wave takes one page where there are enough.
 constexpr int kSfK = 32;
 __device__ __forceinline__ void sf_read_k(const uint32_t (&kr)[8], float4 (&k)[8]) {
     at_bf16x8 x[8];  // (any 16-byte register type)
@@ -550,13 +553,134 @@ __device__ __forceinline__ void sf_add_not_finite(SaState& a, const char* vt, co
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 }
 
+// fp32, tiles of 4 rows (one row a sequence): 4x4x1 products of 16 blocks.  Scores: a block's 4 keys by the 4 rows,
+// so that lane (block, row) holds 4 keys' scores; values: 4 rows by a block's 4 dims, the weights of one block's key
+// handed to all blocks by the instruction.  1024 cycles a page where a tile of 32 takes 8192.  K goes through LDS, whole
+// pages; V's rows go straight into registers, lane by dim.  8 sequences of 30-500 tokens behind 700, 20 heads: 12.9 us
+// with the join (tiles of 32: 19.2), 32 of them 24.6 (37.3); there bound by reading (105 MB), here by the chain.
+constexpr int kSfFew = 4;
+typedef float sf_f32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ void sf_load_v(const char* src, int bytes, int lane, float (&v)[kPage]) {
+#ifdef __HIP_DEVICE_COMPILE__
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(src), 0, bytes, 0x00020000);
+#pragma unroll
+    for (int k = 0; k < kPage; ++k)
+        v[k] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rsrc, lane * 4 + k * 256, 0, 0));
+#endif
+}
+template <int... B>  // the blocks of 4 keys
+__device__ __forceinline__ void sf_pv(const float (&p)[4], const float (&v)[kPage], sf_f32x4 (&o)[2], std::integer_sequence<int, B...>) {
+    ((o[0] = __builtin_amdgcn_mfma_f32_4x4x1f32(p[0], v[4 * B], o[0], 4, B, 0),
+      o[1] = __builtin_amdgcn_mfma_f32_4x4x1f32(p[1], v[4 * B + 1], o[1], 4, B, 0),
+      o[0] = __builtin_amdgcn_mfma_f32_4x4x1f32(p[2], v[4 * B + 2], o[0], 4, B, 0),
+      o[1] = __builtin_amdgcn_mfma_f32_4x4x1f32(p[3], v[4 * B + 3], o[1], 4, B, 0)), ...);
+}
+__device__ __forceinline__ void part_few(const SharedAttnArgs& a, const SharedPlan& pl, const PartWork& w, char* smem, int wave, int lane) {
+    const int n = w.pages > wave ? (w.pages - wave + kSaWaves - 1) / kSaWaves : 0;  // this wave's pages
+    const size_t to_v = (size_t)a.n_kv_head * (kPage * kHeadDim * 4);
+    char* own = smem + wave * kAtStage;
+    PageRef page{};
+    auto fetch = [&](int j0) {  // the wave's pages j0 .. j0 + 63, one a lane
+        const int j = w.page0 + wave + kSaWaves * (j0 + lane);
+        const int id = j0 == 0 ? w.id0 : j0 + lane < n ? w.ids[j - w.page0] : -1;
+        page = page_ref(a, w.kh, 4, id, j0 + lane < n ? w.t.most - j * kPage : 0);
+    };
+    float4 q[16];
+    {
+        const float* qp = reinterpret_cast<const float*>(a.q) + (size_t)max(w.t.row, 0) * a.q_ld + w.t.head * kHeadDim;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) q[i] = *reinterpret_cast<const float4*>(qp + 4 * i);
+    }
+    float m = -INFINITY, l = 0.f;  // of this lane's row; l over this lane's keys
+    sf_f32x4 o[2] = {};            // of the 4 rows, in dim `lane`
+    float v[kPage];
+    for (int u = 0; u < n; ++u) {
+        if ((u & 63) == 0) fetch(u);
+        const int tokens = __builtin_amdgcn_readlane(page.tokens, u & 63);
+        const char* src = page_at(a, page, u & 63);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int row = i * 4 + (lane >> 4);
+            buffer_to_lds16(src, tokens * 256, own + i * 1024, row * 256 + (((lane & 15) ^ (row & 15)) << 4), 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        sf_load_v(src + to_v, tokens * 256, lane, v);
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_waitcnt vmcnt(63)" ::: "memory");  // the 16 loads of K are in, 63 of V's 64 may be out
+        __builtin_amdgcn_sched_barrier(0);
+        sf_f32x4 s[4] = {};
+#pragma unroll
+        for (int c = 0; c < 16; ++c) {
+            const float4 k = *reinterpret_cast<const float4*>(own + lane * 256 + ((c ^ (lane & 15)) << 4));
+            s[0] = __builtin_amdgcn_mfma_f32_4x4x1f32(k.x, q[c].x, s[0], 0, 0, 0);
+            s[1] = __builtin_amdgcn_mfma_f32_4x4x1f32(k.y, q[c].y, s[1], 0, 0, 0);
+            s[2] = __builtin_amdgcn_mfma_f32_4x4x1f32(k.z, q[c].z, s[2], 0, 0, 0);
+            s[3] = __builtin_amdgcn_mfma_f32_4x4x1f32(k.w, q[c].w, s[3], 0, 0, 0);
+        }
+        float p[4], tmax = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            p[i] = (lane & ~3) + i < tokens ? (s[0][i] + s[1][i]) + (s[2][i] + s[3][i]) : -INFINITY;
+            tmax = __builtin_elementwise_maximum(tmax, p[i]);
+        }
+#pragma unroll
+        for (int d = 4; d < kWave; d <<= 1) tmax = __builtin_elementwise_maximum(tmax, __shfl_xor(tmax, d, kWave));
+        tmax *= kSaScale;
+        if (__any(tmax > m + 8.f)) {
+            const float mn = fmaxf(m, tmax), alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+            m = mn;
+            l *= alpha;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float x = __shfl(alpha, i, kWave);
+                o[0][i] *= x;
+                o[1][i] *= x;
+            }
+        }
+        const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            p[i] = __builtin_amdgcn_exp2f(fmaf(p[i], kSaScale, -ref));
+            l += p[i];
+        }
+        sf_pv(p, v, o, std::make_integer_sequence<int, 16>{});
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    o[0] += o[1];
+#pragma unroll
+    for (int d = 4; d < kWave; d <<= 1) l += __shfl_xor(l, d, kWave);
+    __syncthreads();
+    float* mw = reinterpret_cast<float*>(smem);  // the second wave's, lane for lane
+    if (wave > 0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mw[i * 64 + lane] = o[0][i];
+        mw[4 * 64 + lane] = m;
+        mw[5 * 64 + lane] = l;
+    }
+    __syncthreads();
+    if (wave > 0) return;
+    const float m1 = mw[4 * 64 + lane], mm = fmaxf(m, m1), ref = mm == -INFINITY ? 0.f : mm;
+    const float f0 = exp2f(m - ref), f1 = exp2f(m1 - ref);
+    if (lane < kSfFew && w.t.row >= 0) pl.ml[w.part] = make_float2(mm, l * f0 + mw[5 * 64 + lane] * f1);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {  // row i, its partial's place and weights from lane i
+        const float x = o[0][i] * __shfl(f0, i, kWave) + mw[i * 64 + lane] * __shfl(f1, i, kWave);
+        const int64_t part = __shfl(w.part, i, kWave);
+        if (__shfl(w.t.row, i, kWave) >= 0) pl.o[part * kHeadDim + lane] = x;
+    }
+}
+
 template <bool PROMPT>
 __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_f32_kernel(const SharedAttnArgs a, const SharedPlan pl) {
     __shared__ __attribute__((aligned(1024))) char smem[kSaWaves * kAtStage];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int ql = lane & 31, hh = lane >> 5;
     PartWork w;
-    if (!part_work(a, pl, tid, w)) return;
+    if (!part_work<!PROMPT>(a, pl, tid, w)) return;
+    if (!PROMPT && w.size == kSfFew) {
+        part_few(a, pl, w, smem, wave, lane);
+        return;
+    }
     const RowTile& t = w.t;
     char* own = smem + wave * kAtStage;
     const int n = w.pages > wave ? 2 * ((w.pages - wave + kSaWaves - 1) / kSaWaves) : 0;  // this wave's half pages
@@ -882,7 +1006,7 @@ __global__ __launch_bounds__(kSwWaves * 64, 2) void shared_whole_kernel(const Sh
     const OwnTile o = own_tile(a, blockIdx.x / a.n_kv_head, kSaQ, lane);
     const int id0 = early_id(j0 < n_pre ? a.prefix_pages + j0
                                         : a.block_table + (size_t)o.b * a.max_pages + min(j0 - n_pre, a.max_pages - 1));
-    const RowTile t = own_rows(a, o, o.first, kh, lane & 31);
+    const RowTile t = own_rows(a, o, o.first, kSaQ, kh, lane & 31);
     const int P = a.prefix_len, pages = t.inactive ? 0 : n_pre + (t.most + kPage - 1) / kPage;
     const int n = pages > wave ? (pages - wave + kSwWaves - 1) / kSwWaves : 0;  // this wave's pages: wave, wave + 4, ...
     char* own = smem + wave * kAtStage;
@@ -1046,6 +1170,11 @@ __global__ __launch_bounds__(kJoinWaves * 64) void shared_join_kernel(const Shar
 // wide that the grid would pass kOwnGroups workgroups (most of them past their sequence's end).  Prefix: so many that
 // about kPreFew workgroups share it (few rows: bound by reading, and each workgroup leaves 8 KB of partials) or
 // kPreMany (many rows, or fp32: bound by the products), at most kMaxSplit along it.
+//
+// fp32, one row a sequence: tiles of 4 rows cost each row as much in products as 32, but read the pages 8 times as
+// often.  So a sequence's own rows take them up to 8 a key head (two tiles), and the prefix's where they are few or the
+// whole prefix is little work (a tile, key head and page each): 4 sequences of 20/4 heads behind 700 8.6 us (32 rows: 11.8),
+// 16 of 12/12 behind 3000 15.2 (18.9), 32 of 20/20 behind 700 27.7 (24.7).
 constexpr int kOwnGroups = 8192, kPreFew = 256, kPreMany = 640, kMaxSplit = 64;
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
@@ -1053,8 +1182,11 @@ static SharedPlan shared_plan(bool f32, int n_head, int n_kv_head, int B, int ro
     const int g = n_head / n_kv_head;
     const int64_t pages = ceil_div(prefix_len, kPage);
     SharedPlan p{};
-    p.row_tiles = (int)ceil_div((int64_t)rows * g, kSaQ);
-    p.own_tiles = prompt ? (int)((int64_t)rows * g / kSaQ) + B : B * (int)ceil_div(g, kSaQ);
+    const int64_t few = f32 && !prompt ? ceil_div((int64_t)rows * g, kSfFew) : 0;
+    p.q_pre = few && (few <= 4 || few * n_kv_head * pages <= 1024) ? kSfFew : kSaQ;
+    p.q_own = few && g <= 2 * kSfFew ? kSfFew : kSaQ;
+    p.row_tiles = (int)ceil_div((int64_t)rows * g, p.q_pre);
+    p.own_tiles = prompt ? (int)((int64_t)rows * g / kSaQ) + B : B * (int)ceil_div(g, p.q_own);
     const int64_t groups = f32 || p.row_tiles > 4 ? kPreMany : kPreFew;
     const int64_t c_pre = std::max({(int64_t)2, ceil_div(pages * n_kv_head * p.row_tiles, groups), ceil_div(pages, kMaxSplit)});
     const int64_t c_own = std::max((int64_t)(f32 ? 2 : 4), ceil_div((int64_t)max_pages * n_kv_head * p.own_tiles, kOwnGroups));
@@ -1071,9 +1203,9 @@ static SharedPlan shared_plan(bool f32, int n_head, int n_kv_head, int B, int ro
 // The cut pays for another launch, 1.65 ns for 32 rows and a page (own pages, often past a sequence's end: 0.8 of that),
 // and 0.53 ns for a row's partials.  Fitted to 29,004 calls of all three (20/20, 20/4, 32/16, 12/12, 8/8 and 8/1 heads,
 // 1 to 64 sequences of 1 to 1024 rows, prefixes of 0 to 5800 tokens): the least of them missed costs 0.8% of a call on
-// average.  Cut, tiled and packed, us, 20 heads: 32 sequences of 4 rows each behind 1000 tokens 13 / 22 / 37, of 20-220 behind 600
-// 72 / 43 / 36, 64 of 36-58 behind 4000 203 / 174 / 92, 24 of 52-191 with up to 695 tokens behind 563 116 / 43 / 75.  Own lengths
-// are on the device, so the table's width stands for them.
+// average.  Cut, tiled and packed, us, 20 heads: 32 sequences of 4 rows each behind 1000 tokens 13 / 23 / 67, of 32 36 / 25 / 29,
+// of 20-220 behind 600 94 / 44 / 36, 64 of 36-58 behind 4000 186 / 174 / 91, 24 of 52-191 with up to 695 tokens behind 563
+// 105 / 45 / 79, one of 1024 behind 6000 102 / 122 / 122.  Own lengths are on the device, so the table's width stands for them.
 static int shared_tiles(const SharedAttnArgs& a, bool* pack) {
     if (!a.row_offsets) return 0;
     const int64_t pairs = (int64_t)a.rows * (a.n_head / a.n_kv_head), tiles = ceil_div(pairs, kStWaves * kSaQ);
