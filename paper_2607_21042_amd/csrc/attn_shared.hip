@@ -10,7 +10,7 @@
 //          belong to, and each sequence's rows meet its own pages; both kinds of work are cut along the tokens into
 //          workgroups that leave partial results, and a second kernel joins them.  Bound by reading the pages once.
 //   whole  one row a sequence and few pages: a workgroup a sequence and key head, no partials.
-//   tile   many rows: 128 rows share each page on its way through LDS.  Bound by vector and matrix work.
+//   tile   many rows: 128 rows, of one sequence or of several, share each page on its way through LDS.  Bound by vector and matrix work.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -411,8 +411,8 @@ __device__ __forceinline__ void part_finish(const SharedPlan& pl, const PartWork
 //
 // Two waves a workgroup: one wave each measured 1-2 us better for 32 short sequences and 2 worse behind long prefixes,
 // four 1-3 worse nearly everywhere (more idle waves at a run's end).  Traced with the join: 32 sequences of 64-700 tokens
-// behind 1500, 20 heads, 18.6 + 4.0 us for 76 MB; 64 of 100-900 behind 16,001 54 + 5 us for 255 MB (a read reaches
-// 5.9 TB/s: 12.9 and 43 us); 24 of up to 1200 behind 5000, 20 query and 4 key heads, 10 + 4.5 for 22 MB: there a chain of
+// behind 1500, 20 heads, 17.9 + 3.9 us for 76 MB; 64 of 100-900 behind 16,001 53 + 5 us for 255 MB (a read reaches
+// 5.9 TB/s: 12.9 and 43 us); 24 of up to 1200 behind 5000, 20 query and 4 key heads, 9.9 + 3.6 for 22 MB: there a chain of
 // page ids, keys, products, values and the hand-over, not bytes.
 template <bool PROMPT, bool Q32>
 __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_kernel(const SharedAttnArgs a, const SharedPlan pl) {
@@ -855,16 +855,18 @@ __device__ __forceinline__ TilePages tile_pages(const SharedAttnArgs& a, int til
 
 // Many rows: one workgroup per key head and run of 128 rows, whose waves (32 rows each) share 64-token tiles of the
 // prefix and then of the sequences' own pages.  Where many short prompts follow a long prefix a run goes over sequences'
-// ends (packed: a wave passes the own pages of sequences that it has no row of), else each sequence begins one.  Tiles come in whole pages of
-// a head, 8 KB of keys and of values, by direct-to-LDS loads into two stages, a tile ahead; one barrier a tile; three
-// workgroups a CU.  The weights go into the products as bf16 (rounded once; their sum takes the rounded ones).
+// ends (packed: a wave passes the own pages of sequences that it has no row of), else each sequence begins one.  Tiles
+// come in whole pages of a head, 8 KB of keys and of values, by direct-to-LDS loads into two stages, a tile ahead; one
+// barrier a tile; three workgroups a CU.  The weights go into the products as bf16 (rounded once; their sum takes the
+// rounded ones).
 //
-// Four prompts of 1500-2300 rows behind 8000 tokens, 20 heads: 497 us, 790 TFLOP/s (a library product of 8192^3: 1460).
-// Counted there: matrix units busy 34% of the time, vector units 45% (32 exponentials of 8 cycles and about 114
-// operations of 4 a tile of 32 rows and a page), both at once 10%, and 15% of the units' time at the launch's ends.  Measured and not
-// taken: three stages, 64 rows a wave (spills), two waves a workgroup (more loads), the next tile's scores under this
-// one's exponentials (two waves a SIMD: 637 us), half a tile's weights under the other half's products (spills: 525),
-// the maximum of the first tile alone with a second pass where a sum overflows (488, not worth its second path).
+// Four prompts of 1500-2300 rows behind 8000 tokens, 20 heads: 500 us, 785 TFLOP/s (a library product of 8192^3: 1460);
+// 32 of 20-220 behind 600 36 us (a tile for each sequence: 44).  Counted for the long ones: matrix units busy 34% of the
+// time, vector units 45% (32 exponentials of 8 cycles and about 114 operations of 4 a tile of 32 rows and a page), both
+// at once 10%, and 15% of the units' time at the launch's ends.  Measured and not taken: three stages, 64 rows a wave
+// (spills), two waves a workgroup (more loads), the next tile's scores under this one's exponentials (two waves a SIMD:
+// 637 us), half a tile's weights under the other half's products (spills: 525), the maximum of the first tile alone with
+// a second pass where a sum overflows (488, not worth its second path).
 constexpr int kStWaves = 4;
 template <bool PACK>
 __global__ __launch_bounds__(kStWaves * 64, 3) void shared_tile_kernel(const SharedAttnArgs a, int tiles) {
