@@ -404,6 +404,196 @@ __device__ __forceinline__ void part_finish(const SharedPlan& pl, const PartWork
     }
 }
 
+// Tiles of 4 rows (one row a sequence): products of 16 blocks of 4x4.  Scores: a block's 4 keys by the 4 rows, so that
+// lane (block, row) holds 4 keys' scores; values: 4 rows by a block's 4 dims, the weights of one block's keys handed to
+// all blocks by the instruction.  The state: the lane's row's maximum, its sum over the lane's keys, and the 4 rows'
+// outputs in dim `lane`.
+constexpr int kFew = 4;
+typedef float few_f32x4 __attribute__((ext_vector_type(4)));
+struct FewState {
+    float m = -INFINITY, l = 0.f;
+    few_f32x4 o[2] = {};  // (two chains of products)
+};
+// The scores p of a page (-inf: not seen) to weights.
+__device__ __forceinline__ void few_weights(FewState& a, float (&p)[4]) {
+    float tmax = __builtin_elementwise_maximum(__builtin_elementwise_maximum(p[0], p[1]), __builtin_elementwise_maximum(p[2], p[3]));
+#pragma unroll
+    for (int d = 4; d < 16; d <<= 1) tmax = __builtin_elementwise_maximum(tmax, __shfl_xor(tmax, d, kWave));
+    const RowPair p16 = swap16(tmax);
+    const RowPair p32 = swap32(__builtin_elementwise_maximum(p16.a, p16.b));
+    tmax = __builtin_elementwise_maximum(p32.a, p32.b) * kSaScale;
+    if (__any(tmax > a.m + 8.f)) {  // as sa_maximum
+        const float mn = fmaxf(a.m, tmax), alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(a.m - mn);
+        a.m = mn;
+        a.l *= alpha;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float x = __shfl(alpha, i, kWave);
+            a.o[0][i] *= x;
+            a.o[1][i] *= x;
+        }
+    }
+    const float ref = a.m == -INFINITY ? 0.f : a.m;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        p[i] = __builtin_amdgcn_exp2f(fmaf(p[i], kSaScale, -ref));
+        a.l += p[i];
+    }
+}
+// As part_finish.
+__device__ __forceinline__ void few_finish(const SharedPlan& pl, const PartWork& w, FewState& st, char* smem, int wave, int lane) {
+    static_assert(kSaWaves == 2, "one wave hands over to the other");
+    st.o[0] += st.o[1];
+#pragma unroll
+    for (int d = 4; d < kWave; d <<= 1) st.l += __shfl_xor(st.l, d, kWave);
+    __syncthreads();
+    float* mw = reinterpret_cast<float*>(smem) + lane;  // [6][64], lane for lane
+    if (wave > 0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mw[i * 64] = st.o[0][i];
+        mw[4 * 64] = st.m;
+        mw[5 * 64] = st.l;
+    }
+    __syncthreads();
+    if (wave > 0) return;
+    const float m1 = mw[4 * 64], mm = fmaxf(st.m, m1), ref = mm == -INFINITY ? 0.f : mm;
+    const float f0 = exp2f(st.m - ref), f1 = exp2f(m1 - ref), l = st.l * f0 + mw[5 * 64] * f1;
+    if (lane < kFew && w.t.row >= 0) pl.ml[w.part] = make_float2(mm, l);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {  // row i: its weights and its partial's place are lane i's
+        const float o = st.o[0][i] * __shfl(f0, i, kWave) + mw[i * 64] * __shfl(f1, i, kWave);
+        const int64_t part = __shfl(w.part, i, kWave);
+        if (__shfl(w.t.row, i, kWave) >= 0) pl.o[part * kHeadDim + lane] = o;
+    }
+}
+
+// bf16: K and V through LDS as in shared_part_kernel.  32 sequences of 64-700 tokens behind 1500, 20 heads: 18.2 us with
+// the join (tiles of 32 rows: 20.1), 8 of 30-500 behind 700 10.1 (11.3).  Two groups of 4 rows a tile, for 5 to 8 query
+// heads a key head, were slower than one tile of 32: 14.4 us for 24 sequences of 20/4 heads (13.6).
+typedef short few_s16x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ few_s16x4 few_op(uint32_t x, uint32_t y) { return __builtin_bit_cast(few_s16x4, make_uint2(x, y)); }
+// A page's keys, lane by key (kr: its 16-byte pieces).
+__device__ __forceinline__ void few_read_k(const uint32_t (&kr)[8], uint4 (&k)[8]) {
+    at_bf16x8 x[8];
+    asm volatile(
+        "ds_read_b128 %0, %8\n\tds_read_b128 %1, %9\n\tds_read_b128 %2, %10\n\tds_read_b128 %3, %11\n\t"
+        "ds_read_b128 %4, %12\n\tds_read_b128 %5, %13\n\tds_read_b128 %6, %14\n\tds_read_b128 %7, %15\n\ts_waitcnt lgkmcnt(0)"
+        : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7])
+        : "v"(kr[0]), "v"(kr[1]), "v"(kr[2]), "v"(kr[3]), "v"(kr[4]), "v"(kr[5]), "v"(kr[6]), "v"(kr[7])
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 8; ++i) k[i] = __builtin_bit_cast(uint4, x[i]);
+}
+// v[b] = values of keys 4 b .. 4 b + 3 in dim `lane` (vr: the lane's 8 bytes of keys 4 b .. + 3, b % 4).
+__device__ __forceinline__ void few_read_v(const uint32_t (&vr)[4], uint64_t (&v)[16]) {
+#define SA_TR(O, A, S) "ds_read_b64_tr_b16 %" #O ", %" #A " offset:" #S "\n\t"
+    asm volatile(
+        SA_TR(0, 16, 0) SA_TR(1, 17, 0) SA_TR(2, 18, 0) SA_TR(3, 19, 0) SA_TR(4, 16, 2048) SA_TR(5, 17, 2048) SA_TR(6, 18, 2048)
+        SA_TR(7, 19, 2048) SA_TR(8, 16, 4096) SA_TR(9, 17, 4096) SA_TR(10, 18, 4096) SA_TR(11, 19, 4096) SA_TR(12, 16, 6144)
+        SA_TR(13, 17, 6144) SA_TR(14, 18, 6144) SA_TR(15, 19, 6144) "s_waitcnt lgkmcnt(0)"
+        : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]), "=&v"(v[4]), "=&v"(v[5]), "=&v"(v[6]), "=&v"(v[7]),
+          "=&v"(v[8]), "=&v"(v[9]), "=&v"(v[10]), "=&v"(v[11]), "=&v"(v[12]), "=&v"(v[13]), "=&v"(v[14]), "=&v"(v[15])
+        : "v"(vr[0]), "v"(vr[1]), "v"(vr[2]), "v"(vr[3])
+        : "memory");
+#undef SA_TR
+}
+template <int... B>  // the blocks of 4 keys; pl: what the weights' rounding left
+__device__ __forceinline__ void few_pv(FewState& a, few_s16x4 p, few_s16x4 pl, const uint64_t (&v)[16], std::integer_sequence<int, B...>) {
+    ((a.o[0] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(p, __builtin_bit_cast(few_s16x4, v[B]), a.o[0], 4, B, 0),
+      a.o[1] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(pl, __builtin_bit_cast(few_s16x4, v[B]), a.o[1], 4, B, 0)), ...);
+}
+template <bool Q32>
+__device__ __forceinline__ void few_part(const SharedAttnArgs& a, const SharedPlan& pl, const PartWork& w, char* smem, int wave, int lane) {
+    const int n = w.pages > wave ? (w.pages - wave + kSaWaves - 1) / kSaWaves : 0;  // this wave's pages
+    const size_t to_v = (size_t)a.n_kv_head * kAtTile;
+    char* own = smem + wave * kAtStage;
+    PageRef page{};
+    auto fetch = [&](int j0) {  // the wave's pages j0 .. j0 + 63, one a lane
+        const int j = w.page0 + wave + kSaWaves * (j0 + lane);
+        const int id = j0 == 0 ? w.id0 : j0 + lane < n ? w.ids[j - w.page0] : -1;
+        page = page_ref(a, w.kh, 2, id, j0 + lane < n ? w.t.most - j * kPage : 0);
+    };
+    auto load = [&](int j, int kv) {  // as shared_part_kernel's
+        const int tokens = __builtin_amdgcn_readlane(page.tokens, j & 63);
+        const char* src = page_at(a, page, j & 63) + kv * to_v;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int row = i * 8 + (lane >> 3);
+            buffer_to_lds16(src, tokens * 128, own + kv * kAtTile + i * 1024, row * 128 + (((lane & 7) ^ ((row >> 1) & 7)) << 4), 0);
+        }
+        return tokens;
+    };
+    uint4 q[8];
+    const size_t q0 = (size_t)max(w.t.row, 0) * a.q_ld + w.t.head * kHeadDim;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if constexpr (Q32) {
+            const float* qp = reinterpret_cast<const float*>(a.q) + q0 + 8 * i;
+            const float4 x = *reinterpret_cast<const float4*>(qp), y = *reinterpret_cast<const float4*>(qp + 4);
+            q[i] = make_uint4(bf16x2_rne(x.x, x.y), bf16x2_rne(x.z, x.w), bf16x2_rne(y.x, y.y), bf16x2_rne(y.z, y.w));
+        } else {
+            q[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(a.q) + q0 + 8 * i);
+        }
+    }
+    uint32_t kr[8], vr[4];
+    {
+        const uint32_t s0 = lds_address(own);
+        const int i16 = lane & 15;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) kr[c] = s0 + lane * 128 + ((c ^ ((lane >> 1) & 7)) << 4);
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const int row = 4 * b + (i16 >> 2), piece = 2 * (lane >> 4) + ((i16 & 3) >> 1);
+            vr[b] = s0 + kAtTile + row * 128 + ((piece ^ ((row >> 1) & 7)) << 4) + (i16 & 1) * 8;
+        }
+    }
+    FewState st;
+    int next = 0;
+    if (n > 0) {
+        fetch(0);
+        next = load(0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        load(0, 1);
+    }
+    for (int j = 0; j < n; ++j) {
+        const bool more = j + 1 < n;
+        const int tokens = next;
+        asm volatile("s_waitcnt vmcnt(8)" ::: "memory");  // K is in (this wave's own loads), V's 8 loads may be out
+        __builtin_amdgcn_sched_barrier(0);
+        uint4 k[8];
+        few_read_k(kr, k);
+        __builtin_amdgcn_sched_barrier(0);
+        if (more) {
+            if (((j + 1) & 63) == 0) fetch(j + 1);
+            next = load(j + 1, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        few_f32x4 s[2] = {};
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            s[0] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(few_op(k[c].x, k[c].y), few_op(q[c].x, q[c].y), s[0], 0, 0, 0);
+            s[1] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(few_op(k[c].z, k[c].w), few_op(q[c].z, q[c].w), s[1], 0, 0, 0);
+        }
+        float p[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[i] = (lane & ~3) + i < tokens ? s[0][i] + s[1][i] : -INFINITY;
+        few_weights(st, p);
+        const uint32_t h0 = bf16x2_rne(p[0], p[1]), h1 = bf16x2_rne(p[2], p[3]);
+        const uint32_t l0 = bf16x2_rne(p[0] - bf16lo(h0), p[1] - bf16hi(h0)), l1 = bf16x2_rne(p[2] - bf16lo(h1), p[3] - bf16hi(h1));
+        __builtin_amdgcn_sched_barrier(0);
+        if (more) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");  // V is in, the next K may be out
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        uint64_t v[16];
+        few_read_v(vr, v);
+        __builtin_amdgcn_sched_barrier(0);
+        if (more) load(j + 1, 1);
+        __builtin_amdgcn_sched_barrier(0);
+        few_pv(st, few_op(h0, h1), few_op(l0, l1), v, std::make_integer_sequence<int, 16>{});
+    }
+    few_finish(pl, w, st, smem, wave, lane);
+}
+
 // bf16: the waves take a run's pages in turn (wave w: w, w + 2, ...) by direct-to-LDS loads into a stage of their own,
 // the next page's K (V) on its way once this one's is in registers; no barrier in the loop.  The weights go into the
 // products as bf16 and what their rounding left, so that only the output is rounded (the second product is free where
@@ -419,7 +609,8 @@ __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_kernel(const Sha
     __shared__ __attribute__((aligned(1024))) char smem[kSaWaves * kAtStage];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hh = lane >> 5;
     PartWork w;
-    if (!part_work<false>(a, pl, tid, w)) return;
+    if (!part_work<!PROMPT>(a, pl, tid, w)) return;
+    if (!PROMPT && w.size == kFew) return few_part<Q32>(a, pl, w, smem, wave, lane);
     const RowTile& t = w.t;
     char* own = smem + wave * kAtStage;
     const int n = w.pages > wave ? (w.pages - wave + kSaWaves - 1) / kSaWaves : 0;  // this wave's pages
@@ -553,13 +744,9 @@ __device__ __forceinline__ void sf_add_not_finite(SaState& a, const char* vt, co
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 }
 
-// fp32, tiles of 4 rows (one row a sequence): 4x4x1 products of 16 blocks.  Scores: a block's 4 keys by the 4 rows,
-// so that lane (block, row) holds 4 keys' scores; values: 4 rows by a block's 4 dims, the weights of one block's key
-// handed to all blocks by the instruction.  1024 cycles a page where a tile of 32 takes 8192.  K goes through LDS, whole
+// fp32, tiles of 4 rows: 1024 cycles of 4x4x1 products a page where a tile of 32 takes 8192.  K goes through LDS, whole
 // pages; V's rows go straight into registers, lane by dim.  8 sequences of 30-500 tokens behind 700, 20 heads: 12.9 us
 // with the join (tiles of 32: 19.2), 32 of them 24.6 (37.3); there bound by reading (105 MB), here by the chain.
-constexpr int kSfFew = 4;
-typedef float sf_f32x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ void sf_load_v(const char* src, int bytes, int lane, float (&v)[kPage]) {
 #ifdef __HIP_DEVICE_COMPILE__
     const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(src), 0, bytes, 0x00020000);
@@ -569,13 +756,13 @@ __device__ __forceinline__ void sf_load_v(const char* src, int bytes, int lane, 
 #endif
 }
 template <int... B>  // the blocks of 4 keys
-__device__ __forceinline__ void sf_pv(const float (&p)[4], const float (&v)[kPage], sf_f32x4 (&o)[2], std::integer_sequence<int, B...>) {
-    ((o[0] = __builtin_amdgcn_mfma_f32_4x4x1f32(p[0], v[4 * B], o[0], 4, B, 0),
-      o[1] = __builtin_amdgcn_mfma_f32_4x4x1f32(p[1], v[4 * B + 1], o[1], 4, B, 0),
-      o[0] = __builtin_amdgcn_mfma_f32_4x4x1f32(p[2], v[4 * B + 2], o[0], 4, B, 0),
-      o[1] = __builtin_amdgcn_mfma_f32_4x4x1f32(p[3], v[4 * B + 3], o[1], 4, B, 0)), ...);
+__device__ __forceinline__ void sf_few_pv(FewState& a, const float (&p)[4], const float (&v)[kPage], std::integer_sequence<int, B...>) {
+    ((a.o[0] = __builtin_amdgcn_mfma_f32_4x4x1f32(p[0], v[4 * B], a.o[0], 4, B, 0),
+      a.o[1] = __builtin_amdgcn_mfma_f32_4x4x1f32(p[1], v[4 * B + 1], a.o[1], 4, B, 0),
+      a.o[0] = __builtin_amdgcn_mfma_f32_4x4x1f32(p[2], v[4 * B + 2], a.o[0], 4, B, 0),
+      a.o[1] = __builtin_amdgcn_mfma_f32_4x4x1f32(p[3], v[4 * B + 3], a.o[1], 4, B, 0)), ...);
 }
-__device__ __forceinline__ void part_few(const SharedAttnArgs& a, const SharedPlan& pl, const PartWork& w, char* smem, int wave, int lane) {
+__device__ __forceinline__ void sf_few_part(const SharedAttnArgs& a, const SharedPlan& pl, const PartWork& w, char* smem, int wave, int lane) {
     const int n = w.pages > wave ? (w.pages - wave + kSaWaves - 1) / kSaWaves : 0;  // this wave's pages
     const size_t to_v = (size_t)a.n_kv_head * (kPage * kHeadDim * 4);
     char* own = smem + wave * kAtStage;
@@ -591,8 +778,7 @@ __device__ __forceinline__ void part_few(const SharedAttnArgs& a, const SharedPl
 #pragma unroll
         for (int i = 0; i < 16; ++i) q[i] = *reinterpret_cast<const float4*>(qp + 4 * i);
     }
-    float m = -INFINITY, l = 0.f;  // of this lane's row; l over this lane's keys
-    sf_f32x4 o[2] = {};            // of the 4 rows, in dim `lane`
+    FewState st;
     float v[kPage];
     for (int u = 0; u < n; ++u) {
         if ((u & 63) == 0) fetch(u);
@@ -608,7 +794,7 @@ __device__ __forceinline__ void part_few(const SharedAttnArgs& a, const SharedPl
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("s_waitcnt vmcnt(63)" ::: "memory");  // the 16 loads of K are in, 63 of V's 64 may be out
         __builtin_amdgcn_sched_barrier(0);
-        sf_f32x4 s[4] = {};
+        few_f32x4 s[4] = {};
 #pragma unroll
         for (int c = 0; c < 16; ++c) {
             const float4 k = *reinterpret_cast<const float4*>(own + lane * 256 + ((c ^ (lane & 15)) << 4));
@@ -617,57 +803,14 @@ __device__ __forceinline__ void part_few(const SharedAttnArgs& a, const SharedPl
             s[2] = __builtin_amdgcn_mfma_f32_4x4x1f32(k.z, q[c].z, s[2], 0, 0, 0);
             s[3] = __builtin_amdgcn_mfma_f32_4x4x1f32(k.w, q[c].w, s[3], 0, 0, 0);
         }
-        float p[4], tmax = -INFINITY;
+        float p[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            p[i] = (lane & ~3) + i < tokens ? (s[0][i] + s[1][i]) + (s[2][i] + s[3][i]) : -INFINITY;
-            tmax = __builtin_elementwise_maximum(tmax, p[i]);
-        }
-#pragma unroll
-        for (int d = 4; d < kWave; d <<= 1) tmax = __builtin_elementwise_maximum(tmax, __shfl_xor(tmax, d, kWave));
-        tmax *= kSaScale;
-        if (__any(tmax > m + 8.f)) {
-            const float mn = fmaxf(m, tmax), alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
-            m = mn;
-            l *= alpha;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float x = __shfl(alpha, i, kWave);
-                o[0][i] *= x;
-                o[1][i] *= x;
-            }
-        }
-        const float ref = m == -INFINITY ? 0.f : m;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            p[i] = __builtin_amdgcn_exp2f(fmaf(p[i], kSaScale, -ref));
-            l += p[i];
-        }
-        sf_pv(p, v, o, std::make_integer_sequence<int, 16>{});
+        for (int i = 0; i < 4; ++i) p[i] = (lane & ~3) + i < tokens ? (s[0][i] + s[1][i]) + (s[2][i] + s[3][i]) : -INFINITY;
+        few_weights(st, p);
+        sf_few_pv(st, p, v, std::make_integer_sequence<int, 16>{});
         __builtin_amdgcn_sched_barrier(0);
     }
-    o[0] += o[1];
-#pragma unroll
-    for (int d = 4; d < kWave; d <<= 1) l += __shfl_xor(l, d, kWave);
-    __syncthreads();
-    float* mw = reinterpret_cast<float*>(smem);  // the second wave's, lane for lane
-    if (wave > 0) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) mw[i * 64 + lane] = o[0][i];
-        mw[4 * 64 + lane] = m;
-        mw[5 * 64 + lane] = l;
-    }
-    __syncthreads();
-    if (wave > 0) return;
-    const float m1 = mw[4 * 64 + lane], mm = fmaxf(m, m1), ref = mm == -INFINITY ? 0.f : mm;
-    const float f0 = exp2f(m - ref), f1 = exp2f(m1 - ref);
-    if (lane < kSfFew && w.t.row >= 0) pl.ml[w.part] = make_float2(mm, l * f0 + mw[5 * 64 + lane] * f1);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {  // row i, its partial's place and weights from lane i
-        const float x = o[0][i] * __shfl(f0, i, kWave) + mw[i * 64 + lane] * __shfl(f1, i, kWave);
-        const int64_t part = __shfl(w.part, i, kWave);
-        if (__shfl(w.t.row, i, kWave) >= 0) pl.o[part * kHeadDim + lane] = x;
-    }
+    few_finish(pl, w, st, smem, wave, lane);
 }
 
 template <bool PROMPT>
@@ -677,10 +820,7 @@ __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_f32_kernel(const
     const int ql = lane & 31, hh = lane >> 5;
     PartWork w;
     if (!part_work<!PROMPT>(a, pl, tid, w)) return;
-    if (!PROMPT && w.size == kSfFew) {
-        part_few(a, pl, w, smem, wave, lane);
-        return;
-    }
+    if (!PROMPT && w.size == kFew) return sf_few_part(a, pl, w, smem, wave, lane);
     const RowTile& t = w.t;
     char* own = smem + wave * kAtStage;
     const int n = w.pages > wave ? 2 * ((w.pages - wave + kSaWaves - 1) / kSaWaves) : 0;  // this wave's half pages
@@ -1173,9 +1313,10 @@ __global__ __launch_bounds__(kJoinWaves * 64) void shared_join_kernel(const Shar
 // about kPreFew workgroups share it (few rows: bound by reading, and each workgroup leaves 8 KB of partials) or
 // kPreMany (many rows, or fp32: bound by the products), at most kMaxSplit along it.
 //
-// fp32, one row a sequence: tiles of 4 rows cost each row as much in products as 32, but read the pages 8 times as
-// often.  So a sequence's own rows take them up to 8 a key head (two tiles), and the prefix's where they are few or the
-// whole prefix is little work (a tile, key head and page each): 4 sequences of 20/4 heads behind 700 8.6 us (32 rows: 11.8),
+// Tiles of 4 rows (one row a sequence): a sequence's own rows and the prefix's take them where they are up to 4 a key
+// head.  fp32: they cost each row as much in products as tiles of 32, but read the pages 8 times as often.  So a
+// sequence's own rows take them up to 8 a key head (two tiles), and the prefix's also up to 16 or where the whole prefix
+// is little work (a tile, key head and page each): 4 sequences of 20/4 heads behind 700 8.6 us (32 rows: 11.8),
 // 16 of 12/12 behind 3000 15.2 (18.9), 32 of 20/20 behind 700 27.7 (24.7).
 constexpr int kOwnGroups = 8192, kPreFew = 256, kPreMany = 640, kMaxSplit = 64;
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -1184,9 +1325,9 @@ static SharedPlan shared_plan(bool f32, int n_head, int n_kv_head, int B, int ro
     const int g = n_head / n_kv_head;
     const int64_t pages = ceil_div(prefix_len, kPage);
     SharedPlan p{};
-    const int64_t few = f32 && !prompt ? ceil_div((int64_t)rows * g, kSfFew) : 0;
-    p.q_pre = few && (few <= 4 || few * n_kv_head * pages <= 1024) ? kSfFew : kSaQ;
-    p.q_own = few && g <= 2 * kSfFew ? kSfFew : kSaQ;
+    const int64_t few = prompt ? 0 : ceil_div((int64_t)rows * g, kFew);
+    p.q_pre = few && (f32 ? few <= 4 || few * n_kv_head * pages <= 1024 : few == 1) ? kFew : kSaQ;
+    p.q_own = few && g <= (f32 ? 2 : 1) * kFew ? kFew : kSaQ;
     p.row_tiles = (int)ceil_div((int64_t)rows * g, p.q_pre);
     p.own_tiles = prompt ? (int)((int64_t)rows * g / kSaQ) + B : B * (int)ceil_div(g, p.q_own);
     const int64_t groups = f32 || p.row_tiles > 4 ? kPreMany : kPreFew;
