@@ -502,17 +502,11 @@ __device__ __forceinline__ void few_pv(FewState& a, few_s16x4 p, few_s16x4 pl, c
     ((a.o[0] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(p, __builtin_bit_cast(few_s16x4, v[B]), a.o[0], 4, B, 0),
       a.o[1] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(pl, __builtin_bit_cast(few_s16x4, v[B]), a.o[1], 4, B, 0)), ...);
 }
-template <bool Q32>
-__device__ __forceinline__ void few_part(const SharedAttnArgs& a, const SharedPlan& pl, const PartWork& w, char* smem, int wave, int lane) {
-    const int n = w.pages > wave ? (w.pages - wave + kSaWaves - 1) / kSaWaves : 0;  // this wave's pages
+// The wave's n pages, which fetch hands over one a lane, 64 at a time.
+template <bool Q32, typename Fetch>
+__device__ __forceinline__ void few_pages(const SharedAttnArgs& a, const RowTile& t, int n, char* own, int lane, FewState& st, Fetch fetch) {
     const size_t to_v = (size_t)a.n_kv_head * kAtTile;
-    char* own = smem + wave * kAtStage;
     PageRef page{};
-    auto fetch = [&](int j0) {  // the wave's pages j0 .. j0 + 63, one a lane
-        const int j = w.page0 + wave + kSaWaves * (j0 + lane);
-        const int id = j0 == 0 ? w.id0 : j0 + lane < n ? w.ids[j - w.page0] : -1;
-        page = page_ref(a, w.kh, 2, id, j0 + lane < n ? w.t.most - j * kPage : 0);
-    };
     auto load = [&](int j, int kv) {  // as shared_part_kernel's
         const int tokens = __builtin_amdgcn_readlane(page.tokens, j & 63);
         const char* src = page_at(a, page, j & 63) + kv * to_v;
@@ -524,7 +518,7 @@ __device__ __forceinline__ void few_part(const SharedAttnArgs& a, const SharedPl
         return tokens;
     };
     uint4 q[8];
-    const size_t q0 = (size_t)max(w.t.row, 0) * a.q_ld + w.t.head * kHeadDim;
+    const size_t q0 = (size_t)max(t.row, 0) * a.q_ld + t.head * kHeadDim;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         if constexpr (Q32) {
@@ -547,10 +541,9 @@ __device__ __forceinline__ void few_part(const SharedAttnArgs& a, const SharedPl
             vr[b] = s0 + kAtTile + row * 128 + ((piece ^ ((row >> 1) & 7)) << 4) + (i16 & 1) * 8;
         }
     }
-    FewState st;
     int next = 0;
     if (n > 0) {
-        fetch(0);
+        page = fetch(0);
         next = load(0, 0);
         __builtin_amdgcn_sched_barrier(0);
         load(0, 1);
@@ -564,7 +557,7 @@ __device__ __forceinline__ void few_part(const SharedAttnArgs& a, const SharedPl
         few_read_k(kr, k);
         __builtin_amdgcn_sched_barrier(0);
         if (more) {
-            if (((j + 1) & 63) == 0) fetch(j + 1);
+            if (((j + 1) & 63) == 0) page = fetch(j + 1);
             next = load(j + 1, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -591,6 +584,16 @@ __device__ __forceinline__ void few_part(const SharedAttnArgs& a, const SharedPl
         __builtin_amdgcn_sched_barrier(0);
         few_pv(st, few_op(h0, h1), few_op(l0, l1), v, std::make_integer_sequence<int, 16>{});
     }
+}
+template <bool Q32>
+__device__ __forceinline__ void few_part(const SharedAttnArgs& a, const SharedPlan& pl, const PartWork& w, char* smem, int wave, int lane) {
+    const int n = w.pages > wave ? (w.pages - wave + kSaWaves - 1) / kSaWaves : 0;  // this wave's pages
+    FewState st;
+    few_pages<Q32>(a, w.t, n, smem + wave * kAtStage, lane, st, [&](int j0) {
+        const int j = w.page0 + wave + kSaWaves * (j0 + lane);
+        const int id = j0 == 0 ? w.id0 : j0 + lane < n ? w.ids[j - w.page0] : -1;
+        return page_ref(a, w.kh, 2, id, j0 + lane < n ? w.t.most - j * kPage : 0);
+    });
     few_finish(pl, w, st, smem, wave, lane);
 }
 
@@ -1137,24 +1140,59 @@ __global__ __launch_bounds__(kStWaves * 64, 3) void shared_tile_kernel(const Sha
 // Short contexts, one row a sequence: one workgroup per key head and sequence takes the prefix's pages and the
 // sequence's own, its waves in turn, and writes the result at once: the prefix is read by every sequence (through
 // L2), but there is one launch and no partial.  Bound by its chain (ids, keys, products, values, hand-over): 4
-// sequences of up to 90 tokens behind 134, 20 heads, 6.7 us traced (cut: 4.7 + 3.0 and a second launch).
+// sequences of up to 90 tokens behind 134, 20 heads, 5.3 us (cut: 7.2).  FEW: up to 4 query heads a key head, in tiles
+// of 4 rows (of 32: 6.4).
 constexpr int kSwWaves = 4;
-template <bool Q32>
+template <bool Q32, bool FEW>
 __global__ __launch_bounds__(kSwWaves * 64, 2) void shared_whole_kernel(const SharedAttnArgs a) {
     __shared__ __attribute__((aligned(1024))) char smem[kSwWaves * kAtStage];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hh = lane >> 5;
     const int kh = blockIdx.x % a.n_kv_head;
     const int n_pre = (a.prefix_len + kPage - 1) / kPage, j0 = wave + kSwWaves * lane;
-    const OwnTile o = own_tile(a, blockIdx.x / a.n_kv_head, kSaQ, lane);
+    constexpr int size = FEW ? kFew : kSaQ;
+    const OwnTile o = own_tile(a, blockIdx.x / a.n_kv_head, size, lane);
     const int id0 = early_id(j0 < n_pre ? a.prefix_pages + j0
                                         : a.block_table + (size_t)o.b * a.max_pages + min(j0 - n_pre, a.max_pages - 1));
-    const RowTile t = own_rows(a, o, o.first, kSaQ, kh, lane & 31);
+    const RowTile t = own_rows(a, o, o.first, size, kh, lane & (size - 1));
     const int P = a.prefix_len, pages = t.inactive ? 0 : n_pre + (t.most + kPage - 1) / kPage;
     const int n = pages > wave ? (pages - wave + kSwWaves - 1) / kSwWaves : 0;  // this wave's pages: wave, wave + 4, ...
     char* own = smem + wave * kAtStage;
     const size_t to_v = (size_t)a.n_kv_head * kAtTile;  // from a page's keys to its values
     // lane i: the wave's i-th page (the launcher bounds them by 64)
     const PageRef page = page_ref(a, kh, 2, id0, j0 >= pages ? 0 : j0 < n_pre ? P - j0 * kPage : t.most - (j0 - n_pre) * kPage);
+    if constexpr (FEW) {
+        FewState few;
+        few_pages<Q32>(a, t, n, own, lane, few, [&](int) { return page; });
+        few.o[0] += few.o[1];
+#pragma unroll
+        for (int d = 4; d < kWave; d <<= 1) few.l += __shfl_xor(few.l, d, kWave);
+        __syncthreads();
+        float* mrg = reinterpret_cast<float*>(smem);  // [4][6][64]
+        float* mw = mrg + wave * 6 * 64 + lane;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mw[i * 64] = few.o[0][i];
+        mw[4 * 64] = few.m;
+        mw[5 * 64] = few.l;
+        __syncthreads();
+        static_assert(kSwWaves == kFew, "a wave sums a row");
+        const int row = __shfl(t.row, wave, kWave), head = __shfl(t.head, wave, kWave);
+        if (row < 0) return;
+        float mm = -INFINITY, l = 0.f, x = 0.f;
+#pragma unroll
+        for (int w = 0; w < kSwWaves; ++w) mm = fmaxf(mm, mrg[(w * 6 + 4) * 64 + wave]);
+        const float ref = mm == -INFINITY ? 0.f : mm;
+#pragma unroll
+        for (int w = 0; w < kSwWaves; ++w) {
+            const float f = exp2f(mrg[(w * 6 + 4) * 64 + wave] - ref);
+            l += mrg[(w * 6 + 5) * 64 + wave] * f;
+            x += mrg[(w * 6 + wave) * 64 + lane] * f;
+        }
+        x *= l == 0.f ? 0.f : 1.0f / l;
+        const size_t at = (size_t)row * a.o_ld + head * kHeadDim + lane;
+        if (a.o_f32) reinterpret_cast<float*>(a.o)[at] = x;
+        else reinterpret_cast<uint16_t*>(a.o)[at] = (uint16_t)bf16x2_rne(x, 0.f);
+        return;
+    }
     auto load = [&](int i, int kv) {  // the wave's i-th page, K (kv 0) or V; zeros for what is not seen
         const int tokens = __builtin_amdgcn_readlane(page.tokens, i);
         const char* src = page_at(a, page, i) + kv * to_v;
@@ -1363,19 +1401,19 @@ static int shared_tiles(const SharedAttnArgs& a, bool* pack) {
     return (int)(*pack ? tiles : pairs / (kStWaves * kSaQ) + a.B);
 }
 
-// Whether shared_whole_kernel takes a call of one row a sequence.  Its chain is a quarter of a sequence's pages (0.3 us
-// a page while about 300 workgroups run, two a unit fit), and every sequence reads the prefix; the cut pays for another launch
-// and 1 ns for 32 rows and a page.  Fitted to 432 calls of both (20/20, 4/4 and 20/4 heads, 1 to 64 sequences of up
-// to 1200 tokens behind 0 to 2000): the worse of the two costs 0.4% of a call on average.  Whole and cut, us, 20 heads:
-// 1 sequence of 50 behind 60 5.5 / 7.8, 8 of 250 behind 250 7.5 / 9.2, 8 of 250 behind 1000 12.6 / 10.8, 32 of 250
-// behind 60 14.6 / 14.4, 32 of 1200 behind 2000 56 / 37.  The table's width stands for the own lengths (for the cut, up to
+// Whether shared_whole_kernel takes a call of one row a sequence.  Its chain is a quarter of a sequence's pages (0.32 us
+// a page while about 240 workgroups run), and every sequence reads the prefix; the cut pays for another launch and 1.3 ns
+// for 32 rows and a page.  Fitted to 18,489 calls of both (20/20, 12/12, 8/8, 4/4, 32/16, 20/4 and 8/1 heads, 1 to 64
+// sequences of up to 1200 tokens behind 0 to 2900): the worse of the two costs 0.12% of a call on average.  Whole and cut,
+// us, 20 heads: 1 sequence of 50 behind 60 4.2 / 7.0, 8 of 250 behind 250 6.2 / 8.8, 8 of 250 behind 1000 9.3 / 9.4, 32 of 250
+// behind 60 12.6 / 13.3, 32 of 1200 behind 2000 55 / 43.  The table's width stands for the own lengths (for the cut, up to
 // 16 pages of it: a wide table is rarely full).
 static bool shared_whole(const SharedAttnArgs& a) {
     if (a.row_offsets || ceil_div(a.prefix_len, kPage) + a.max_pages > kWave * kSwWaves) return false;
     const double g = a.n_head / a.n_kv_head, pages = (double)ceil_div(a.prefix_len, kPage), own = a.max_pages;
     const double tiles = (double)a.B * ceil_div(a.n_head / a.n_kv_head, kSaQ);
-    const double whole = 4.0 + 0.3 * (pages + own) * std::max(1.0, tiles * a.n_kv_head / 300);
-    const double cut = 8.0 + 1e-3 * a.n_kv_head * (pages * std::ceil(a.B * g / kSaQ) + tiles * std::min(own, 16.0));
+    const double whole = 3.5 + 0.32 * (pages + own) * std::max(1.0, tiles * a.n_kv_head / 240);
+    const double cut = 8.5 + 1.3e-3 * a.n_kv_head * (pages * std::ceil(a.B * g / kSaQ) + tiles * std::min(own, 16.0));
     return whole <= cut;
 }
 
@@ -1402,8 +1440,11 @@ hipError_t launch_shared_attention(int dtype, const SharedAttnArgs& a, void* ws,
     if (!f32 && shared_whole(a)) {
         const int64_t own_tiles = a.B * ceil_div(a.n_head / a.n_kv_head, kSaQ);
         const dim3 wg((unsigned)(own_tiles * a.n_kv_head)), wt(kSwWaves * 64);
-        if (a.q_f32) hipLaunchKernelGGL(shared_whole_kernel<true>, wg, wt, 0, st, a);
-        else hipLaunchKernelGGL(shared_whole_kernel<false>, wg, wt, 0, st, a);
+        const bool few = a.n_head <= kFew * a.n_kv_head;
+        if (few && a.q_f32) hipLaunchKernelGGL((shared_whole_kernel<true, true>), wg, wt, 0, st, a);
+        else if (few) hipLaunchKernelGGL((shared_whole_kernel<false, true>), wg, wt, 0, st, a);
+        else if (a.q_f32) hipLaunchKernelGGL((shared_whole_kernel<true, false>), wg, wt, 0, st, a);
+        else hipLaunchKernelGGL((shared_whole_kernel<false, false>), wg, wt, 0, st, a);
         return hipGetLastError();
     }
     SharedPlan p = shared_plan(f32, a.n_head, a.n_kv_head, a.B, a.rows, a.row_offsets != nullptr, a.prefix_len, a.max_pages);

@@ -182,8 +182,8 @@ def kernel(b):
     B, g, pages, own = len(b.lens), b.H // b.KH, -(-b.P // 64), b.width
     if b.cu is None:
         tiles = B * -(-g // 32)
-        whole = 4.0 + 0.3 * (pages + own) * max(1.0, tiles * b.KH / 300)
-        fits = pages + own <= 256 and whole <= 8.0 + 1e-3 * b.KH * (pages * -(-B * g // 32) + tiles * min(own, 16))
+        whole = 3.5 + 0.32 * (pages + own) * max(1.0, tiles * b.KH / 240)
+        fits = pages + own <= 256 and whole <= 8.5 + 1.3e-3 * b.KH * (pages * -(-B * g // 32) + tiles * min(own, 16))
         return "whole" if fits else "cut"
     pairs, tiles = b.T * g, -(-b.T * g // 128)
     tile = 5.5 + 0.8 * (pages + 1.1 * own) * max(1.0, (pairs / 128 + 0.5 * B) * b.KH / 256)
@@ -233,6 +233,17 @@ def test_single_token_batches(dtype, B, prefix, lens):
     rng = np.random.default_rng(B)
     b = Batch(dtype, 3, 3, prefix, lens or rng.integers(-2, 150, B).tolist()).gpu()
     print(f"single token batch: {dtype} B {B}, prefix {prefix}", flush=True)
+    b.call()
+    b.check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,KH,B,prefix", [(4, 1, 3, 70), (8, 1, 1, 900), (16, 2, 3, 900), (9, 1, 2, 900), (17, 1, 5, 40),
+                                           (33, 1, 3, 0), (40, 1, 2, 1500)])
+def test_many_query_heads_a_key_head(dtype, H, KH, B, prefix):
+    """Rows that fill their tiles of 4 and 32, pass them by one, and need several."""
+    b = Batch(dtype, H, KH, prefix, [70, 300, 1, 0, 513][:B]).gpu()
+    print(f"query heads: {dtype} {H}/{KH}, B {B}, prefix {prefix}: {kernel(b)}", flush=True)
     b.call()
     b.check()
 
