@@ -604,8 +604,8 @@ __device__ __forceinline__ void few_part(const SharedAttnArgs& a, const SharedPl
 //
 // Two waves a workgroup: one wave each measured 1-2 us better for 32 short sequences and 2 worse behind long prefixes,
 // four 1-3 worse nearly everywhere (more idle waves at a run's end).  Traced with the join: 32 sequences of 64-700 tokens
-// behind 1500, 20 heads, 17.9 + 3.9 us for 76 MB; 64 of 100-900 behind 16,001 53 + 5 us for 255 MB (a read reaches
-// 5.9 TB/s: 12.9 and 43 us); 24 of up to 1200 behind 5000, 20 query and 4 key heads, 9.9 + 3.6 for 22 MB: there a chain of
+// behind 1500, 20 heads, 15.9 + 3.9 us for 76 MB; 64 of 100-900 behind 16,001 50 + 5 us for 255 MB (a read reaches
+// 5.9 TB/s: 12.9 and 43 us); 24 of up to 1200 behind 5000, 20 query and 4 key heads, 10 + 3.7 for 22 MB: there a chain of
 // page ids, keys, products, values and the hand-over, not bytes.
 template <bool PROMPT, bool Q32>
 __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_kernel(const SharedAttnArgs a, const SharedPlan pl) {
@@ -1003,7 +1003,7 @@ __device__ __forceinline__ TilePages tile_pages(const SharedAttnArgs& a, int til
 // barrier a tile; three workgroups a CU.  The weights go into the products as bf16 (rounded once; their sum takes the
 // rounded ones).
 //
-// Four prompts of 1500-2300 rows behind 8000 tokens, 20 heads: 500 us, 785 TFLOP/s (a library product of 8192^3: 1460);
+// Four prompts of 1500-2300 rows behind 8000 tokens, 20 heads: 491 us, 800 TFLOP/s (a library product of 8192^3: 1460);
 // 32 of 20-220 behind 600 36 us (a tile for each sequence: 44).  Counted for the long ones: matrix units busy 34% of the
 // time, vector units 45% (32 exponentials of 8 cycles and about 114 operations of 4 a tile of 32 rows and a page), both
 // at once 10%, and 15% of the units' time at the launch's ends.  Measured and not taken: three stages, 64 rows a wave
