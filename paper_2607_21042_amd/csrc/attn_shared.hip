@@ -5,12 +5,13 @@
 //
 // A softmax over two disjoint sets of tokens is joined from (m, l, o) of each: m = max(m1, m2),
 // l = l1 e^(m1 - m) + l2 e^(m2 - m), o likewise.  Four kernels share that, chosen by rules on sizes
-// (shared_whole, shared_tiles):
+// (shared_whole, tile_plan):
 //   cut    (shared_part_*_kernel): the batch's rows meet the prefix as one matrix, whatever sequence they
 //          belong to, and each sequence's rows meet its own pages; both kinds of work are cut along the tokens into
 //          workgroups that leave partial results, and a second kernel joins them.  Bound by reading the pages once.
 //   whole  one row a sequence and few pages: a workgroup a sequence and key head, no partials.
-//   tile   many rows: 128 rows, of one sequence or of several, share each page on its way through LDS.  Bound by vector and matrix work.
+//   tile   many rows: 128 rows, of one sequence or of several, share each page on its way through LDS; a long chain of
+//          pages of few tiles is cut into parts, which the second kernel joins.  Bound by vector and matrix work.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -1011,27 +1012,33 @@ __device__ __forceinline__ TilePages tile_pages(const SharedAttnArgs& a, int til
 // 637 us), half a tile's weights under the other half's products (spills: 525), the maximum of the first tile alone with
 // a second pass where a sum overflows (488, not worth its second path).
 constexpr int kStWaves = 4;
-template <bool PACK>
-__global__ __launch_bounds__(kStWaves * 64, 3) void shared_tile_kernel(const SharedAttnArgs a, int tiles) {
+template <bool PACK, bool CUT>
+__global__ __launch_bounds__(kStWaves * 64, 3) void shared_tile_kernel(const SharedAttnArgs a, int tiles, const SharedPlan pl) {
     constexpr int kRows = kStWaves * kSaQ, kLoads = 8 / kStWaves;
     __shared__ __attribute__((aligned(1024))) char smem[2 * kAtStage];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int ql = lane & 31, hh = lane >> 5;
     // Each XCD (workgroups are dealt to the 8 in turn) gets a contiguous run of (key head, tile), tiles fastest, so
     // that a head's pages are read through one L2.
-    int tile, kh;
+    int tile, kh, part = 0;
     {
         const int T = gridDim.x, i = blockIdx.x, x = i & 7, q = T >> 3, r = T & 7;
         const int t = (x < r ? x * (q + 1) : r * (q + 1) + (x - r) * q) + (i >> 3);
         tile = t % tiles;
         kh = t / tiles;
+        if constexpr (CUT) {
+            part = kh % pl.s_pre;
+            kh /= pl.s_pre;
+        }
     }
     const int g = a.n_head / a.n_kv_head;
     const TilePages o = tile_pages<PACK>(a, tile, kRows, lane);
     if (o.first >= o.end) return;
-    const int P = a.prefix_len, n = o.n_pre + o.n_own;
+    const int P = a.prefix_len, all = o.n_pre + o.n_own;
+    const int per = CUT ? (all + pl.s_pre - 1) / pl.s_pre : all, j0 = CUT ? min(part * per, all) : 0, n = min(per, all - j0);
     // This lane's pair, the tile's last one where it is past it (which is not written twice).
     const int pair = o.first + wave * kSaQ + ql, row = min(pair, o.end - 1) / g, head = kh * g + min(pair, o.end - 1) % g;
+    bool inactive = false;
     int seq = -1, own_lim = 0, pre_lim = 0;  // its sequence, the own tokens and those of the prefix that it sees
     for (uint64_t m = o.seqs; m; m &= m - 1) {
         const int b = __builtin_ctzll(m), r0 = __builtin_amdgcn_readlane(o.row0, b), rn = __builtin_amdgcn_readlane(o.n, b);
@@ -1039,7 +1046,8 @@ __global__ __launch_bounds__(kStWaves * 64, 3) void shared_tile_kernel(const Sha
         if (row < r0 || row >= r0 + rn) continue;
         seq = b;
         own_lim = own_seen(a, len, rn, row - r0);
-        pre_lim = len < 0 ? 0 : P;
+        inactive = len < 0;
+        pre_lim = inactive ? 0 : P;
     }
     const bool rows = o.first + wave * kSaQ < o.end;
     SaState st;
@@ -1049,8 +1057,8 @@ __global__ __launch_bounds__(kStWaves * 64, 3) void shared_tile_kernel(const Sha
     const size_t to_v = (size_t)a.n_kv_head * kAtTile;  // from a page's keys to its values
     PageRef page{};
     int whose = 0;  // the page's sequence (kWave: the prefix) and its number there, in the low 24 bits
-    auto fetch = [&](int j0) {  // pages j0 .. j0 + 63 of the chain, one a lane
-        const int j = j0 + lane, own = j - o.n_pre;
+    auto fetch = [&](int i) {  // the workgroup's pages i .. i + 63, one a lane
+        const int j = j0 + i + lane, own = j - o.n_pre;
         const int32_t* id = own < 0 ? a.prefix_pages + j : nullptr;
         int left = P - j * kPage;
         whose = kWave << 24 | j;
@@ -1062,7 +1070,7 @@ __global__ __launch_bounds__(kStWaves * 64, 3) void shared_tile_kernel(const Sha
             left = most - k * kPage;
             whose = b << 24 | k;
         }
-        page = page_ref(a, kh, 2, id && j < n ? *id : -1, left);
+        page = page_ref(a, kh, 2, id && j < all ? *id : -1, left);
     };
     uint32_t vo[kLoads];
 #pragma unroll
@@ -1124,6 +1132,18 @@ __global__ __launch_bounds__(kStWaves * 64, 3) void shared_tile_kernel(const Sha
     }
     const RowPair ls = swap32(st.l);
     const float l = ls.a + ls.b, inv = l == 0.f ? 0.f : 1.0f / l;
+    if constexpr (CUT) {
+        if (pair >= o.end || seq < 0) return;
+        const int64_t at = part * ((int64_t)a.rows * a.n_head) + (int64_t)row * a.n_head + head;
+        if (hh == 0) pl.ml[at] = make_float2(st.m, inactive ? -1.f : l);
+        float4* to = reinterpret_cast<float4*>(pl.o + at * kHeadDim) + hh;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            to[2 * e] = make_float4(st.o0[4 * e], st.o0[4 * e + 1], st.o0[4 * e + 2], st.o0[4 * e + 3]);
+            to[8 + 2 * e] = make_float4(st.o1[4 * e], st.o1[4 * e + 1], st.o1[4 * e + 2], st.o1[4 * e + 3]);
+        }
+        return;
+    }
     uint16_t* out = reinterpret_cast<uint16_t*>(a.o) + (size_t)row * a.o_ld + head * kHeadDim + hh * 8;
     const bool write = pair < o.end && seq >= 0;
     // 8 dims of a piece are in both halves of the wave: one half takes even pieces, the other odd ones
@@ -1378,27 +1398,46 @@ static SharedPlan shared_plan(bool f32, int n_head, int n_kv_head, int B, int ro
     return p;
 }
 
-// Tiles of 128 rows for shared_tile_kernel, 0 if the call is to be cut along the tokens.  A tile's pages are one chain,
-// 0.8 us a page (packed: 0.88) while a unit has one workgroup, 256 of them, and so many times that where it has more; in
-// its own tiles a sequence has half of one to spare, packed it meets the own pages of 1 + (B - 1) / tiles sequences.
-// The cut pays for another launch, 1.65 ns for 32 rows and a page (own pages, often past a sequence's end: 0.8 of that),
-// and 0.53 ns for a row's partials.  Fitted to 29,004 calls of all three (20/20, 20/4, 32/16, 12/12, 8/8 and 8/1 heads,
-// 1 to 64 sequences of 1 to 1024 rows, prefixes of 0 to 5800 tokens): the least of them missed costs 0.8% of a call on
-// average.  Cut, tiled and packed, us, 20 heads: 32 sequences of 4 rows each behind 1000 tokens 13 / 23 / 67, of 32 36 / 25 / 29,
-// of 20-220 behind 600 94 / 44 / 36, 64 of 36-58 behind 4000 186 / 174 / 91, 24 of 52-191 with up to 695 tokens behind 563
-// 105 / 45 / 79, one of 1024 behind 6000 102 / 122 / 122.  Own lengths are on the device, so the table's width stands for them.
-static int shared_tiles(const SharedAttnArgs& a, bool* pack) {
-    if (!a.row_offsets) return 0;
-    const int64_t pairs = (int64_t)a.rows * (a.n_head / a.n_kv_head), tiles = ceil_div(pairs, kStWaves * kSaQ);
-    const double KH = a.n_kv_head, pages = (double)ceil_div(a.prefix_len, kPage), own = a.max_pages;
-    const double t_own = (double)pairs / (kStWaves * kSaQ) + 0.5 * a.B, with = 1.0 + (double)(a.B - 1) / tiles;
-    const double plain = 5.5 + 0.8 * (pages + 1.1 * own) * std::max(1.0, t_own * KH / 256);
-    const double packed = 5.5 + 0.88 * (pages + 1.1 * own * with) * std::max(1.0, tiles * KH / 256);
-    const double cut = 9.0 + 1.65e-3 * KH * ((double)ceil_div(pairs, kSaQ) * pages + 0.8 * ((double)pairs / kSaQ + a.B) * own) +
-                       0.53e-3 * (double)a.rows * a.n_head;
-    if (std::min(plain, packed) > cut) return 0;
-    *pack = packed < plain;
-    return (int)(*pack ? tiles : pairs / (kStWaves * kSaQ) + a.B);
+// How shared_tile_kernel takes a call: 128-row tiles, whether they go over sequences' ends, and the workgroups along a
+// tile's chain of pages.
+struct TilePlan {
+    int tiles, parts;  // tiles 0: the call is cut into tiles of 32
+    bool pack;
+};
+// A tile's pages are one chain, 0.8 us a page (packed: 0.88) while a unit has one workgroup, 256 of them, and so many
+// times that where it has more; in its own tiles a sequence has half of one to spare, packed it meets the own pages of
+// 1 + (B - 1) / tiles sequences.  Parts of a chain pay for another launch and a row's partials, 0.7 us a page (packed:
+// 0.77), and half a round of units more where the last one is not full.  Tiles of 32 pay for the other launch, 1.65 ns
+// for 32 rows and a page (own pages, often past a sequence's end: 0.8 of that), and 0.53 ns for a row's partials.
+// Fitted to 29,004 calls of tiles of 32, of 128 and packed (20/20, 20/4, 32/16, 12/12, 8/8 and 8/1 heads, 1 to 64
+// sequences of 1 to 1024 rows, prefixes of 0 to 8100 tokens), and 8,954 calls of those and of 2 to 16 parts: the least of
+// eleven times missed costs 1.5% of a call on average.  Tiles of 32, of 128 and packed, us, 20 heads: 32 sequences of
+// 4 rows each behind 1000 tokens 13 / 23 / 67, of 20-220 behind 600 97 / 45 / 37, 64 of 36-58 behind 4000 190 / 176 / 91,
+// 24 of 52-191 with up to 695 tokens behind 563 106 / 46 / 79.  Tiles of 32, of 128 and those in 2, 4 and 8 parts: one of
+// 1024 behind 6000 103 / 121 / 83 / 65 / 67, 2 of 56-361 behind 6000, 20/4 heads, 58 / 112 / 66 / 47 / 42.  Own lengths
+// are on the device, so the table's width stands for them.
+static TilePlan tile_plan(const SharedAttnArgs& a) {
+    TilePlan best{0, 1, false};
+    if (!a.row_offsets) return best;
+    const int64_t pairs = (int64_t)a.rows * (a.n_head / a.n_kv_head), tiles = ceil_div(pairs, kStWaves * kSaQ), pages = ceil_div(a.prefix_len, kPage);
+    const double KH = a.n_kv_head, own = a.max_pages, row_heads = (double)a.rows * a.n_head;
+    double least = 9.0 + 1.65e-3 * KH * ((double)ceil_div(pairs, kSaQ) * pages + 0.8 * ((double)pairs / kSaQ + a.B) * own) + 0.53e-3 * row_heads;
+    for (const bool pack : {false, true}) {
+        const double units = KH * (pack ? (double)tiles : (double)pairs / (kStWaves * kSaQ) + 0.5 * a.B) / 256;
+        const double chain = pages + 1.1 * own * (pack ? 1.0 + (double)(a.B - 1) / tiles : 1.0);
+        const int64_t n = pack ? tiles : pairs / (kStWaves * kSaQ) + a.B;
+        // (parts of 4 pages or more in 2048 workgroups or fewer: within shared_attention_bytes)
+        for (int parts = 1; parts == 1 || (parts <= 16 && 4 * parts <= pages + a.max_pages && n * a.n_kv_head * parts <= 2048); parts *= 2) {
+            const double rate = pack ? 1.1 : 1.0, u = units * parts;
+            const double t = parts == 1 ? 5.5 + 0.8 * rate * chain * std::max(1.0, u)
+                                        : 13.0 + 0.7 * rate * (chain / parts + 0.5) * std::max(1.0, 0.5 * (u + std::ceil(u))) +
+                                              0.03e-3 * parts * row_heads;
+            if (t > least || (pack && t == least)) continue;
+            least = t;
+            best = {(int)n, parts, pack};
+        }
+    }
+    return best;
 }
 
 // Whether shared_whole_kernel takes a call of one row a sequence.  Its chain is a quarter of a sequence's pages (0.32 us
@@ -1429,12 +1468,26 @@ size_t shared_attention_bytes(int n_head, int rows, int prefix_len, int max_page
 hipError_t launch_shared_attention(int dtype, const SharedAttnArgs& a, void* ws, size_t ws_bytes, hipStream_t st) {
     const bool f32 = dtype == FTTS_F32;
     if (a.row_offsets && (a.q_f32 || a.o_f32)) return hipErrorInvalidValue;  // (the decode step's forms)
-    bool pack = false;
-    const int tiles = f32 ? 0 : shared_tiles(a, &pack);
-    if (tiles > 0) {
-        const dim3 wg((unsigned)(tiles * a.n_kv_head)), wt(kStWaves * 64);
-        if (pack) hipLaunchKernelGGL(shared_tile_kernel<true>, wg, wt, 0, st, a, tiles);
-        else hipLaunchKernelGGL(shared_tile_kernel<false>, wg, wt, 0, st, a, tiles);
+    const TilePlan tp = f32 ? TilePlan{0, 1, false} : tile_plan(a);
+    const int64_t rows_heads = (int64_t)a.rows * a.n_head;
+    const dim3 jg((unsigned)((rows_heads + kJoinWaves - 1) / kJoinWaves)), jt(kJoinWaves * 64);
+    if (tp.tiles > 0) {
+        const dim3 wg((unsigned)(tp.tiles * a.n_kv_head * tp.parts)), wt(kStWaves * 64);
+        SharedPlan p{};
+        if (tp.parts > 1) {
+            p.s_pre = tp.parts;
+            if ((size_t)p.s_pre * rows_heads * (kHeadDim + 2) * 4 > ws_bytes) return hipErrorInvalidValue;
+            p.o = reinterpret_cast<float*>(ws);
+            p.ml = reinterpret_cast<float2*>(p.o + p.s_pre * rows_heads * kHeadDim);
+            if (tp.pack) hipLaunchKernelGGL((shared_tile_kernel<true, true>), wg, wt, 0, st, a, tp.tiles, p);
+            else hipLaunchKernelGGL((shared_tile_kernel<false, true>), wg, wt, 0, st, a, tp.tiles, p);
+            if (hipError_t e = hipGetLastError()) return e;
+            hipLaunchKernelGGL(shared_join_kernel<false>, jg, jt, 0, st, a, p);
+        } else if (tp.pack) {
+            hipLaunchKernelGGL((shared_tile_kernel<true, false>), wg, wt, 0, st, a, tp.tiles, p);
+        } else {
+            hipLaunchKernelGGL((shared_tile_kernel<false, false>), wg, wt, 0, st, a, tp.tiles, p);
+        }
         return hipGetLastError();
     }
     if (!f32 && shared_whole(a)) {
@@ -1448,7 +1501,6 @@ hipError_t launch_shared_attention(int dtype, const SharedAttnArgs& a, void* ws,
         return hipGetLastError();
     }
     SharedPlan p = shared_plan(f32, a.n_head, a.n_kv_head, a.B, a.rows, a.row_offsets != nullptr, a.prefix_len, a.max_pages);
-    const int64_t rows_heads = (int64_t)a.rows * a.n_head;
     if ((size_t)(p.s_pre + p.s_own) * rows_heads * (kHeadDim + 2) * 4 > ws_bytes) return hipErrorInvalidValue;
     p.o = reinterpret_cast<float*>(ws);
     p.ml = reinterpret_cast<float2*>(p.o + (p.s_pre + p.s_own) * rows_heads * kHeadDim);
@@ -1460,7 +1512,6 @@ hipError_t launch_shared_attention(int dtype, const SharedAttnArgs& a, void* ws,
     else if (a.q_f32) hipLaunchKernelGGL((shared_part_kernel<false, true>), g, t, 0, st, a, p);
     else hipLaunchKernelGGL((shared_part_kernel<false, false>), g, t, 0, st, a, p);
     if (hipError_t e = hipGetLastError()) return e;
-    const dim3 jg((unsigned)((rows_heads + kJoinWaves - 1) / kJoinWaves)), jt(kJoinWaves * 64);
     if (f32 || a.o_f32) hipLaunchKernelGGL(shared_join_kernel<true>, jg, jt, 0, st, a, p);
     else hipLaunchKernelGGL(shared_join_kernel<false>, jg, jt, 0, st, a, p);
     return hipGetLastError();

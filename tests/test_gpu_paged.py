@@ -176,7 +176,8 @@ class Batch:
 
 def kernel(b):
     """Which of the launcher's kernels a call takes: "whole" (one row a sequence, one launch), "tile" (128 rows of a
-    sequence share pages, one launch), "packed" (128 rows of all) or "cut" (along the tokens, joined); fp32 is always cut."""
+    sequence share pages, one launch), "packed" (128 rows of all), either of them " in" parts that are joined, or "cut"
+    (tiles of 32 or fewer, along the tokens, joined); fp32 is always cut."""
     if b.f32:
         return "cut"
     B, g, pages, own = len(b.lens), b.H // b.KH, -(-b.P // 64), b.width
@@ -186,10 +187,20 @@ def kernel(b):
         fits = pages + own <= 256 and whole <= 8.5 + 1.3e-3 * b.KH * (pages * -(-B * g // 32) + tiles * min(own, 16))
         return "whole" if fits else "cut"
     pairs, tiles = b.T * g, -(-b.T * g // 128)
-    tile = 5.5 + 0.8 * (pages + 1.1 * own) * max(1.0, (pairs / 128 + 0.5 * B) * b.KH / 256)
-    packed = 5.5 + 0.88 * (pages + 1.1 * own * (1 + (B - 1) / tiles)) * max(1.0, tiles * b.KH / 256)
-    cut = 9.0 + 1.65e-3 * b.KH * (-(-pairs // 32) * pages + 0.8 * (pairs / 32 + B) * own) + 0.53e-3 * b.T * b.H
-    return "cut" if min(tile, packed) > cut else "packed" if packed < tile else "tile"
+    least, name = 9.0 + 1.65e-3 * b.KH * (-(-pairs // 32) * pages + 0.8 * (pairs / 32 + B) * own) + 0.53e-3 * b.T * b.H, "cut"
+    for pack in (False, True):
+        units = b.KH * (tiles if pack else pairs / 128 + 0.5 * B) / 256
+        chain = pages + 1.1 * own * (1 + (B - 1) / tiles if pack else 1)
+        for parts in (1, 2, 4, 8, 16):
+            if parts > 1 and (4 * parts > pages + own or (tiles if pack else pairs // 128 + B) * b.KH * parts > 2048):
+                break
+            rate, u = 1.1 if pack else 1.0, units * parts
+            t = 5.5 + 0.8 * rate * chain * max(1.0, u)
+            if parts > 1:
+                t = 13 + 0.7 * rate * (chain / parts + 0.5) * max(1.0, 0.5 * (u + np.ceil(u))) + 0.03e-3 * parts * b.T * b.H
+            if t < least or (t == least and not pack):
+                least, name = t, ("packed" if pack else "tile") + (f" in {parts}" if parts > 1 else "")
+    return name
 
 
 def test_the_cases_take_every_kernel():
@@ -303,22 +314,54 @@ def test_prompts_that_share_row_tiles(H, KH, prefix, B, longest):
 
 def test_prompts_that_share_row_tiles_over_many_pages():
     """Chains whose 64th page is one of the prefix, or in the middle of the sequences' own ones."""
-    for prefix in (64 * 61 + 5, 64 * 70):
-        b = packed_batch(20, 20, prefix, 40, 60, 8).gpu()
-        assert kernel(b) == "packed"
-        print(f"packed prompts behind {prefix}", flush=True)
+    for prefix, B, takes in ((64 * 61 + 5, 64, "packed"), (64 * 70, 64, "packed"), (64 * 61 + 5, 40, "packed in 4"), (64 * 70, 40, "packed in 4")):
+        b = packed_batch(20, 20, prefix, B, 60, 8).gpu()
+        assert kernel(b) == takes
+        print(f"{takes}: prompts behind {prefix}", flush=True)
         b.call()
         torch.cuda.synchronize()
-        for seq in (0, 1, 7, 20, 39):
+        for seq in (0, 1, 7, 20, B - 1):
             ref, got = reference64(b, seq, sorted({0, b.rows[seq] // 2, b.rows[seq] - 1}))
             assert (got - ref).norm() <= 2.0 ** -8 * ref.norm(), seq
+        assert (b.out[b.cu[3]:b.cu[4]] == 0).all()
+        assert (b.out[:3] == -7).all() and (b.out[-4:] == -7).all()
 
 
-def test_values_that_are_not_finite_stay_with_their_sequence():
+@pytest.mark.parametrize("H,KH,prefix,past,rows,takes", [
+    (12, 4, 2500, [10, 0, 300], [90, 130, 90], "packed in 8"), (20, 4, 2000, [0, 64, 3, 700], [90, 0, 128, 129], "tile in 4"),
+    (20, 20, 0, [2900], [300], "tile in 4")])
+def test_prompts_whose_pages_are_cut_into_parts(H, KH, prefix, past, rows, takes):
+    """Parts that end inside the prefix and inside the own pages, an inactive sequence, a page outside the pool."""
+    b = Batch("bf16", H, KH, prefix, [p + n for p, n in zip(past, rows)], rows, extra_rows=2, packed=True, layers=1).gpu()
+    assert kernel(b) == takes
+    print(f"{takes}: {H}/{KH} heads, prefix {prefix}, rows {rows}", flush=True)
+    b.call()
+    torch.cuda.synchronize()
+    for seq in range(len(rows)):
+        if rows[seq]:
+            ref, got = reference64(b, seq, list(range(rows[seq])))
+            assert (got - ref).norm() <= 2.0 ** -8 * ref.norm() and (got - ref).abs().max() <= 2.0 ** -7 * ref.abs().max(), seq
+    assert (b.out[-2:] == -7).all()
+    again = b.out.clone()
+    b.ws.fill_(0xFF)
+    b.call()
+    assert torch.equal(b.out, again)
+    b.lens[-1] = -1
+    b.pt.seq_lens.copy_(dev(b.lens))
+    b.call()
+    torch.cuda.synchronize()
+    assert (b.out[b.cu[-2]:b.cu[-1]] == 0).all()
+    # (a shorter chain has other parts, which round otherwise: both are within 2^-8 of the exact result, as above)
+    x, y = b.out[:b.cu[-2]].float(), again[:b.cu[-2]].float()
+    assert (x - y).norm() <= 2.0 ** -7 * y.norm()
+
+
+@pytest.mark.parametrize("prefix,takes", [(333, "packed"), (64 * 61 + 5, "packed in 4")])
+def test_values_that_are_not_finite_stay_with_their_sequence(prefix, takes):
     """A sequence's own page of NaN and infinities changes no row of the others in its row tile, nor of an inactive
     sequence a prefix's."""
-    b = packed_batch(20, 20, 333, 40, 80, 5).gpu()
-    assert kernel(b) == "packed"
+    b = packed_batch(20, 20, prefix, 40, 80 if prefix < 1000 else 60, 5).gpu()
+    assert kernel(b) == takes
     b.call()
     clean = b.out.clone()
     r = slice(int(b.cu[4]), int(b.cu[5]))
@@ -373,11 +416,12 @@ def test_rows_that_see_nothing(dtype, rows):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("H,KH,B,prefix", [(4, 4, 2, 70), (8, 8, 12, 70), (6, 1, 2, 70), (4, 4, 1, 900), (6, 3, 2, 600)])
+@pytest.mark.parametrize("H,KH,B,prefix", [(4, 4, 2, 70), (8, 8, 12, 70), (6, 1, 2, 70), (4, 4, 1, 900), (6, 3, 2, 600),
+                                           (12, 4, 3, 2500)])
 def test_values_that_are_not_finite_reach_only_rows_that_see_them(dtype, H, KH, B, prefix):
     rows = [90] * B
     b = Batch(dtype, H, KH, prefix, [100] * B, rows).gpu()
-    assert kernel(b) == ("cut" if dtype == "f32" or prefix > 70 else "tile")
+    assert kernel(b) == ("cut" if dtype == "f32" or 70 < prefix < 1000 else "tile in 8" if prefix > 1000 else "tile")
     b.call()
     clean = b.out.clone()
     for tok, what in ((100 - 90 + 45, float("nan")), (99, float("inf")), (10 + 63, float("-inf")), (10 + 1, float("inf"))):
@@ -418,7 +462,8 @@ def reference64(b, seq, rows):
 
 @pytest.mark.parametrize("dtype,H,KH,prefix,lens,rows,takes", [
     ("bf16", 1, 1, 560000, [70], None, "cut"), ("f32", 1, 1, 300000, [70], None, "cut"),
-    ("bf16", 8, 8, 5000, [3000], [3000], "tile"), ("bf16", 8, 2, 9000, [40, 2500], [40, 1500], "cut"),
+    ("bf16", 8, 8, 5000, [3000], [3000], "tile in 4"), ("bf16", 8, 2, 9000, [40, 2500], [40, 1500], "tile in 4"),
+    ("bf16", 20, 20, 4500, [2500], [2500], "tile"), ("bf16", 4, 4, 9000, [40, 100], [4, 6], "cut"),
     ("bf16", 4, 4, 130, [20000, 5], None, "cut"), ("bf16", 20, 20, 0, [700, 3000], [700, 3000], "tile")])
 def test_long_contexts(dtype, H, KH, prefix, lens, rows, takes):
     """Chains of more than 64 pages (page ids come 64 at a time) and the longest prefixes, against float64 on the
