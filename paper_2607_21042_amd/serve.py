@@ -63,7 +63,8 @@ class Scheduler:
     """In-flight batching over ``max_slots`` decode slots.
 
     model      ftts.DeviceModel; shape its ModelShape.
-    n_pages    KV pages in the shared pool (64 tokens each).
+    n_pages    KV pages in the shared pool (64 tokens each); a request that needs more than the pool
+               holds besides the shared prefix is refused.
     max_ctx    longest prefix + budget a request may have (sizes the block table).
     sampling   ftts.Sampling shared by all requests.
     chunk      decode steps per chunk (ids are handed out once per chunk).
@@ -141,6 +142,10 @@ class Scheduler:
         need = req.prefix.shape[0] + req.max_new
         if req.max_new < 1 or req.prefix.shape[0] < 1 or need > self.max_pages * ftts.PAGE:
             raise ValueError("request does not fit max_ctx")
+        # pages that requests hold come back; those of the shared prefix do not
+        most = len(self.pool.free) + sum(len(p) for p in self.slot_pages)
+        if -(-need // ftts.PAGE) > most:
+            raise ValueError(f"request needs more than the pool's {most} pages")
         req.rid = self.next_rid
         self.next_rid += 1
         self.waiting.append(req)
