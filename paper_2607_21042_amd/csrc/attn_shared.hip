@@ -956,8 +956,7 @@ __device__ __forceinline__ TilePages tile_pages(const SharedAttnArgs& a, int til
     const bool in = lane < a.B;
     const int lo = in ? a.row_offsets[lane] : 0, hi = in ? a.row_offsets[lane + 1] : 0;
     TilePages t;
-    t.len = in ? a.seq_lens[lane] + a.len_add : -1;
-    if (a.active && in && !a.active[lane]) t.len = -1;
+    t.len = in ? a.seq_lens[lane] : -1;
     t.row0 = min(max(lo, 0), a.rows);
     t.n = min(max(hi, t.row0), a.rows) - t.row0;
     if constexpr (PACK) {
@@ -1161,10 +1160,11 @@ __global__ __launch_bounds__(kStWaves * 64, 3) void shared_tile_kernel(const Sha
 // sequence's own, its waves in turn, and writes the result at once: the prefix is read by every sequence (through
 // L2), but there is one launch and no partial.  Bound by its chain (ids, keys, products, values, hand-over): 4
 // sequences of up to 90 tokens behind 134, 20 heads, 5.3 us (cut: 7.2).  FEW: up to 4 query heads a key head, in tiles
-// of 4 rows (of 32: 6.4).
+// of 4 rows (of 32: 6.4); the decode step's form (Q32) has one query head a key head.
 constexpr int kSwWaves = 4;
 template <bool Q32, bool FEW>
 __global__ __launch_bounds__(kSwWaves * 64, 2) void shared_whole_kernel(const SharedAttnArgs a) {
+    static_assert(FEW || !Q32, "fp32 queries come in tiles of 4 rows");
     __shared__ __attribute__((aligned(1024))) char smem[kSwWaves * kAtStage];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hh = lane >> 5;
     const int kh = blockIdx.x % a.n_kv_head;
@@ -1209,7 +1209,7 @@ __global__ __launch_bounds__(kSwWaves * 64, 2) void shared_whole_kernel(const Sh
         }
         x *= l == 0.f ? 0.f : 1.0f / l;
         const size_t at = (size_t)row * a.o_ld + head * kHeadDim + lane;
-        if (a.o_f32) reinterpret_cast<float*>(a.o)[at] = x;
+        if (Q32 && a.o_f32) reinterpret_cast<float*>(a.o)[at] = x;
         else reinterpret_cast<uint16_t*>(a.o)[at] = (uint16_t)bf16x2_rne(x, 0.f);
         return;
     }
@@ -1223,7 +1223,7 @@ __global__ __launch_bounds__(kSwWaves * 64, 2) void shared_whole_kernel(const Sh
         }
     };
     uint4 qr[4];
-    sa_load_q<Q32>(a, t, hh, qr);
+    sa_load_q<false>(a, t, hh, qr);
     const AtAddr ad = at_addresses(lds_address(own), lane);
     SaState st;
     sa_init(st);
@@ -1296,8 +1296,7 @@ __global__ __launch_bounds__(kSwWaves * 64, 2) void shared_whole_kernel(const Sh
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
         const float y[4] = {x[4 * g] * inv, x[4 * g + 1] * inv, x[4 * g + 2] * inv, x[4 * g + 3] * inv};
-        if (a.o_f32) *reinterpret_cast<float4*>(reinterpret_cast<float*>(a.o) + at + 8 * g) = make_float4(y[0], y[1], y[2], y[3]);
-        else *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.o) + at + 8 * g) = make_uint2(bf16x2_rne(y[0], y[1]), bf16x2_rne(y[2], y[3]));
+        *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.o) + at + 8 * g) = make_uint2(bf16x2_rne(y[0], y[1]), bf16x2_rne(y[2], y[3]));
     }
 }
 
@@ -1467,7 +1466,10 @@ size_t shared_attention_bytes(int n_head, int rows, int prefix_len, int max_page
 
 hipError_t launch_shared_attention(int dtype, const SharedAttnArgs& a, void* ws, size_t ws_bytes, hipStream_t st) {
     const bool f32 = dtype == FTTS_F32;
-    if (a.row_offsets && (a.q_f32 || a.o_f32)) return hipErrorInvalidValue;  // (the decode step's forms)
+    // (the decode step's forms)
+    if (a.q_f32 || a.o_f32 || a.active || a.len_add) {
+        if (a.row_offsets || a.n_head > kFew * a.n_kv_head) return hipErrorInvalidValue;
+    }
     const TilePlan tp = f32 ? TilePlan{0, 1, false} : tile_plan(a);
     const int64_t rows_heads = (int64_t)a.rows * a.n_head;
     const dim3 jg((unsigned)((rows_heads + kJoinWaves - 1) / kJoinWaves)), jt(kJoinWaves * 64);
@@ -1494,9 +1496,8 @@ hipError_t launch_shared_attention(int dtype, const SharedAttnArgs& a, void* ws,
         const int64_t own_tiles = a.B * ceil_div(a.n_head / a.n_kv_head, kSaQ);
         const dim3 wg((unsigned)(own_tiles * a.n_kv_head)), wt(kSwWaves * 64);
         const bool few = a.n_head <= kFew * a.n_kv_head;
-        if (few && a.q_f32) hipLaunchKernelGGL((shared_whole_kernel<true, true>), wg, wt, 0, st, a);
+        if (a.q_f32) hipLaunchKernelGGL((shared_whole_kernel<true, true>), wg, wt, 0, st, a);
         else if (few) hipLaunchKernelGGL((shared_whole_kernel<false, true>), wg, wt, 0, st, a);
-        else if (a.q_f32) hipLaunchKernelGGL((shared_whole_kernel<true, false>), wg, wt, 0, st, a);
         else hipLaunchKernelGGL((shared_whole_kernel<false, false>), wg, wt, 0, st, a);
         return hipGetLastError();
     }
