@@ -500,7 +500,8 @@ int ftts_prefill_shared(const ftts_weights* w, const ftts_shared_prefix* prefix,
                         const ftts_kv_pool* kv, float* last_logits, void* ws, size_t ws_bytes, void* stream);
 
 /* ftts_decode_step_hidden (hidden_out may be NULL) for sequences that continue `prefix`; an own
- * length of 0 is a sequence's first token right behind it.  One kernel per phase: FTTS_E_UNSUPPORTED
+ * length of 0 is a sequence's first token right behind it.  The step's queries reach the scores as
+ * without a prefix: fp32, or over a bf16 pool two bf16 parts of each (16 bits).  One kernel per phase: FTTS_E_UNSUPPORTED
  * where the persistent step is forced. */
 int ftts_decode_step_shared(const ftts_weights* w, const ftts_shared_prefix* prefix, const int32_t* tokens,
                             const int32_t* positions, const ftts_page_table* pt, const ftts_kv_pool* kv,

@@ -305,20 +305,20 @@ __device__ __forceinline__ void sa_add_not_finite(SaState& a, const char* vt, co
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 }
 
-// The rows' queries as at_load_q gives them; Q32: fp32 ones, rounded to bf16 as the prefill's are.
-template <bool Q32>
-__device__ __forceinline__ void sa_load_q(const SharedAttnArgs& a, const RowTile& t, int hh, uint4 (&qr)[4]) {
-    const size_t q0 = (size_t)max(t.row, 0) * a.q_ld + t.head * kHeadDim;
-    if constexpr (Q32) {
-        const float* qp = reinterpret_cast<const float*>(a.q) + q0 + hh * 8;
+// Four fp32 queries as bf16, and what their rounding left, in bf16 too: scores then see 16 bits of each, as in the
+// decode step without a prefix (8 bits alone let two scores of 100 move against each other by 0.04 and more).
+__device__ __forceinline__ uint2 sa_round_q(const float4& x, uint2& left) {
+    const uint2 r = make_uint2(bf16x2_rne(x.x, x.y), bf16x2_rne(x.z, x.w));
+    left = make_uint2(bf16x2_rne(x.x - bf16lo(r.x), x.y - bf16hi(r.x)), bf16x2_rne(x.z - bf16lo(r.y), x.w - bf16hi(r.y)));
+    return r;
+}
+// Adds the scores of the queries' second part.
+__device__ __forceinline__ void sa_scores_left(const uint4 (&ka)[4], const uint4 (&kb)[4], const uint4 (&ql)[4], at_f32x16 (&s)[2]) {
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-            const float4 x = *reinterpret_cast<const float4*>(qp + kk * 16), y = *reinterpret_cast<const float4*>(qp + kk * 16 + 4);
-            qr[kk] = make_uint4(bf16x2_rne(x.x, x.y), bf16x2_rne(x.z, x.w), bf16x2_rne(y.x, y.y), bf16x2_rne(y.z, y.w));
-        }
-    } else {
-        at_load_q(reinterpret_cast<const uint16_t*>(a.q) + q0, hh, qr);
-    }
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)
+            s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at_op(b ? kb[kk] : ka[kk]), at_op(ql[kk]), s[b], 0, 0, 0);
 }
 
 // A page id asked for before it is known whether the page is seen (a plain load could be moved behind that): the ids
@@ -473,6 +473,32 @@ __device__ __forceinline__ void few_finish(const SharedPlan& pl, const PartWork&
 // heads a key head, were slower than one tile of 32: 14.4 us for 24 sequences of 20/4 heads (13.6).
 typedef short few_s16x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ few_s16x4 few_op(uint32_t x, uint32_t y) { return __builtin_bit_cast(few_s16x4, make_uint2(x, y)); }
+// fp32 queries: lane (block, row) rounds its 4 dims of the row, and through LDS (at s0, where the first page's values
+// land afterwards) every lane gets both parts of its row: a sixteenth of the rounding, and one load a lane.  A step of 24
+// layers behind 1500 tokens, 32, 8 and 1 sequences: 1383, 1118 and 845 us; where every lane rounds its row 1399, 1134 and
+// 867; 8-bit queries 1390, 1121 and 842.
+__device__ __forceinline__ void few_exchange_q(const float4& x, uint32_t s0, int lane, uint4 (&q)[8], uint4 (&ql)[8]) {
+    uint2 left;
+    const uint2 r = sa_round_q(x, left);
+    const uint32_t row = s0 + (lane & 3) * 272, to = row + (lane >> 2) * 8;  // (256 bytes a row, and 16 so that rows lie in other banks)
+    at_bf16x8 o[16];
+    asm volatile(
+        "ds_write_b64 %16, %18\n\tds_write_b64 %16, %19 offset:128\n\ts_waitcnt lgkmcnt(0)\n\t"
+        "ds_read_b128 %0, %17\n\tds_read_b128 %1, %17 offset:16\n\tds_read_b128 %2, %17 offset:32\n\tds_read_b128 %3, %17 offset:48\n\t"
+        "ds_read_b128 %4, %17 offset:64\n\tds_read_b128 %5, %17 offset:80\n\tds_read_b128 %6, %17 offset:96\n\tds_read_b128 %7, %17 offset:112\n\t"
+        "ds_read_b128 %8, %17 offset:128\n\tds_read_b128 %9, %17 offset:144\n\tds_read_b128 %10, %17 offset:160\n\tds_read_b128 %11, %17 offset:176\n\t"
+        "ds_read_b128 %12, %17 offset:192\n\tds_read_b128 %13, %17 offset:208\n\tds_read_b128 %14, %17 offset:224\n\tds_read_b128 %15, %17 offset:240\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(o[0]), "=&v"(o[1]), "=&v"(o[2]), "=&v"(o[3]), "=&v"(o[4]), "=&v"(o[5]), "=&v"(o[6]), "=&v"(o[7]),
+          "=&v"(o[8]), "=&v"(o[9]), "=&v"(o[10]), "=&v"(o[11]), "=&v"(o[12]), "=&v"(o[13]), "=&v"(o[14]), "=&v"(o[15])
+        : "v"(to), "v"(row), "v"(__builtin_bit_cast(few_s16x4, r)), "v"(__builtin_bit_cast(few_s16x4, left))
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        q[i] = __builtin_bit_cast(uint4, o[i]);
+        ql[i] = __builtin_bit_cast(uint4, o[8 + i]);
+    }
+}
 // A page's keys, lane by key (kr: its 16-byte pieces).
 __device__ __forceinline__ void few_read_k(const uint32_t (&kr)[8], uint4 (&k)[8]) {
     at_bf16x8 x[8];
@@ -518,17 +544,14 @@ __device__ __forceinline__ void few_pages(const SharedAttnArgs& a, const RowTile
         }
         return tokens;
     };
-    uint4 q[8];
+    uint4 q[8], ql[Q32 ? 8 : 1];
     const size_t q0 = (size_t)max(t.row, 0) * a.q_ld + t.head * kHeadDim;
+    float4 q32;  // Q32: lane (block, row) takes dims 4 block .. + 3 of the row
+    if constexpr (Q32) {
+        q32 = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(a.q) + q0 + (lane & ~3));
+    } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if constexpr (Q32) {
-            const float* qp = reinterpret_cast<const float*>(a.q) + q0 + 8 * i;
-            const float4 x = *reinterpret_cast<const float4*>(qp), y = *reinterpret_cast<const float4*>(qp + 4);
-            q[i] = make_uint4(bf16x2_rne(x.x, x.y), bf16x2_rne(x.z, x.w), bf16x2_rne(y.x, y.y), bf16x2_rne(y.z, y.w));
-        } else {
-            q[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(a.q) + q0 + 8 * i);
-        }
+        for (int i = 0; i < 8; ++i) q[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(a.q) + q0 + 8 * i);
     }
     uint32_t kr[8], vr[4];
     {
@@ -547,6 +570,10 @@ __device__ __forceinline__ void few_pages(const SharedAttnArgs& a, const RowTile
         page = fetch(0);
         next = load(0, 0);
         __builtin_amdgcn_sched_barrier(0);
+        if constexpr (Q32) {
+            few_exchange_q(q32, lds_address(own + kAtTile), lane, q, ql);
+            __builtin_amdgcn_sched_barrier(0);
+        }
         load(0, 1);
     }
     for (int j = 0; j < n; ++j) {
@@ -562,11 +589,19 @@ __device__ __forceinline__ void few_pages(const SharedAttnArgs& a, const RowTile
             next = load(j + 1, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
-        few_f32x4 s[2] = {};
+        few_f32x4 s[2] = {}, sl[2] = {};
 #pragma unroll
         for (int c = 0; c < 8; ++c) {
             s[0] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(few_op(k[c].x, k[c].y), few_op(q[c].x, q[c].y), s[0], 0, 0, 0);
             s[1] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(few_op(k[c].z, k[c].w), few_op(q[c].z, q[c].w), s[1], 0, 0, 0);
+            if constexpr (Q32) {
+                sl[0] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(few_op(k[c].x, k[c].y), few_op(ql[c].x, ql[c].y), sl[0], 0, 0, 0);
+                sl[1] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(few_op(k[c].z, k[c].w), few_op(ql[c].z, ql[c].w), sl[1], 0, 0, 0);
+            }
+        }
+        if constexpr (Q32) {
+            s[0] += sl[0];
+            s[1] += sl[1];
         }
         float p[4];
 #pragma unroll
@@ -635,8 +670,20 @@ __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_kernel(const Sha
         }
         return tokens > 0;
     };
-    uint4 qr[4];
-    sa_load_q<Q32>(a, t, hh, qr);
+    uint4 qr[4], ql[Q32 ? 4 : 1];
+    const size_t q0 = (size_t)max(t.row, 0) * a.q_ld + t.head * kHeadDim;
+    if constexpr (Q32) {
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+            const float4* qp = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(a.q) + q0 + hh * 8 + kk * 16);
+            uint2 l0, l1;
+            const uint2 r0 = sa_round_q(qp[0], l0), r1 = sa_round_q(qp[1], l1);
+            qr[kk] = make_uint4(r0.x, r0.y, r1.x, r1.y);
+            ql[kk] = make_uint4(l0.x, l0.y, l1.x, l1.y);
+        }
+    } else {
+        at_load_q(reinterpret_cast<const uint16_t*>(a.q) + q0, hh, qr);
+    }
     const AtAddr ad = at_addresses(lds_address(own), lane);
     SaState st;
     sa_init(st);
@@ -662,6 +709,7 @@ __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_kernel(const Sha
         __builtin_amdgcn_sched_barrier(0);
         at_f32x16 s[2];
         at_scores(ka, kb, qr, s);
+        if constexpr (Q32) sa_scores_left(ka, kb, ql, s);
         uint32_t pw[16], plo[16];
         const int lim = seen ? t.lim : 0;
         if (__any(lim < k0 + kAtK)) sa_mask(s, k0, lim, hh);
@@ -1223,7 +1271,7 @@ __global__ __launch_bounds__(kSwWaves * 64, 2) void shared_whole_kernel(const Sh
         }
     };
     uint4 qr[4];
-    sa_load_q<false>(a, t, hh, qr);
+    at_load_q(reinterpret_cast<const uint16_t*>(a.q) + (size_t)max(t.row, 0) * a.q_ld + t.head * kHeadDim, hh, qr);
     const AtAddr ad = at_addresses(lds_address(own), lane);
     SaState st;
     sa_init(st);

@@ -1,0 +1,113 @@
+"""Serving behind a shared prefix where it can go wrong: near-ties between large scores, values and
+scores that are not finite, pages outside the pool, tables far wider than their sequences."""
+import numpy as np
+import pytest
+
+from paper_2607_21042_amd import ftts, workload
+from tests import helpers
+from tests.test_gpu_paged import Batch, dev, kernel, reference64  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+
+# ---- the decode step's queries ----------------------------------------------------------------
+ONE = workload.ModelShape(n_layer=1, d_model=256, n_head=4, d_head=64, d_ff=512, vocab=640)
+
+
+def wide_model():
+    """One layer whose queries are about 6 wide, whose out-projection is the identity and whose MLP adds
+    nothing, on rows of 0.01: the hidden state is LayerNorm(the attention's output), near enough."""
+    m, d = workload.master_weights(ONE, seed=11), ONE.d_model
+    m["tok_emb"], m["pos_emb"] = m["tok_emb"] * 0.5, m["pos_emb"] * 0.5
+    m["lnf_g"], m["lnf_b"] = np.ones_like(m["lnf_g"]), np.zeros_like(m["lnf_b"])
+    w = m["layers"][0]
+    w["w_qkv"] = w["w_qkv"].copy()
+    w["w_qkv"][:d] *= 6.0 / (0.02 * np.sqrt(d))
+    w["w_out"], w["b_out"] = np.eye(d, dtype=np.float32), np.zeros_like(w["b_out"])
+    w["w_fc2"], w["b_fc2"] = np.zeros_like(w["w_fc2"]), np.zeros_like(w["b_fc2"])
+    return workload.bf16_weights(m)
+
+
+def queries(m, tokens, pos):
+    x = m["tok_emb"][tokens].astype(np.float64) + m["pos_emb"][pos]
+    w = m["layers"][0]
+    n = (x - x.mean(1, keepdims=True)) / np.sqrt(x.var(1, keepdims=True) + 1e-5) * w["ln1_g"] + w["ln1_b"]
+    return (n @ w["w_qkv"][:256].astype(np.float64).T + w["b_qkv"][:256]).reshape(len(tokens), 4, 64)
+
+
+@pytest.mark.parametrize("B,P,own", [(1, 64, 3), (2, 192, 70), (3, 1984, 130), (8, 1280, 200), (24, 640, 66), (33, 320, 40)])
+def test_decode_queries_keep_their_bits_behind_a_shared_prefix(B, P, own):
+    """A decode step's fp32 query reaches the scores with 16 bits, as in the step without a prefix.  Each
+    sequence and head has a token of its own whose score ties with the prefix's largest, among scores of
+    some 100: a query of 8 bits moves such a pair against each other by 0.04 and more.
+
+    The same pages serve as a shared prefix and as the first pages of every block table, so queries, keys
+    and values of both calls are the same bits.  Bound: with S the largest sum_d |q_d k_d| / 8, the
+    two-part query (2^-18 of itself) and the sum of 64 products in fp32 (64 u = 2^-18) shift a score by at
+    most 2^-17 S; with scaling and exponential eps = 3 * 2^-18 S.  An output o moves by sum_j p_j ds_j
+    (v_j - o), at most eps sum p |v - o| a side, sixteen-bit outputs by 2^-8 of themselves a side more, and
+    LayerNorm, a projection and a scale, keeps errors relative to |o - mean| (5% for the rows it adds)."""
+    m = wide_model()
+    rng = np.random.default_rng(B)
+    tokens, pos = rng.integers(0, ONE.vocab, B), np.full(B, 2)
+    n_pre, n_own = P // 64, -(-(own + 1) // 64)
+    n_pages = n_pre + B * n_own
+    ids = rng.permutation(n_pages)
+    pre, table = ids[:n_pre], ids[n_pre:].reshape(B, n_own)
+    pool = np.zeros((1, n_pages, 2, 4, 64, 64), dtype=np.float32)
+    pool[:, :, 0] = workload.bf16_round(rng.standard_normal((1, n_pages, 4, 64, 64)).astype(np.float32) * np.float32(6))
+    pool[:, table, 0] = workload.bf16_round(pool[:, table, 0] * np.float32(0.5))   # (the prefix's largest stays the largest)
+    pool[:, :, 1] = workload.bf16_round(rng.standard_normal((1, n_pages, 4, 64, 64)).astype(np.float32))
+    q = queries(m, tokens, pos)
+    move, out, S, near = np.zeros((B, 4, 64)), np.zeros((B, 4, 64)), 0.0, 0
+    for b in range(B):
+        for h in range(4):
+            best = (pool[0, pre, 0, h].reshape(-1, 64) @ q[b, h]).max()
+            t = int(rng.integers(0, own))
+            k = rng.standard_normal(64) * 6
+            k += (best - k @ q[b, h]) / (q[b, h] @ q[b, h]) * q[b, h]
+            pool[0, table[b, t // 64], 0, h, t % 64] = workload.bf16_round(k.astype(np.float32))
+            pg = np.concatenate([pre, table[b]])
+            key, val = (pool[0, pg, j, h].reshape(-1, 64)[:P + own].astype(np.float64) for j in (0, 1))
+            s = key @ q[b, h] / 8
+            p = np.exp(s - s.max())
+            p /= p.sum()
+            near += np.sort(p)[-2] > 0.05
+            out[b, h] = p @ val
+            move[b, h] = p @ np.abs(val - out[b, h])
+            S = max(S, (np.abs(key) @ np.abs(q[b, h])).max() / 8)
+    assert near >= 2 * B
+    dm = ftts.DeviceModel(m, ONE, ftts.BF16)
+    cache = torch.from_numpy(pool).cuda().bfloat16()
+
+    class View(ftts.KVCache):
+        def __init__(self, pool):
+            self.pool = pool
+            self._view()
+
+    hid = []
+    for shared in (True, False):
+        kv = View(cache.clone())
+        bt = table if shared else np.concatenate([np.tile(pre, (B, 1)), table], 1)
+        pt = ftts.PageTableView(dev(bt), dev(np.full(B, own + (0 if shared else P))))
+        ws = torch.zeros(ftts.shared_workspace_bytes(dm.cfg, B, B, P, bt.shape[1]), dtype=torch.uint8, device="cuda")
+        logits, ids_out = torch.empty((B, ONE.vocab), device="cuda"), dev(np.zeros(B))
+        h = torch.empty((B, 256), device="cuda")
+        kw = dict(hidden_out=h)
+        greedy = ftts.Sampling(1.0, 1, 1.0)
+        print(f"decode queries: B {B}, prefix {P}, {'shared' if shared else 'copied'}", flush=True)
+        if shared:
+            ftts.decode_step_shared(dm, ftts.SharedPrefix(dev(pre), P), dev(tokens), dev(pos), pt, kv, logits, ids_out, None,
+                                    greedy, ws, **kw)
+        else:
+            ftts.decode_step(dm, dev(tokens), dev(pos), pt, kv, logits, ids_out, None, greedy, ws, **kw)
+        torch.cuda.synchronize()
+        hid.append((h.cpu().numpy().astype(np.float64), kv.pool))
+    assert torch.equal(hid[0][1], hid[1][1])
+    move, out = move.reshape(B, 256), out.reshape(B, 256)
+    ratio = np.linalg.norm(move, axis=1) / np.linalg.norm(out - out.mean(1, keepdims=True), axis=1)
+    bound = 1.05 * (2 * 3 * 2.0 ** -18 * S * ratio + 2 * 2.0 ** -8 * (B >= 5))  # (from 5 rows on the step's outputs are bf16)
+    err = np.linalg.norm(hid[0][0] - hid[1][0], axis=1) / np.linalg.norm(hid[1][0], axis=1)
+    print(f"error {err.max():.2e}, bound {bound.min():.2e}, S {S:.0f}", flush=True)
+    assert (err <= bound).all(), (err / bound).max()
