@@ -201,7 +201,15 @@ __device__ __forceinline__ void sa_maximum(SaState& a, const at_f32x16 (&s)[N]) 
         }
     }
 }
-// The weights as bf16 pairs, their sum over this lane's half of the keys and (LO) what their rounding left, in bf16 too.
+// Weights x, y >= 0 in two bf16 parts each, the larger one below the weight, so that what is left is above 0 where the
+// weight is: with both times an infinite value the product stays infinite (a part of 0, or below it, would make NaN of
+// it).  Within 2^-16 of the weight: the larger part leaves less than 2^-7 of it, rounded by 2^-9 of that.
+__device__ __forceinline__ uint32_t sa_split(float x, float y, uint32_t& left) {
+    const uint32_t a = __builtin_elementwise_sub_sat(__float_as_uint(x), 1u), b = __builtin_elementwise_sub_sat(__float_as_uint(y), 1u);
+    left = bf16x2_rne(x - __uint_as_float(a & 0xFFFF0000u), y - __uint_as_float(b & 0xFFFF0000u));
+    return __builtin_amdgcn_perm(b, a, 0x07060302u);
+}
+// The weights as bf16 pairs, their sum over this lane's half of the keys and (LO) their second parts.
 template <bool LO>
 __device__ __forceinline__ float sa_weights(const SaState& a, const at_f32x16 (&s)[2], uint32_t (&pw)[16], uint32_t (&pl)[LO ? 16 : 1]) {
     const float ref = a.m == -INFINITY ? 0.f : a.m;  // nothing seen: every score is -inf and every weight 0
@@ -212,12 +220,12 @@ __device__ __forceinline__ float sa_weights(const SaState& a, const at_f32x16 (&
         for (int i = 0; i < 16; i += 2) {
             const float x = __builtin_amdgcn_exp2f(fmaf(s[b][i], kSaScale, -ref));
             const float y = __builtin_amdgcn_exp2f(fmaf(s[b][i + 1], kSaScale, -ref));
-            const uint32_t w = bf16x2_rne(x, y);
-            pw[b * 8 + i / 2] = w;
             if constexpr (LO) {
                 l += x + y;
-                pl[b * 8 + i / 2] = bf16x2_rne(x - bf16lo(w), y - bf16hi(w));
+                pw[b * 8 + i / 2] = sa_split(x, y, pl[b * 8 + i / 2]);
             } else {
+                const uint32_t w = bf16x2_rne(x, y);
+                pw[b * 8 + i / 2] = w;
                 l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(sa_bf16x2, w), __builtin_bit_cast(sa_bf16x2, 0x3F803F80u), l, false);
             }
         }
@@ -524,7 +532,7 @@ __device__ __forceinline__ void few_read_v(const uint32_t (&vr)[4], uint64_t (&v
         : "memory");
 #undef SA_TR
 }
-template <int... B>  // the blocks of 4 keys; pl: what the weights' rounding left
+template <int... B>  // the blocks of 4 keys; pl: the weights' second parts
 __device__ __forceinline__ void few_pv(FewState& a, few_s16x4 p, few_s16x4 pl, const uint64_t (&v)[16], std::integer_sequence<int, B...>) {
     ((a.o[0] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(p, __builtin_bit_cast(few_s16x4, v[B]), a.o[0], 4, B, 0),
       a.o[1] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(pl, __builtin_bit_cast(few_s16x4, v[B]), a.o[1], 4, B, 0)), ...);
@@ -607,8 +615,8 @@ __device__ __forceinline__ void few_pages(const SharedAttnArgs& a, const RowTile
 #pragma unroll
         for (int i = 0; i < 4; ++i) p[i] = (lane & ~3) + i < tokens ? s[0][i] + s[1][i] : -INFINITY;
         few_weights(st, p);
-        const uint32_t h0 = bf16x2_rne(p[0], p[1]), h1 = bf16x2_rne(p[2], p[3]);
-        const uint32_t l0 = bf16x2_rne(p[0] - bf16lo(h0), p[1] - bf16hi(h0)), l1 = bf16x2_rne(p[2] - bf16lo(h1), p[3] - bf16hi(h1));
+        uint32_t l0, l1;
+        const uint32_t h0 = sa_split(p[0], p[1], l0), h1 = sa_split(p[2], p[3], l1);
         __builtin_amdgcn_sched_barrier(0);
         if (more) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");  // V is in, the next K may be out
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -635,7 +643,7 @@ __device__ __forceinline__ void few_part(const SharedAttnArgs& a, const SharedPl
 
 // bf16: the waves take a run's pages in turn (wave w: w, w + 2, ...) by direct-to-LDS loads into a stage of their own,
 // the next page's K (V) on its way once this one's is in registers; no barrier in the loop.  The weights go into the
-// products as bf16 and what their rounding left, so that only the output is rounded (the second product is free where
+// products in two bf16 parts (sa_split), so that only the output is rounded (the second product is free where
 // reading bounds).  PROMPT: several rows a sequence, so a tile's rows may see different tokens.
 //
 // Two waves a workgroup: one wave each measured 1-2 us better for 32 short sequences and 2 worse behind long prefixes,

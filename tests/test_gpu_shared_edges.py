@@ -111,3 +111,54 @@ def test_decode_queries_keep_their_bits_behind_a_shared_prefix(B, P, own):
     err = np.linalg.norm(hid[0][0] - hid[1][0], axis=1) / np.linalg.norm(hid[1][0], axis=1)
     print(f"error {err.max():.2e}, bound {bound.min():.2e}, S {S:.0f}", flush=True)
     assert (err <= bound).all(), (err / bound).max()
+
+
+# ---- values and scores that are not finite ------------------------------------------------------
+FORMS = [  # dtype, heads, prefix, own tokens before the rows, rows (None: one a sequence), the kernel
+    ("bf16", 4, 4, 60, [3, 40, 200], None, "whole"), ("bf16", 5, 1, 60, [3, 40], None, "whole"),
+    ("bf16", 4, 4, 4000, [70, 5], None, "cut"), ("bf16", 4, 4, 2500, [70, 5, 300, 1, 64, 90], None, "cut"),
+    ("bf16", 10, 1, 3000, [70, 5], None, "cut"), ("f32", 4, 4, 70, [70, 5], None, "cut"),
+    ("f32", 4, 4, 4000, [70, 5, 300, 1, 64, 90], None, "cut"), ("f32", 9, 1, 400, [70, 5], None, "cut"),
+    ("bf16", 4, 4, 700, [20, 0], [40, 30], "cut"), ("f32", 4, 4, 700, [20, 0], [40, 30], "cut"),
+    ("bf16", 8, 8, 70, [10] * 12, [90] * 12, "tile"), ("bf16", 20, 20, 333, [0] * 40, [40] * 40, "packed"),
+    ("bf16", 12, 4, 2500, [10, 0, 300], [90, 130, 90], "packed in 8"), ("bf16", 20, 4, 2000, [0, 64, 700], [90, 128, 129], "tile in 4")]
+
+
+def form(dtype, H, KH, prefix, past, rows, takes, **kw):
+    lens = past if rows is None else [p + n for p, n in zip(past, rows)]
+    b = Batch(dtype, H, KH, prefix, lens, rows, layers=1, **kw).gpu()
+    assert kernel(b) == takes
+    print(f"{takes}: {dtype} {H}/{KH} heads, prefix {prefix}, {len(lens)} sequences", flush=True)
+    return b
+
+
+def place(b, seq, tok):
+    """(page, slot) of token `tok` of sequence seq, or of the prefix (seq None)."""
+    return (b.pre if seq is None else b.table[seq])[tok // 64], tok % 64
+
+
+def seen(b, seq, tok):
+    """Rows that see the token: a slice of rows of the batch for a sequence's own, all for the prefix's."""
+    if seq is None:
+        return slice(0, b.T)
+    if b.rows is None:
+        return slice(seq, seq + 1)
+    return slice(int(b.cu[seq]) + max(tok - (b.lens[seq] - b.rows[seq]), 0), int(b.cu[seq + 1]))
+
+
+@pytest.mark.parametrize("dtype,H,KH,prefix,past,rows,takes", FORMS)
+def test_an_infinite_value_is_infinite_where_it_is_seen(dtype, H, KH, prefix, past, rows, takes):
+    """p * inf = inf for a weight above 0, in its dim alone: one in the prefix, one of a sequence's own tokens."""
+    b = form(dtype, H, KH, prefix, past, rows, takes)
+    b.call()
+    torch.cuda.synchronize()
+    want = b.out.view(b.T, H, 64).clone()
+    own = 1 if rows is None else past[0] + rows[0] // 2
+    for seq, tok, dim, what in ((None, min(prefix - 1, 37), 5, float("inf")), (None, prefix - 1, 40, float("-inf")),
+                                (0, own, 63, float("-inf")), (0, own, 17, float("inf"))):
+        pg, slot = place(b, seq, tok)
+        b.kv.pool[0, pg, 1, :, slot, dim] = what
+        want[seen(b, seq, tok), :, dim] = what
+    b.call()
+    torch.cuda.synchronize()
+    assert torch.equal(b.out.view(b.T, H, 64), want)
