@@ -281,8 +281,9 @@ __device__ __forceinline__ void sa_take_out(uint64_t (&v)[2][2][4]) {
                 v[d][e][st] = (uint64_t)x[1] << 32 | x[0];
             }
 }
-// ... and are added here where the weight is not 0.  vt: the tile in LDS.
-__device__ __forceinline__ void sa_add_not_finite(SaState& a, const char* vt, const uint32_t (&pw)[16], int hh) {
+// ... and are added here to the rows that see the token, at a weight of 0 too.  vt: the tile in LDS; seen: its tokens that
+// this lane's row sees.
+__device__ __forceinline__ void sa_add_not_finite(SaState& a, const char* vt, const uint32_t (&pw)[16], int seen, int hh) {
     uint32_t p[16];
 #pragma unroll
     for (int j = 0; j < 16; ++j) p[j] = pw[j];
@@ -301,7 +302,7 @@ __device__ __forceinline__ void sa_add_not_finite(SaState& a, const char* vt, co
                 const float f[4] = {bf16lo(v.x), bf16hi(v.x), bf16lo(v.y), bf16hi(v.y)};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float y = pk != 0.f && !(fabsf(f[i]) < INFINITY) ? pk * f[i] : 0.f;
+                    const float y = key < seen && !(fabsf(f[i]) < INFINITY) ? pk * f[i] : 0.f;
                     if (c < 4) a.o0[4 * (c & 3) + i] += y;
                     else a.o1[4 * (c & 3) + i] += y;
                 }
@@ -732,7 +733,7 @@ __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_kernel(const Sha
         __builtin_amdgcn_sched_barrier(0);
         // (rows without a token in the tile have weights of 0, those past a tile's end zeros for values)
         if (PROMPT && __any(t.lim < min(t.most, k0 + kAtK)) && sa_not_finite(v, s)) {
-            sa_add_not_finite(st, own + kAtTile, pw, hh);
+            sa_add_not_finite(st, own + kAtTile, pw, lim - k0, hh);
             sa_read_v<0>(ad, v);
             sa_take_out(v);
         }
@@ -777,7 +778,7 @@ __device__ __forceinline__ void sf_read_v(const uint32_t (&a)[8], int flip, floa
 #undef SF_R
 }
 // As sa_add_not_finite.
-__device__ __forceinline__ void sf_add_not_finite(SaState& a, const char* vt, const at_f32x16& pw, int hh) {
+__device__ __forceinline__ void sf_add_not_finite(SaState& a, const char* vt, const at_f32x16& pw, int seen, int hh) {
     at_f32x16 p = pw;
 #pragma unroll 1
     for (int j = 0; j < 16; ++j) {
@@ -792,7 +793,7 @@ __device__ __forceinline__ void sf_add_not_finite(SaState& a, const char* vt, co
                 const float f[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float y = pk != 0.f && !(fabsf(f[i]) < INFINITY) ? pk * f[i] : 0.f;
+                    const float y = key < seen && !(fabsf(f[i]) < INFINITY) ? pk * f[i] : 0.f;
                     if (c < 4) a.o0[4 * (c & 3) + i] += y;
                     else a.o1[4 * (c & 3) + i] += y;
                 }
@@ -977,7 +978,7 @@ __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_f32_kernel(const
 #pragma unroll
             for (int i = 0; i < 16; ++i) z = fmaf(v0[i], 0.f, fmaf(v1[i], 0.f, z));
             if (__any(z != 0.f)) {  // (NaN: a value that is not finite, in a tile that some row sees in part)
-                sf_add_not_finite(st, own + kAtTile, s[0], hh);
+                sf_add_not_finite(st, own + kAtTile, s[0], lim - k0, hh);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     v0[i] = fabsf(v0[i]) < INFINITY ? v0[i] : 0.f;
@@ -1175,7 +1176,7 @@ __global__ __launch_bounds__(kStWaves * 64, 3) void shared_tile_kernel(const Sha
         sa_maximum(st, s);
         st.l += sa_weights<false>(st, s, pw, none);
         if (mask && __any(lim < k0 + tokens) && sa_not_finite(v, s)) {
-            sa_add_not_finite(st, smem + SO + kAtTile, pw, hh);
+            sa_add_not_finite(st, smem + SO + kAtTile, pw, lim - k0, hh);
             sa_read_v<SO>(ad, v);
             sa_take_out(v);
         }

@@ -162,3 +162,21 @@ def test_an_infinite_value_is_infinite_where_it_is_seen(dtype, H, KH, prefix, pa
     b.call()
     torch.cuda.synchronize()
     assert torch.equal(b.out.view(b.T, H, 64), want)
+
+
+@pytest.mark.parametrize("dtype,H,KH,prefix,past,rows,takes", [f for f in FORMS if f[5]])
+def test_a_value_that_is_not_finite_counts_at_a_weight_of_zero(dtype, H, KH, prefix, past, rows, takes):
+    """0 * NaN = NaN, in a tile that some rows see in part as in the others; rows before the token keep their bits."""
+    b = form(dtype, H, KH, prefix, past, rows, takes)
+    b.qd.abs_().add_(0.25)
+    pg, slot = place(b, 0, past[0] + rows[0] // 2)
+    b.kv.pool[0, pg, 0, :, slot] = -300.0        # a score below -600: its weight is below 2^-800
+    b.call()
+    torch.cuda.synchronize()
+    want = b.out.clone()
+    assert torch.isfinite(want.float()).all()
+    b.kv.pool[0, pg, 1, :, slot] = float("nan")
+    want[seen(b, 0, past[0] + rows[0] // 2)] = float("nan")
+    b.call()
+    torch.cuda.synchronize()
+    assert torch.equal(b.out.float().nan_to_num(123.0), want.float().nan_to_num(123.0))
