@@ -465,8 +465,8 @@ size_t ftts_shared_attention_workspace_bytes(const ftts_attn_shape* shape, int32
  *   prefix       the shared prefix, or NULL for none.
  *   pt           block table and own lengths; a length past max_pages * 64 ends there, a
  *                negative one makes its sequence inactive: its rows become 0.
- * A row that sees no token becomes 0, and tokens in pages outside the pool are not seen; slots
- * of a page past a sequence's end may hold anything.  A value that is not finite reaches only
+ * A row that sees no token becomes 0 (one that sees tokens, all with a score of -inf, NaN), and
+ * tokens in pages outside the pool are not seen; slots of a page past a sequence's end may hold anything.  A value that is not finite reaches only
  * rows that see its token.  In bf16 the scores and the sums are fp32 and the output is rounded
  * once; the weights multiply the values in 16-bit products.
  * 1 <= B <= FTTS_MAX_BATCH, n_rows <= 2^24, n_rows * n_head < 2^31.  `ws` holds intermediate results of the call only;

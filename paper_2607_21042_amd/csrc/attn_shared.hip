@@ -163,6 +163,12 @@ struct SaState {
     float m, l;
 };
 
+// A maximum of kSaLowest marks a row that has seen tokens, all with a score of -inf: it has no softmax unless others join.
+constexpr float kSaLowest = -3.402823466e38f;
+__device__ __forceinline__ float sa_marked(float m, bool saw) { return saw && m == -INFINITY ? kSaLowest : m; }
+// 1 / l: where nothing has been seen 0, where every score was -inf NaN.
+__device__ __forceinline__ float sa_inverse(float l, float m) { return l != 0.f ? 1.0f / l : m == kSaLowest ? NAN : 0.f; }
+
 __device__ __forceinline__ void sa_init(SaState& a) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) a.o0[i] = a.o1[i] = 0.f;
@@ -423,6 +429,7 @@ typedef float few_f32x4 __attribute__((ext_vector_type(4)));
 struct FewState {
     float m = -INFINITY, l = 0.f;
     few_f32x4 o[2] = {};  // (two chains of products)
+    bool saw = false;     // a token
 };
 // The scores p of a page (-inf: not seen) to weights.
 __device__ __forceinline__ void few_weights(FewState& a, float (&p)[4]) {
@@ -454,6 +461,7 @@ __device__ __forceinline__ void few_weights(FewState& a, float (&p)[4]) {
 __device__ __forceinline__ void few_finish(const SharedPlan& pl, const PartWork& w, FewState& st, char* smem, int wave, int lane) {
     static_assert(kSaWaves == 2, "one wave hands over to the other");
     st.o[0] += st.o[1];
+    st.m = sa_marked(st.m, st.saw);
 #pragma unroll
     for (int d = 4; d < kWave; d <<= 1) st.l += __shfl_xor(st.l, d, kWave);
     __syncthreads();
@@ -577,6 +585,7 @@ __device__ __forceinline__ void few_pages(const SharedAttnArgs& a, const RowTile
     int next = 0;
     if (n > 0) {
         page = fetch(0);
+        st.saw = __any(page.tokens > 0);
         next = load(0, 0);
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (Q32) {
@@ -594,7 +603,10 @@ __device__ __forceinline__ void few_pages(const SharedAttnArgs& a, const RowTile
         few_read_k(kr, k);
         __builtin_amdgcn_sched_barrier(0);
         if (more) {
-            if (((j + 1) & 63) == 0) page = fetch(j + 1);
+            if (((j + 1) & 63) == 0) {
+                page = fetch(j + 1);
+                st.saw |= __any(page.tokens > 0);
+            }
             next = load(j + 1, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -696,7 +708,7 @@ __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_kernel(const Sha
     const AtAddr ad = at_addresses(lds_address(own), lane);
     SaState st;
     sa_init(st);
-    bool ok = false;
+    bool ok = false, saw = false;
     if (n > 0) {
         fetch(0);
         ok = load(0, 0);
@@ -721,6 +733,7 @@ __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_kernel(const Sha
         if constexpr (Q32) sa_scores_left(ka, kb, ql, s);
         uint32_t pw[16], plo[16];
         const int lim = seen ? t.lim : 0;
+        saw |= lim > k0;
         if (__any(lim < k0 + kAtK)) sa_mask(s, k0, lim, hh);
         sa_maximum(st, s);
         st.l += sa_weights<true>(st, s, pw, plo);
@@ -742,6 +755,7 @@ __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_kernel(const Sha
         sa_pv(st, v, pw);
         sa_pv(st, v, plo);
     }
+    st.m = sa_marked(st.m, saw);
     part_finish(pl, w, st, smem, wave, lane);
 }
 
@@ -842,7 +856,10 @@ __device__ __forceinline__ void sf_few_part(const SharedAttnArgs& a, const Share
     FewState st;
     float v[kPage];
     for (int u = 0; u < n; ++u) {
-        if ((u & 63) == 0) fetch(u);
+        if ((u & 63) == 0) {
+            fetch(u);
+            st.saw |= __any(page.tokens > 0);
+        }
         const int tokens = __builtin_amdgcn_readlane(page.tokens, u & 63);
         const char* src = page_at(a, page, u & 63);
 #pragma unroll
@@ -922,7 +939,7 @@ __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_f32_kernel(const
     }
     SaState st;
     sa_init(st);
-    bool ok = false;
+    bool ok = false, saw = false;
     if (n > 0) {
         fetch(0);
         ok = load(0, 0);
@@ -953,6 +970,7 @@ __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_f32_kernel(const
             s[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(k[i].w, q[i].w, s[0], 0, 0, 0);
         }
         const int lim = seen ? t.lim : 0;
+        saw |= lim > k0;
         if (__any(lim < k0 + kSfK)) {
 #pragma unroll
             for (int i = 0; i < 16; ++i)
@@ -994,6 +1012,7 @@ __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_f32_kernel(const
             st.o1 = __builtin_amdgcn_mfma_f32_32x32x2f32(v1[i], s[0][i], st.o1, 0, 0, 0);
         }
     }
+    st.m = sa_marked(st.m, saw);
     part_finish(pl, w, st, smem, wave, lane);
 }
 
@@ -1147,6 +1166,7 @@ __global__ __launch_bounds__(kStWaves * 64, 3) void shared_tile_kernel(const Sha
         return tokens;
     };
     const AtAddr ad = at_addresses(lds_address(smem), lane);
+    bool saw = false;
     int next = n > 0 ? load(0, 0) : 0, next_whose = n > 0 ? __builtin_amdgcn_readlane(whose, 0) : 0;
     auto step = [&](auto stage, int j) {  // tile j, in the stage at SO
         constexpr int SO = decltype(stage)::value;
@@ -1161,6 +1181,7 @@ __global__ __launch_bounds__(kStWaves * 64, 3) void shared_tile_kernel(const Sha
         }
         const int lim = of == kWave ? pre_lim : !PACK || of == seq ? own_lim : 0;
         if (tokens == 0 || !rows || !__any(lim > k0)) return;  // nothing for this wave
+        saw |= lim > k0;
         const bool mask = __any(lim < k0 + kAtK);
         uint4 ka[4], kb[4];
         at_f32x16 s[2];
@@ -1187,7 +1208,8 @@ __global__ __launch_bounds__(kStWaves * 64, 3) void shared_tile_kernel(const Sha
         if (j + 1 < n) step(std::integral_constant<int, kAtStage>{}, j + 1);
     }
     const RowPair ls = swap32(st.l);
-    const float l = ls.a + ls.b, inv = l == 0.f ? 0.f : 1.0f / l;
+    st.m = sa_marked(st.m, saw);
+    const float l = ls.a + ls.b, inv = sa_inverse(l, st.m);
     if constexpr (CUT) {
         if (pair >= o.end || seq < 0) return;
         const int64_t at = part * ((int64_t)a.rows * a.n_head) + (int64_t)row * a.n_head + head;
@@ -1241,6 +1263,7 @@ __global__ __launch_bounds__(kSwWaves * 64, 2) void shared_whole_kernel(const Sh
         FewState few;
         few_pages<Q32>(a, t, n, own, lane, few, [&](int) { return page; });
         few.o[0] += few.o[1];
+        few.m = sa_marked(few.m, few.saw);
 #pragma unroll
         for (int d = 4; d < kWave; d <<= 1) few.l += __shfl_xor(few.l, d, kWave);
         __syncthreads();
@@ -1264,7 +1287,7 @@ __global__ __launch_bounds__(kSwWaves * 64, 2) void shared_whole_kernel(const Sh
             l += mrg[(w * 6 + 5) * 64 + wave] * f;
             x += mrg[(w * 6 + wave) * 64 + lane] * f;
         }
-        x *= l == 0.f ? 0.f : 1.0f / l;
+        x *= sa_inverse(l, mm);
         const size_t at = (size_t)row * a.o_ld + head * kHeadDim + lane;
         if (Q32 && a.o_f32) reinterpret_cast<float*>(a.o)[at] = x;
         else reinterpret_cast<uint16_t*>(a.o)[at] = (uint16_t)bf16x2_rne(x, 0.f);
@@ -1317,6 +1340,7 @@ __global__ __launch_bounds__(kSwWaves * 64, 2) void shared_whole_kernel(const Sh
         sa_pv(st, v, pw);
         sa_pv(st, v, plo);
     }
+    st.m = sa_marked(st.m, __any(page.tokens > 0));
     // the waves' (m, l, O) through LDS, lane for lane; each wave then sums a quarter of the dims
     __syncthreads();
     float* mrg = reinterpret_cast<float*>(smem);  // [4][34][64]
@@ -1346,7 +1370,7 @@ __global__ __launch_bounds__(kSwWaves * 64, 2) void shared_whole_kernel(const Sh
         for (int i = 0; i < 8; ++i) x[i] += mw[(8 * wave + i) * 64 + lane] * f;
     }
     const RowPair ls = swap32(l);
-    const float sum = ls.a + ls.b, inv = sum == 0.f ? 0.f : 1.0f / sum;
+    const float inv = sa_inverse(ls.a + ls.b, mm);
     if (t.row < 0) return;
     // element 8 wave + i: dims 16 wave + 8 (i / 4) + 4 hh + i % 4
     const size_t at = (size_t)t.row * a.o_ld + t.head * kHeadDim + 16 * wave + 4 * hh;
@@ -1412,7 +1436,7 @@ __global__ __launch_bounds__(kJoinWaves * 64) void shared_join_kernel(const Shar
         o[i] = p32.a + p32.b;
     }
     if (grp != 0) return;
-    const float inv = inactive || l == 0.f ? 0.f : 1.0f / l;
+    const float inv = inactive ? 0.f : sa_inverse(l, m);
     if (inactive) o[0] = o[1] = o[2] = o[3] = 0.f;
     const size_t at = (size_t)r * a.o_ld + h * kHeadDim + d;
     if constexpr (F32)

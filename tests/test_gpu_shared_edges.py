@@ -164,6 +164,51 @@ def test_an_infinite_value_is_infinite_where_it_is_seen(dtype, H, KH, prefix, pa
     assert torch.equal(b.out.view(b.T, H, 64), want)
 
 
+@pytest.mark.parametrize("dtype,H,KH,prefix,past,rows,takes", FORMS)
+def test_rows_whose_every_score_is_minus_infinity(dtype, H, KH, prefix, past, rows, takes):
+    """Such a row has no softmax: NaN, where a row that sees no token is 0.  Tokens with a score of -inf next
+    to others weigh nothing, wherever they are."""
+    b = form(dtype, H, KH, prefix, past, rows, takes)
+    b.qd.abs_().add_(0.25)
+    clean = b.kv.pool.clone()
+    pages = torch.from_numpy(b.pre).cuda()
+    own = torch.from_numpy(b.table[b.table >= 0]).cuda()
+    # all of them
+    b.kv.pool[:, :, 0] = -float("inf")
+    b.call()
+    torch.cuda.synchronize()
+    assert torch.isnan(b.out.float()).all()
+    # the prefix's: what the call without a prefix gives; the first own page's: what is left is finite
+    b.kv.pool.copy_(clean)
+    b.kv.pool[:, pages, 0] = -float("inf")
+    b.call()
+    torch.cuda.synchronize()
+    got = b.out.clone()
+    alone, none = torch.empty_like(b.out), torch.full_like(b.ws, 0xFF)
+    ftts.shared_attention(b.qd[:, :H * 64], b.kv, 0, b.pt, None, alone, none, row_offsets=b.cud)
+    torch.cuda.synchronize()
+    assert torch.isfinite(got.float()).all()
+    err = (got.float() - alone.float()).norm() / alone.float().norm()
+    assert err <= (2e-5 if dtype == "f32" else 2.0 ** -7), err    # (each is within half of that of the exact result)
+    b.kv.pool.copy_(clean)
+    b.kv.pool[:, own, 0] = -float("inf")
+    b.call()
+    torch.cuda.synchronize()
+    got = b.out.clone()
+    few = ftts.PageTableView(torch.full_like(b.pt.block_table, -1), b.pt.seq_lens)
+    ftts.shared_attention(b.qd[:, :H * 64], b.kv, 0, few, b.prefix, alone, none, row_offsets=b.cud)
+    torch.cuda.synchronize()
+    err = (got.float() - alone.float()).norm() / alone.float().norm()
+    assert torch.isfinite(got.float()).all() and err <= (2e-5 if dtype == "f32" else 2.0 ** -7), err
+    # a row that sees no token, next to those: no page of sequence 0 is in the pool, and the prefix is none
+    b.kv.pool[:, :, 0] = -float("inf")
+    b.pt.block_table[0] = -1
+    ftts.shared_attention(b.qd[:, :H * 64], b.kv, 0, b.pt, None, alone, none, row_offsets=b.cud)
+    torch.cuda.synchronize()
+    first = slice(0, 1 if rows is None else rows[0])
+    assert (alone[first] == 0).all() and torch.isnan(alone[first.stop:].float()).all()
+
+
 @pytest.mark.parametrize("dtype,H,KH,prefix,past,rows,takes", [f for f in FORMS if f[5]])
 def test_a_value_that_is_not_finite_counts_at_a_weight_of_zero(dtype, H, KH, prefix, past, rows, takes):
     """0 * NaN = NaN, in a tile that some rows see in part as in the others; rows before the token keep their bits."""
