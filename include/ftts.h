@@ -478,6 +478,22 @@ int ftts_shared_attention(const ftts_attn_shape* shape, const void* q, int64_t q
                           int32_t layer, void* out, int64_t out_stride, void* ws, size_t ws_bytes,
                           void* stream);
 
+/* How ftts_shared_attention runs a call of these sizes (prompts: with row_offsets).  Host only: a pure
+ * function of its arguments that touches no device.  Errors as ftts_shared_attention's. */
+#define FTTS_SHARED_CUT 0    /* the prefix for all rows at once and the own pages, in runs along the tokens */
+#define FTTS_SHARED_WHOLE 1  /* a workgroup a sequence and key head */
+#define FTTS_SHARED_TILE 2   /* 128 rows of a sequence share its pages */
+#define FTTS_SHARED_PACKED 3 /* 128 rows of several sequences do */
+typedef struct {
+    int32_t kernel;                  /* FTTS_SHARED_* */
+    int32_t parts;                   /* workgroups along a row's pages (cut: 0) */
+    int32_t prefix_rows, own_rows;   /* cut: (row, head) pairs of a workgroup on either side, */
+    int32_t prefix_pages, own_pages; /*   and its pages (0 without a prefix); else 0 */
+    int32_t partials;                /* partial results a row and head, for a second launch to join; 0: none */
+} ftts_shared_launch;
+int ftts_shared_attention_plan(const ftts_attn_shape* shape, int32_t B, int32_t n_rows, int32_t prompts,
+                               int32_t prefix_len, int32_t max_pages, ftts_shared_launch* out);
+
 /* ---- the model behind a shared prefix --------------------------------------------------------
  *
  * One voice prompt, many sentences: the prompt's rows are prefilled once, as a sequence of its

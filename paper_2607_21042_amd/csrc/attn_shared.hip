@@ -1545,23 +1545,48 @@ size_t shared_attention_bytes(int n_head, int rows, int prefix_len, int max_page
     return (size_t)n * (kHeadDim + 2) * 4 + 256;
 }
 
+// How a call runs (ftts_shared_attention_plan hands it out).
+struct SharedChoice {
+    int kernel, slots;  // FTTS_SHARED_*; partials a row
+    TilePlan tile;
+    SharedPlan cut;
+};
+static SharedChoice shared_choice(bool f32, const SharedAttnArgs& a) {
+    SharedChoice c{};
+    if (!f32) c.tile = tile_plan(a);
+    if (c.tile.tiles > 0) {
+        c.kernel = c.tile.pack ? FTTS_SHARED_PACKED : FTTS_SHARED_TILE;
+        c.slots = c.tile.parts > 1 ? c.tile.parts : 0;
+    } else if (!f32 && shared_whole(a)) {
+        c.kernel = FTTS_SHARED_WHOLE;
+    } else {
+        c.kernel = FTTS_SHARED_CUT;
+        c.cut = shared_plan(f32, a.n_head, a.n_kv_head, a.B, a.rows, a.row_offsets != nullptr, a.prefix_len, a.max_pages);
+        c.slots = c.cut.s_pre + c.cut.s_own;
+    }
+    return c;
+}
+
 hipError_t launch_shared_attention(int dtype, const SharedAttnArgs& a, void* ws, size_t ws_bytes, hipStream_t st) {
     const bool f32 = dtype == FTTS_F32;
     // (the decode step's forms)
     if (a.q_f32 || a.o_f32 || a.active || a.len_add) {
         if (a.row_offsets || a.n_head > kFew * a.n_kv_head) return hipErrorInvalidValue;
     }
-    const TilePlan tp = f32 ? TilePlan{0, 1, false} : tile_plan(a);
+    const SharedChoice c = shared_choice(f32, a);
+    const TilePlan& tp = c.tile;
     const int64_t rows_heads = (int64_t)a.rows * a.n_head;
     const dim3 jg((unsigned)((rows_heads + kJoinWaves - 1) / kJoinWaves)), jt(kJoinWaves * 64);
+    SharedPlan p = c.cut;
+    if (c.slots > 0) {
+        if ((size_t)c.slots * rows_heads * (kHeadDim + 2) * 4 > ws_bytes) return hipErrorInvalidValue;
+        p.o = reinterpret_cast<float*>(ws);
+        p.ml = reinterpret_cast<float2*>(p.o + c.slots * rows_heads * kHeadDim);
+    }
     if (tp.tiles > 0) {
         const dim3 wg((unsigned)(tp.tiles * a.n_kv_head * tp.parts)), wt(kStWaves * 64);
-        SharedPlan p{};
         if (tp.parts > 1) {
-            p.s_pre = tp.parts;
-            if ((size_t)p.s_pre * rows_heads * (kHeadDim + 2) * 4 > ws_bytes) return hipErrorInvalidValue;
-            p.o = reinterpret_cast<float*>(ws);
-            p.ml = reinterpret_cast<float2*>(p.o + p.s_pre * rows_heads * kHeadDim);
+            p.s_pre = tp.parts;  // (for the join)
             if (tp.pack) hipLaunchKernelGGL((shared_tile_kernel<true, true>), wg, wt, 0, st, a, tp.tiles, p);
             else hipLaunchKernelGGL((shared_tile_kernel<false, true>), wg, wt, 0, st, a, tp.tiles, p);
             if (hipError_t e = hipGetLastError()) return e;
@@ -1573,7 +1598,7 @@ hipError_t launch_shared_attention(int dtype, const SharedAttnArgs& a, void* ws,
         }
         return hipGetLastError();
     }
-    if (!f32 && shared_whole(a)) {
+    if (c.kernel == FTTS_SHARED_WHOLE) {
         const int64_t own_tiles = a.B * ceil_div(a.n_head / a.n_kv_head, kSaQ);
         const dim3 wg((unsigned)(own_tiles * a.n_kv_head)), wt(kSwWaves * 64);
         const bool few = a.n_head <= kFew * a.n_kv_head;
@@ -1582,10 +1607,6 @@ hipError_t launch_shared_attention(int dtype, const SharedAttnArgs& a, void* ws,
         else hipLaunchKernelGGL((shared_whole_kernel<false, false>), wg, wt, 0, st, a);
         return hipGetLastError();
     }
-    SharedPlan p = shared_plan(f32, a.n_head, a.n_kv_head, a.B, a.rows, a.row_offsets != nullptr, a.prefix_len, a.max_pages);
-    if ((size_t)(p.s_pre + p.s_own) * rows_heads * (kHeadDim + 2) * 4 > ws_bytes) return hipErrorInvalidValue;
-    p.o = reinterpret_cast<float*>(ws);
-    p.ml = reinterpret_cast<float2*>(p.o + (p.s_pre + p.s_own) * rows_heads * kHeadDim);
     const int64_t groups = (int64_t)((a.n_kv_head * p.s_pre + 7) / 8 * 8) * p.row_tiles + (int64_t)a.n_kv_head * p.own_tiles * p.s_own;
     const dim3 g((unsigned)groups), t(kSaWaves * 64);
     if (f32 && a.row_offsets) hipLaunchKernelGGL(shared_part_f32_kernel<true>, g, t, 0, st, a, p);
@@ -1630,6 +1651,28 @@ size_t ftts_shared_attention_workspace_bytes(const ftts_attn_shape* shape, int32
                                              int32_t prefix_len, int32_t max_pages) {
     if (check_shape(shape, B, n_rows, prefix_len, max_pages) != FTTS_OK) return 0;
     return shared_attention_bytes(shape->n_head, n_rows, prefix_len, max_pages);
+}
+
+int ftts_shared_attention_plan(const ftts_attn_shape* shape, int32_t B, int32_t n_rows, int32_t prompts, int32_t prefix_len,
+                               int32_t max_pages, ftts_shared_launch* out) {
+    if (!out) return set_error(FTTS_E_INVALID_ARG, "shared_attention_plan: out is NULL");
+    if (int rc = check_shape(shape, B, n_rows, prefix_len, max_pages)) return rc;
+    if (n_rows < 1 || (!prompts && n_rows != B))
+        return set_error(FTTS_E_SHAPE, "shared_attention_plan: n_rows must be at least 1, and B without row offsets");
+    const int32_t offsets = 0;  // (the rules ask only whether there are any)
+    SharedAttnArgs a{};
+    a.n_head = shape->n_head;
+    a.n_kv_head = shape->n_kv_head;
+    a.max_pages = max_pages;
+    a.row_offsets = prompts ? &offsets : nullptr;
+    a.prefix_len = prefix_len;
+    a.B = B;
+    a.rows = n_rows;
+    const SharedChoice c = shared_choice(shape->dtype == FTTS_F32, a);
+    const bool cut = c.kernel == FTTS_SHARED_CUT;
+    *out = ftts_shared_launch{c.kernel, cut ? 0 : c.tile.tiles > 0 ? c.tile.parts : 1, c.cut.q_pre, c.cut.q_own,
+                              cut && prefix_len > 0 ? c.cut.c_pre : 0, c.cut.c_own, c.slots};
+    return FTTS_OK;
 }
 
 int ftts_shared_attention(const ftts_attn_shape* shape, const void* q, int64_t q_stride, const int32_t* row_offsets,

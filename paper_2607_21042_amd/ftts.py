@@ -25,6 +25,7 @@ MAX_TOP_K = 64
 MAX_BATCH = 64
 MAX_TABLE_BATCH = 1024
 MAX_SHARED_PREFIX = 1 << 20
+SHARED_CUT, SHARED_WHOLE, SHARED_TILE, SHARED_PACKED = 0, 1, 2, 3
 PAGE = 64
 
 _c = ctypes
@@ -87,6 +88,11 @@ class AttnShape(_c.Structure):
     _fields_ = [("dtype", i32), ("n_head", i32), ("n_kv_head", i32), ("d_head", i32)]
 
 
+class SharedLaunch(_c.Structure):
+    _fields_ = [("kernel", i32), ("parts", i32), ("prefix_rows", i32), ("own_rows", i32), ("prefix_pages", i32),
+                ("own_pages", i32), ("partials", i32)]
+
+
 class LinearShape(_c.Structure):
     _fields_ = [("rows_large", i32), ("large_rows", i32), ("large_cols", i32), ("small_cols", i32), ("splits", i32),
                 ("scratch_counters", i32), ("scratch_floats", _c.c_int64)]
@@ -147,6 +153,8 @@ def lib():
         L.ftts_append_kv.argtypes = [i32, i32, vp, i64, vp, i64, i32, vp, P(KvPool), i32, i32, vp]
         L.ftts_shared_attention_workspace_bytes.restype = _c.c_size_t
         L.ftts_shared_attention_workspace_bytes.argtypes = [P(AttnShape), i32, i32, i32, i32]
+        L.ftts_shared_attention_plan.restype = _c.c_int
+        L.ftts_shared_attention_plan.argtypes = [P(AttnShape), i32, i32, i32, i32, i32, P(SharedLaunch)]
         L.ftts_shared_attention.restype = _c.c_int
         L.ftts_shared_attention.argtypes = [P(AttnShape), vp, i64, vp, i32, i32, P(SharedPrefixC), P(PageTable),
                                             P(KvPool), i32, vp, i64, vp, _c.c_size_t, vp]
@@ -440,6 +448,15 @@ def shared_attention_workspace_bytes(n_head: int, n_kv_head: int, dtype: int, ba
     if n == 0:
         raise FTTSError(-1, lib().ftts_last_error().decode())
     return n
+
+
+def shared_attention_plan(n_head: int, n_kv_head: int, dtype: int, batch: int, rows: int, prompts: bool, prefix_len: int,
+                          max_pages: int) -> SharedLaunch:
+    """ftts_shared_attention_plan: how a call of those sizes is launched (host only; prompts: with row_offsets)."""
+    out = SharedLaunch()
+    s = AttnShape(dtype, n_head, n_kv_head, 64)
+    _check(lib().ftts_shared_attention_plan(_c.byref(s), batch, rows, int(prompts), prefix_len, max_pages, _c.byref(out)))
+    return out
 
 
 def shared_attention(q, kv, layer: int, page_table, prefix, out, ws, row_offsets=None, stream=None):
