@@ -225,3 +225,34 @@ def test_a_value_that_is_not_finite_counts_at_a_weight_of_zero(dtype, H, KH, pre
     b.call()
     torch.cuda.synchronize()
     assert torch.equal(b.out.float().nan_to_num(123.0), want.float().nan_to_num(123.0))
+
+
+# ---- pages outside the pool, wide tables ----------------------------------------------------------
+@pytest.mark.parametrize("H,KH,prefix,past,rows,takes", [
+    (12, 4, 2500, [10, 0, 300], [90, 130, 90], "packed in 8"), (20, 4, 2000, [0, 64, 3, 700], [90, 0, 128, 129], "tile in 4"),
+    (20, 20, 0, [2900], [300], "tile in 4")])
+def test_parts_with_pages_outside_the_pool(H, KH, prefix, past, rows, takes):
+    """A page of the prefix, an own page and a sequence of fewer tokens than rows, where a tile's chain is cut."""
+    b = Batch("bf16", H, KH, prefix, [p + n for p, n in zip(past, rows)], rows, extra_rows=2, layers=1)
+    if prefix:
+        b.pre = b.pre.copy()
+        b.pre[len(b.pre) // 2], b.pre[0] = b.pool.shape[1], -1
+    b.table[-1, 2], b.table[0, 0] = 2 ** 31 - 1, -7
+    b.lens[0] = rows[0] - 40 if len(rows) > 1 else b.lens[0]
+    b.gpu()
+    assert kernel(b) == takes
+    print(f"{takes}: pages outside the pool, {H}/{KH} heads, prefix {prefix}, rows {rows}", flush=True)
+    b.call()
+    b.check()
+
+
+@pytest.mark.parametrize("dtype,H,KH,prefix,lens,rows", [
+    ("bf16", 20, 20, 300, [700, 0, 1, 64, 65, 513, 129, 300] * 4, None), ("f32", 20, 20, 130, [700, 0, 1, 513, 129, 300], None),
+    ("bf16", 20, 4, 0, [1200, 33, 7] * 21, None), ("bf16", 6, 3, 65, [90, 1, 300], [3, 1, 40]),
+    ("f32", 4, 2, 65, [90, 1, 300], [3, 1, 40]), ("bf16", 20, 20, 700, [200, 260], [120, 200])])
+def test_tables_far_wider_than_their_sequences(dtype, H, KH, prefix, lens, rows):
+    """512 pages a sequence, as a server's table may have: runs of own pages grow with the table."""
+    b = Batch(dtype, H, KH, prefix, lens, rows, layers=1, width=512).gpu()
+    print(f"wide table: {dtype} {H}/{KH} heads, prefix {prefix}, {len(lens)} sequences: {kernel(b)}", flush=True)
+    b.call()
+    b.check()
