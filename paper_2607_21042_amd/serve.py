@@ -174,26 +174,28 @@ class Scheduler:
             return
         slots = [s for s, _ in group]
         lens = [r.prefix.shape[0] for _, r in group]
-        i32 = dict(dtype=torch.int32, device="cuda")
-        bt_d = torch.full((len(group), self.max_pages), -1, **i32)
-        # the pages just taken, in order, for prefix and budget
-        ftts.build_tables(torch.tensor([n + r.max_new for n, (_, r) in zip(lens, group)], **i32),
-                          torch.tensor([p for s in slots for p in self.slot_pages[s]], **i32), self.kv.n_pages, bt_d,
-                          torch.empty(len(group) + 1, **i32), None, torch.empty(2, **i32))
+        budgets = [r.max_new for _, r in group]
+        # everything in one copy: lengths with the budget, prefix lengths, slots, budgets and the pages just taken
+        n, i32 = len(group), dict(dtype=torch.int32, device="cuda")
+        host = [a + b for a, b in zip(lens, budgets)] + lens + slots + budgets + [p for s in slots for p in self.slot_pages[s]]
+        ints = torch.tensor(host, **i32)
+        total, lens_d, slots_d, budgets_d = ints[:4 * n].view(4, n)
+        bt_d, out = torch.empty((n, self.max_pages), **i32), torch.empty(n + 3, **i32)
+        # (none is refused: submit and the pool have seen to the pages)
+        ftts.build_tables(total, ints[4 * n:], self.kv.n_pages, bt_d, out[:n + 1], None, out[n + 1:])
         prefix = self._rows([r.prefix for _, r in group])
-        pt = ftts.PageTableView(bt_d, torch.zeros(len(group), **i32))
+        pt = ftts.PageTableView(bt_d, lens_d)
         if self.shared is None:
             ftts.prefill(self.model, prefix, lens, pt, self.kv, None, self.ws)
         else:
             ftts.prefill_shared(self.model, self.shared, prefix, lens, None, [0] * len(group), 0, 0, pt, self.kv, None,
                                 self.ws)
-        idx = torch.tensor(slots, dtype=torch.int64, device="cuda")
+        idx = slots_d.long()
         self.block_table.index_copy_(0, idx, bt_d)
-        self.pt.seq_lens.index_copy_(0, idx, torch.tensor(lens, dtype=torch.int32, device="cuda"))
+        self.pt.seq_lens.index_copy_(0, idx, lens_d)
         self.tokens.index_fill_(0, idx, self.shape.start_token)
         self.positions.index_fill_(0, idx, 0)
-        self.remaining.index_copy_(0, idx, torch.tensor([r.max_new for _, r in group], dtype=torch.int32,
-                                                       device="cuda"))
+        self.remaining.index_copy_(0, idx, budgets_d)
 
     # -- one chunk of decode steps -----------------------------------------------------------
     def _launch_chunk(self, k: int):
