@@ -493,11 +493,34 @@ def shared_workspace_bytes(cfg: Config, max_batch: int, max_rows: int, prefix_le
     return n
 
 
+def _sized(name, t, n, dtype):
+    """Checks that tensor t has dtype `dtype` and n elements (None and bare addresses pass)."""
+    if t is None or isinstance(t, int):
+        return
+    if t.dtype != dtype:
+        raise FTTSError(-3, f"{name} must be {dtype}")
+    if t.numel() != n:
+        raise FTTSError(-2, f"{name} must have {n} elements, not {t.numel()}")
+
+
+def _table_of(page_table, B):
+    if page_table.block_table.shape[0] < B or page_table.seq_lens.numel() < B:
+        raise FTTSError(-2, f"the page table must have {B} rows and lengths")
+
+
 def prefill_shared(model, prefix, cond_emb, cond_lens, text_ids, text_lens, text_vocab, text_pos0, page_table, kv,
                    last_logits, ws, stream=None):
     """ftts_prefill_shared: ftts_prefill_ids for sequences that continue `prefix` (a SharedPrefix);
     `cond_lens` and `text_lens` are host sequences."""
-    B = len(cond_lens)
+    B, rows, texts = len(cond_lens), sum(int(x) for x in cond_lens), sum(int(x) for x in text_lens)
+    if len(text_lens) != B:
+        raise FTTSError(-2, f"text_lens must have {B} entries, as cond_lens has")
+    if cond_emb is None and rows > 0:
+        raise FTTSError(-1, "cond_emb is None, cond_lens are not 0")
+    _sized("cond_emb", cond_emb, rows * model.shape.d_model, act_dtype(model.wdtype))
+    _sized("text_ids", text_ids, texts, torch.int32)
+    _sized("last_logits", last_logits, B * model.shape.vocab, torch.float32)
+    _table_of(page_table, B)
     cl = (i32 * B)(*[int(x) for x in cond_lens])
     tl = (i32 * B)(*[int(x) for x in text_lens])
     _check(lib().ftts_prefill_shared(_c.byref(model.c), _c.byref(prefix.c), _ptr(cond_emb), cl, _ptr(text_ids), tl,
@@ -508,6 +531,13 @@ def prefill_shared(model, prefix, cond_emb, cond_lens, text_ids, text_lens, text
 def decode_step_shared(model, prefix, tokens, positions, page_table, kv, logits_out, sampled_out, uniforms,
                        sampling: Sampling, ws, stream=None, hidden_out=None):
     """ftts_decode_step_shared: a decode step of sequences that continue `prefix` (a SharedPrefix)."""
+    B = tokens.numel()
+    for name, t in (("tokens", tokens), ("positions", positions), ("sampled_out", sampled_out)):
+        _sized(name, t, B, torch.int32)
+    for name, t, n in (("logits_out", logits_out, B * model.shape.vocab), ("hidden_out", hidden_out, B * model.shape.d_model),
+                       ("uniforms", uniforms, B)):
+        _sized(name, t, n, torch.float32)
+    _table_of(page_table, B)
     _check(lib().ftts_decode_step_shared(_c.byref(model.c), _c.byref(prefix.c), _ptr(tokens), _ptr(positions),
                                          _c.byref(page_table.c), _c.byref(kv.c), _ptr(logits_out), _ptr(hidden_out),
                                          _ptr(sampled_out), _ptr(uniforms), _c.byref(sampling), tokens.numel(),

@@ -1,4 +1,6 @@
 """What the scheduler takes as a request, on the host alone: no GPU, no model."""
+from types import SimpleNamespace
+
 import numpy as np
 import pytest
 
@@ -8,6 +10,7 @@ from paper_2607_21042_amd import ftts, serve
 def scheduler(n_pages, max_pages, prefix_pages=0):
     """A scheduler's host state: its pool after the shared prefix has taken its pages, and two empty slots."""
     s = serve.Scheduler.__new__(serve.Scheduler)
+    s.shape = SimpleNamespace(d_model=4)
     s.max_pages, s.pool = max_pages, ftts.PagePool(n_pages)
     s.pool.alloc(prefix_pages)
     s.slot_pages, s.waiting, s.next_rid = [[], []], [], 0
