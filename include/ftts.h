@@ -466,9 +466,13 @@ size_t ftts_shared_attention_workspace_bytes(const ftts_attn_shape* shape, int32
  *   pt           block table and own lengths; a length past max_pages * 64 ends there, a
  *                negative one makes its sequence inactive: its rows become 0.
  * A row that sees no token becomes 0 (one that sees tokens, all with a score of -inf, NaN), and
- * tokens in pages outside the pool are not seen; slots of a page past a sequence's end may hold anything.  A value that is not finite reaches only
- * rows that see its token.  In bf16 the scores and the sums are fp32 and the output is rounded
- * once; the weights multiply the values in 16-bit products.
+ * tokens in pages outside the pool are not seen; slots of a page past a sequence's end may hold
+ * anything.  A value that is not finite reaches only rows that see its token.  In bf16 the scores and the sums are fp32 and the output is rounded
+ * once; the weights meet the values in bf16 products, as two parts of each (within 2^-16 of it) in
+ * FTTS_SHARED_CUT and FTTS_SHARED_WHOLE, rounded once (2^-8), as in ftts_prefill, in the tiles of
+ * prompts (ftts_shared_attention_plan says which a call takes).  Equal calls give equal bits; how a
+ * row's tokens are cut into sums follows the whole call, its neighbours' lengths in packed tiles
+ * among it, so a row's rounding may differ between batches.
  * 1 <= B <= FTTS_MAX_BATCH, n_rows <= 2^24, n_rows * n_head < 2^31.  `ws` holds intermediate results of the call only;
  * calls that can run at the same time need one each.
  */
@@ -517,8 +521,9 @@ int ftts_prefill_shared(const ftts_weights* w, const ftts_shared_prefix* prefix,
 
 /* ftts_decode_step_hidden (hidden_out may be NULL) for sequences that continue `prefix`; an own
  * length of 0 is a sequence's first token right behind it.  The step's queries reach the scores as
- * without a prefix: fp32, or over a bf16 pool two bf16 parts of each (16 bits).  One kernel per phase: FTTS_E_UNSUPPORTED
- * where the persistent step is forced. */
+ * without a prefix: fp32, or over a bf16 pool two bf16 parts of each (16 bits).  One kernel per
+ * phase: FTTS_E_UNSUPPORTED where the persistent step is forced, and slower for one or two
+ * sequences than that step on copies of the prefix. */
 int ftts_decode_step_shared(const ftts_weights* w, const ftts_shared_prefix* prefix, const int32_t* tokens,
                             const int32_t* positions, const ftts_page_table* pt, const ftts_kv_pool* kv,
                             float* logits_out, float* hidden_out, int32_t* sampled_out, const float* uniforms,

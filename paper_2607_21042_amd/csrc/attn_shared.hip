@@ -485,8 +485,8 @@ __device__ __forceinline__ void few_finish(const SharedPlan& pl, const PartWork&
     }
 }
 
-// bf16: K and V through LDS as in shared_part_kernel.  32 sequences of 64-700 tokens behind 1500, 20 heads: 18.2 us with
-// the join (tiles of 32 rows: 20.1), 8 of 30-500 behind 700 10.1 (11.3).  Two groups of 4 rows a tile, for 5 to 8 query
+// bf16: K and V through LDS as in shared_part_kernel.  In a graph, with the join, 32 sequences of 64-700 tokens behind
+// 1500, 20 heads, 18.2 us (tiles of 32 rows: 20.1), 8 of 30-500 behind 700 10.1 (11.3).  Two groups of 4 rows a tile, for 5 to 8 query
 // heads a key head, were slower than one tile of 32: 14.4 us for 24 sequences of 20/4 heads (13.6).
 typedef short few_s16x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ few_s16x4 few_op(uint32_t x, uint32_t y) { return __builtin_bit_cast(few_s16x4, make_uint2(x, y)); }
@@ -660,9 +660,9 @@ __device__ __forceinline__ void few_part(const SharedAttnArgs& a, const SharedPl
 // reading bounds).  PROMPT: several rows a sequence, so a tile's rows may see different tokens.
 //
 // Two waves a workgroup: one wave each measured 1-2 us better for 32 short sequences and 2 worse behind long prefixes,
-// four 1-3 worse nearly everywhere (more idle waves at a run's end).  Traced with the join: 32 sequences of 64-700 tokens
-// behind 1500, 20 heads, 15.9 + 3.9 us for 76 MB; 64 of 100-900 behind 16,001 50 + 5 us for 255 MB (a read reaches
-// 5.9 TB/s: 12.9 and 43 us); 24 of up to 1200 behind 5000, 20 query and 4 key heads, 10 + 3.7 for 22 MB: there a chain of
+// four 1-3 worse nearly everywhere (more idle waves at a run's end).  Calls in a row, the join included: 32 sequences of
+// 64-700 tokens behind 1500, 20 heads, 17.8 us for 76 MB; 64 of 100-900 behind 16,001 53 us for 255 MB (a read reaches
+// 5.9 TB/s: 12.9 and 43 us); 24 of up to 1200 behind 5000, 20 query and 4 key heads, 12.9 for 22 MB: there a chain of
 // page ids, keys, products, values and the hand-over, not bytes.
 template <bool PROMPT, bool Q32>
 __global__ __launch_bounds__(kSaWaves * 64, 2) void shared_part_kernel(const SharedAttnArgs a, const SharedPlan pl) {
@@ -1081,7 +1081,7 @@ __device__ __forceinline__ TilePages tile_pages(const SharedAttnArgs& a, int til
 //
 // Four prompts of 1500-2300 rows behind 8000 tokens, 20 heads: 491 us, 800 TFLOP/s (a library product of 8192^3: 1460);
 // 32 of 20-220 behind 600 36 us (a tile for each sequence: 44).  Counted for the long ones: matrix units busy 34% of the
-// time, vector units 45% (32 exponentials of 8 cycles and about 114 operations of 4 a tile of 32 rows and a page), both
+// time, vector units 49% (32 exponentials of 8 cycles and about 114 operations of 4 a tile of 32 rows and a page), both
 // at once 10%, and 15% of the units' time at the launch's ends.  Measured and not taken: three stages, 64 rows a wave
 // (spills), two waves a workgroup (more loads), the next tile's scores under this one's exponentials (two waves a SIMD:
 // 637 us), half a tile's weights under the other half's products (spills: 525), the maximum of the first tile alone with

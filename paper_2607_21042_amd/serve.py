@@ -75,7 +75,9 @@ class Scheduler:
     stop_on_token  end a request when it samples the stop code (stop_token, default the
                shape's), not only when its budget runs out.
     shared_prefix  rows [P][d_model] that every request continues (a voice prompt), or None;
-               requests' prefixes and max_ctx count what follows them.
+               requests' prefixes and max_ctx count what follows them.  With one or two slots a
+               copy of the rows in every request decodes faster (the persistent step, which takes
+               no shared prefix).
     """
 
     def __init__(self, model, shape, max_slots: int, n_pages: int, max_ctx: int, sampling, chunk: int = 16,
