@@ -467,10 +467,11 @@ size_t ftts_shared_attention_workspace_bytes(const ftts_attn_shape* shape, int32
  *                negative one makes its sequence inactive: its rows become 0.
  * A row that sees no token becomes 0 (one that sees tokens, all with a score of -inf, NaN), and
  * tokens in pages outside the pool are not seen; slots of a page past a sequence's end may hold
- * anything.  A value that is not finite reaches only rows that see its token.  In bf16 the scores and the sums are fp32 and the output is rounded
- * once; the weights meet the values in bf16 products, as two parts of each (within 2^-16 of it) in
- * FTTS_SHARED_CUT and FTTS_SHARED_WHOLE, rounded once (2^-8), as in ftts_prefill, in the tiles of
- * prompts (ftts_shared_attention_plan says which a call takes).  Equal calls give equal bits; how a
+ * anything.  A value that is not finite reaches only rows that see its token.  In bf16 the scores
+ * and the sums are fp32 and the output is rounded once; the weights meet the values in bf16
+ * products, as two parts of each (within 2^-16 of it) in FTTS_SHARED_CUT and FTTS_SHARED_WHOLE,
+ * rounded once (2^-8), as in ftts_prefill, in FTTS_SHARED_TILE and FTTS_SHARED_PACKED
+ * (ftts_shared_attention_plan says which a call takes).  Equal calls give equal bits; how a
  * row's tokens are cut into sums follows the whole call, its neighbours' lengths in packed tiles
  * among it, so a row's rounding may differ between batches.
  * 1 <= B <= FTTS_MAX_BATCH, n_rows <= 2^24, n_rows * n_head < 2^31.  `ws` holds intermediate results of the call only;

@@ -85,7 +85,7 @@ class Scheduler:
                  stop_on_token: bool = False, stop_token: int | None = None, shared_prefix: np.ndarray | None = None):
         if chunk < 1 or overlap < 0 or overlap >= chunk:
             raise ValueError("need chunk >= 1 and 0 <= overlap < chunk")
-        if shared_prefix is not None and (shared_prefix.ndim != 2 or shared_prefix.shape[1] != shape.d_model):
+        if shared_prefix is not None and len(shared_prefix) and np.shape(shared_prefix)[1:] != (shape.d_model,):
             raise ValueError(f"shared_prefix must be rows of {shape.d_model}")
         if graphs:
             ftts.graph_steps(chunk)                 # a chunk is one captured graph
@@ -143,7 +143,7 @@ class Scheduler:
 
     # -- requests ----------------------------------------------------------------------------
     def submit(self, req: Request) -> Request:
-        if req.prefix.ndim != 2 or req.prefix.shape[1] != self.shape.d_model:
+        if np.shape(req.prefix)[1:] != (self.shape.d_model,):
             raise ValueError(f"a prefix is rows of d_model, {self.shape.d_model}")
         need = req.prefix.shape[0] + req.max_new
         if req.max_new < 1 or req.prefix.shape[0] < 1 or need > self.max_pages * ftts.PAGE:
