@@ -427,6 +427,75 @@ int ftts_append_kv(int32_t src_dtype, int32_t kv_dtype, const void* k, int64_t k
                    int64_t v_stride, int32_t n_rows, const int32_t* slots, const ftts_kv_pool* kv,
                    int32_t layer, int32_t n_kv_head, void* stream);
 
+/* ---- positions as rotations -------------------------------------------------------------------
+ *
+ * Decoders whose heads carry positions as rotations turn the first `dim` columns of each head of
+ * 64 by the row's position before they meet: pair i of a head's columns, (a, b), becomes
+ *     a' = scale * (a cos t - b sin t),  b' = scale * (b cos t + a sin t),
+ *     t = 2 pi * position * turns[i],
+ * and the columns from dim on pass as they are.  A pair is (i, i + dim / 2) in FTTS_ROTARY_HALVES,
+ * (2 i, 2 i + 1) in FTTS_ROTARY_PAIRS.  Angles are reduced in fp64, so that a position of 2^20 is
+ * turned as exactly as one of 1, and the products are fp32.
+ */
+#define FTTS_ROTARY_HALVES 0
+#define FTTS_ROTARY_PAIRS 1
+#define FTTS_ROTARY_MAX_PAIRS 32
+typedef struct {
+    int32_t dim;                          /* columns turned: even, 2 .. 64                        */
+    int32_t layout;                       /* FTTS_ROTARY_HALVES or FTTS_ROTARY_PAIRS              */
+    float scale;                          /* factor of the turned columns, finite                 */
+    double turns[FTTS_ROTARY_MAX_PAIRS];  /* [dim / 2] turns a position, at most 1 in size        */
+} ftts_rotary;
+
+/* Fills `out` ([host]) for frequencies base^(-2 i / dim) radians a position:
+ *   FTTS_ROTARY_PLAIN   as they are;
+ *   FTTS_ROTARY_LINEAR  divided by factor (positions interpolated);
+ *   FTTS_ROTARY_BASE    from a base larger by factor^(dim / (dim - 2)), which divides the slowest
+ *                       one by factor and leaves the fastest (dim >= 4);
+ *   FTTS_ROTARY_PARTS   by how often a pair turns within `original` positions: `fast` times and
+ *                       more as it is, `slow` times and less divided by factor, linearly mixed
+ *                       between; scale becomes 0.1 ln(factor) + 1 (overwrite it where a model has
+ *                       another).
+ * scale is 1 otherwise.  base > 1, factor >= 1, original >= 1 and 0 <= slow < fast where they are
+ * used (FTTS_E_RANGE otherwise).  Host only. */
+#define FTTS_ROTARY_PLAIN 0
+#define FTTS_ROTARY_LINEAR 1
+#define FTTS_ROTARY_BASE 2
+#define FTTS_ROTARY_PARTS 3
+int ftts_rotary_init(int32_t dim, int32_t layout, double base, int32_t scaling, double factor, double original,
+                     double slow, double fast, ftts_rotary* out);
+
+/*
+ * Rows turned by their positions.
+ *   src_dtype, dst_dtype  FTTS_F32 or FTTS_BF16, of x and out; fp32 rows going to bf16 are rounded
+ *                to nearest even, once, after the rotation; bf16 rows into fp32 are FTTS_E_DTYPE.
+ *   rot          [host].
+ *   x, out       row r at x + r * x_stride (elements), head h in columns 64 h .. 64 h + 63; 16-byte
+ *                aligned, strides a multiple of 16 bytes and at least 64 * n_head.  out may be x
+ *                (same type and stride), or other columns of the same rows; any other overlap is
+ *                FTTS_E_INVALID_ARG.
+ *   positions    [n_rows] int32, any value (negative ones turn back).
+ * n_rows 0 is allowed and enqueues nothing.  n_rows <= 2^24, n_head <= 256.
+ */
+int ftts_rotate(int32_t src_dtype, int32_t dst_dtype, const ftts_rotary* rot, const void* x, int64_t x_stride,
+                int32_t n_rows, int32_t n_head, const int32_t* positions, void* out, int64_t out_stride,
+                void* stream);
+
+/*
+ * ftts_append_kv of keys turned by their positions, and the same rows' queries turned on the way:
+ * what a layer does between its projection and its attention, in one launch.  A position need not
+ * be the slot's: drafted tokens lie side by side and stand one behind the other.
+ *   q, q_out     query rows of n_head heads as in ftts_rotate, to q_out in the pool's type; both
+ *                NULL (n_head 0): no queries.  q_out may be q, or other columns of the same rows
+ *                (not those of k or v).
+ *   k, v, slots, kv, layer, n_kv_head  as in ftts_append_kv, with its limits; k is turned, v is not.
+ * A row whose slot is negative or past the pool is skipped, its row of q_out too.
+ */
+int ftts_append_rotated(int32_t src_dtype, int32_t kv_dtype, const ftts_rotary* rot, const void* q, int64_t q_stride,
+                        int32_t n_head, void* q_out, int64_t q_out_stride, const void* k, int64_t k_stride,
+                        const void* v, int64_t v_stride, int32_t n_rows, const int32_t* positions,
+                        const int32_t* slots, const ftts_kv_pool* kv, int32_t layer, int32_t n_kv_head, void* stream);
+
 /* A prefix that every sequence of a batch continues: its token t lives in page pages[t / 64]
  * (device int32 [ceil(len / 64)]) at slot t % 64 of the same pool.  len is a host value,
  * 0 <= len <= FTTS_MAX_SHARED_PREFIX. */

@@ -16,8 +16,10 @@ quant   -- weight-only quantisation of the GPT linears to W8A16 / W4A16
 sample  -- greedy and temperature / top-k / top-p sampling of the next token.
 paged   -- block tables and slot maps, the write of keys and values by slot, and
            attention behind a shared prefix.
+tree    -- rows turned by their positions, attention of a tree of drafted tokens
+           and the commit of its accepted path.
 
 All arithmetic runs in the dtype the caller picks (fp64 for self-checks, fp32
 for parity); readings of points the paper leaves open are listed in each module.
 """
-from . import gpt, paged, quant, sample  # noqa: F401
+from . import gpt, paged, quant, sample, tree  # noqa: F401

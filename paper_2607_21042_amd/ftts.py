@@ -26,6 +26,9 @@ MAX_BATCH = 64
 MAX_TABLE_BATCH = 1024
 MAX_SHARED_PREFIX = 1 << 20
 SHARED_CUT, SHARED_WHOLE, SHARED_TILE, SHARED_PACKED = 0, 1, 2, 3
+ROTARY_HALVES, ROTARY_PAIRS = 0, 1
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_PARTS = 0, 1, 2, 3
+ROTARY_MAX_PAIRS = 32
 PAGE = 64
 
 _c = ctypes
@@ -93,6 +96,10 @@ class SharedLaunch(_c.Structure):
                 ("own_pages", i32), ("partials", i32)]
 
 
+class RotaryC(_c.Structure):
+    _fields_ = [("dim", i32), ("layout", i32), ("scale", f32), ("turns", _c.c_double * ROTARY_MAX_PAIRS)]
+
+
 class LinearShape(_c.Structure):
     _fields_ = [("rows_large", i32), ("large_rows", i32), ("large_cols", i32), ("small_cols", i32), ("splits", i32),
                 ("scratch_counters", i32), ("scratch_floats", _c.c_int64)]
@@ -151,6 +158,14 @@ def lib():
         L.ftts_build_tables.argtypes = [vp, vp, i32, vp, i32, i32, vp, i32, vp, vp, vp, i32, vp, vp]
         L.ftts_append_kv.restype = _c.c_int
         L.ftts_append_kv.argtypes = [i32, i32, vp, i64, vp, i64, i32, vp, P(KvPool), i32, i32, vp]
+        f64 = _c.c_double
+        L.ftts_rotary_init.restype = _c.c_int
+        L.ftts_rotary_init.argtypes = [i32, i32, f64, i32, f64, f64, f64, f64, P(RotaryC)]
+        L.ftts_rotate.restype = _c.c_int
+        L.ftts_rotate.argtypes = [i32, i32, P(RotaryC), vp, i64, i32, i32, vp, vp, i64, vp]
+        L.ftts_append_rotated.restype = _c.c_int
+        L.ftts_append_rotated.argtypes = [i32, i32, P(RotaryC), vp, i64, i32, vp, i64, vp, i64, vp, i64, i32, vp, vp,
+                                          P(KvPool), i32, i32, vp]
         L.ftts_shared_attention_workspace_bytes.restype = _c.c_size_t
         L.ftts_shared_attention_workspace_bytes.argtypes = [P(AttnShape), i32, i32, i32, i32]
         L.ftts_shared_attention_plan.restype = _c.c_int
@@ -424,6 +439,63 @@ def append_kv(k, v, slots, kv, layer: int, stream=None):
         raise FTTSError(-1, f"the pool is on {kv.pool.device}, k is not")
     _enqueue(dev, stream, lib().ftts_append_kv, _wdtype("k", k.dtype), kv.dtype, *_rows("k", k, dev, shape),
              *_rows("v", v, dev, shape), shape[0], _int32("slots", slots, dev, shape[0]), _c.byref(kv.c), layer, heads)
+
+
+class Rotary:
+    """How the heads of a decoder turn with the position (ftts_rotary_init): `dim` leading columns of each head,
+    frequencies base^(-2 i / dim) radians a position, scaled for long contexts by `scaling`.  `scale` replaces the
+    factor of the turned columns."""
+
+    def __init__(self, dim: int = 64, layout: int = ROTARY_HALVES, base: float = 10000.0, scaling: int = ROTARY_PLAIN,
+                 factor: float = 1.0, original: float = 1024, slow: float = 1.0, fast: float = 32.0, scale=None):
+        self.c = RotaryC()
+        _check(lib().ftts_rotary_init(int(dim), int(layout), base, int(scaling), factor, original, slow, fast,
+                                      _c.byref(self.c)))
+        if scale is not None:
+            self.c.scale = scale
+        self.dim, self.layout = int(dim), int(layout)
+
+    @property
+    def turns(self):
+        """Turns a position of each pair."""
+        return list(self.c.turns)[:self.dim // 2]
+
+
+def rotate(x, rotary, positions, out, stream=None):
+    """ftts_rotate: rows x [T][n_head * 64] (rows may be strided) turned by their positions [T] into out, which may be
+    x itself."""
+    T, width = x.shape
+    dev = x.get_device()
+    if width % 64:
+        raise FTTSError(-2, "x must be [T][n_head * 64]")
+    _enqueue(dev, stream, lib().ftts_rotate, _wdtype("x", x.dtype), _wdtype("out", out.dtype), _c.byref(rotary.c),
+             *_rows("x", x, dev, (T, width)), T, width // 64, _int32("positions", positions, dev, T),
+             *_rows("out", out, dev, (T, width)))
+
+
+def append_rotated(k, v, rotary, positions, slots, kv, layer: int, q=None, q_out=None, stream=None):
+    """ftts_append_rotated: append_kv of keys turned by their positions [T], and queries q [T][n_head * 64] of the same
+    rows turned into q_out (the pool's dtype; may be q itself)."""
+    dev, layers, heads, T = k.get_device(), kv.pool.shape[0], kv.pool.shape[3], k.shape[0]
+    if (q is None) != (q_out is None):
+        raise FTTSError(-1, "q and q_out come together")
+    if k.dtype != v.dtype or (q is not None and q.dtype != k.dtype):
+        raise FTTSError(-3, "q, k and v must have one dtype")
+    if not 0 <= layer < layers:
+        raise FTTSError(-5, f"layer must be in [0, {layers})")
+    if kv.pool.get_device() != dev:
+        raise FTTSError(-1, f"the pool is on {kv.pool.device}, k is not")
+    queries = (None, 0, 0, None, 0)
+    if q is not None:
+        if q.dim() != 2 or q.shape[1] % 64:
+            raise FTTSError(-2, "q must be [T][n_head * 64]")
+        if q_out.dtype != kv.pool.dtype:
+            raise FTTSError(-3, "q_out must have the pool's dtype")
+        shape = (T, q.shape[1])
+        queries = (*_rows("q", q, dev, shape), shape[1] // 64, *_rows("q_out", q_out, dev, shape))
+    _enqueue(dev, stream, lib().ftts_append_rotated, _wdtype("k", k.dtype), kv.dtype, _c.byref(rotary.c), *queries,
+             *_rows("k", k, dev, (T, heads * 64)), *_rows("v", v, dev, (T, heads * 64)), T,
+             _int32("positions", positions, dev, T), _int32("slots", slots, dev, T), _c.byref(kv.c), layer, heads)
 
 
 class SharedPrefix:
