@@ -568,6 +568,45 @@ typedef struct {
 int ftts_shared_attention_plan(const ftts_attn_shape* shape, int32_t B, int32_t n_rows, int32_t prompts,
                                int32_t prefix_len, int32_t max_pages, ftts_shared_launch* out);
 
+/* ---- checking drafted trees -------------------------------------------------------------------
+ *
+ * A draft proposes several continuations of each sequence as a tree of tokens, and one pass of the
+ * model checks them all: the tree's rows are packed sequence after sequence (row_offsets), its first
+ * row is the token already chosen, every other one follows a parent before it.  Their keys and
+ * values are appended behind the sequence's cached tokens (ftts_build_tables, then ftts_append_kv or
+ * ftts_append_rotated), ftts_tree_attention lets each row see the cached tokens and its own
+ * ancestors, and once the model's choices are known (ftts_sample on every row's logits)
+ * ftts_tree_commit keeps the accepted path: its tokens' keys and values move together.
+ */
+#define FTTS_MAX_TREE 256 /* tokens of a tree */
+
+/* Bytes of device workspace for ftts_tree_attention over up to B sequences, n_rows rows, a prefix of
+ * prefix_len and max_pages pages a sequence (enough for every smaller call too).  Returns 0 for
+ * invalid arguments. */
+size_t ftts_tree_attention_workspace_bytes(const ftts_attn_shape* shape, int32_t B, int32_t n_rows,
+                                           int32_t prefix_len, int32_t max_pages);
+
+/*
+ * ftts_shared_attention for trees of drafted tokens: sequence b's n_b rows are the last n_b of its
+ * seq_lens[b] own tokens, whose keys and values are in its pages already; row i sees every token of
+ * the prefix, the own tokens before the tree, 0 .. seq_lens[b] - n_b - 1, and of the tree's tokens,
+ * seq_lens[b] - n_b + j, those whose bit j its mask has.
+ *   masks        [n_rows][mask_words] device words of 64 bits, 8-byte aligned: bit j % 64 of word
+ *                j / 64 is the tree's token j (a row's own bit among them: nothing is seen but by its
+ *                bit).  Bits from n_b on mean nothing, tokens from 64 * mask_words on are not seen.
+ *   mask_words   1 .. FTTS_MAX_TREE / 64.
+ *   row_offsets  [B + 1] device, as in ftts_shared_attention; not NULL.
+ * Everything else is as in ftts_shared_attention, but that a length below n_b (a negative one among
+ * them) makes its sequence inactive.  In bf16 the scores, sums and weights are held in fp32, the
+ * weights meet the values as two bf16 parts of each (within 2^-16 of it), and the output is rounded
+ * once.  Equal calls give equal bits.  `ws` holds intermediate results of the call only; calls that
+ * can run at the same time need one each.
+ */
+int ftts_tree_attention(const ftts_attn_shape* shape, const void* q, int64_t q_stride, const int32_t* row_offsets,
+                        int32_t n_rows, int32_t B, const int64_t* masks, int32_t mask_words,
+                        const ftts_shared_prefix* prefix, const ftts_page_table* pt, const ftts_kv_pool* kv,
+                        int32_t layer, void* out, int64_t out_stride, void* ws, size_t ws_bytes, void* stream);
+
 /* ---- the model behind a shared prefix --------------------------------------------------------
  *
  * One voice prompt, many sentences: the prompt's rows are prefilled once, as a sequence of its

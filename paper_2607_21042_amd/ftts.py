@@ -25,6 +25,7 @@ MAX_TOP_K = 64
 MAX_BATCH = 64
 MAX_TABLE_BATCH = 1024
 MAX_SHARED_PREFIX = 1 << 20
+MAX_TREE = 256
 SHARED_CUT, SHARED_WHOLE, SHARED_TILE, SHARED_PACKED = 0, 1, 2, 3
 ROTARY_HALVES, ROTARY_PAIRS = 0, 1
 ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_PARTS = 0, 1, 2, 3
@@ -173,6 +174,11 @@ def lib():
         L.ftts_shared_attention.restype = _c.c_int
         L.ftts_shared_attention.argtypes = [P(AttnShape), vp, i64, vp, i32, i32, P(SharedPrefixC), P(PageTable),
                                             P(KvPool), i32, vp, i64, vp, _c.c_size_t, vp]
+        L.ftts_tree_attention_workspace_bytes.restype = _c.c_size_t
+        L.ftts_tree_attention_workspace_bytes.argtypes = [P(AttnShape), i32, i32, i32, i32]
+        L.ftts_tree_attention.restype = _c.c_int
+        L.ftts_tree_attention.argtypes = [P(AttnShape), vp, i64, vp, i32, i32, vp, i32, P(SharedPrefixC), P(PageTable),
+                                          P(KvPool), i32, vp, i64, vp, _c.c_size_t, vp]
         L.ftts_shared_workspace_bytes.restype = _c.c_size_t
         L.ftts_shared_workspace_bytes.argtypes = [P(Config), i32, i32, i32, i32]
         L.ftts_prefill_shared.restype = _c.c_int
@@ -555,6 +561,61 @@ def shared_attention(q, kv, layer: int, page_table, prefix, out, ws, row_offsets
              _int32("row_offsets", row_offsets, dev, B + 1), T, B, None if prefix is None else _c.byref(prefix.c),
              _c.byref(page_table.c), _c.byref(kv.c), layer, *_rows("out", out, dev, (T, width)), _data("ws", ws, dev),
              ws.numel() * ws.element_size())
+
+
+def tree_masks(parents, words=None):
+    """The masks of one tree for tree_attention, [n][words] int64 on the host: each token's own bit and its ancestors',
+    from its tokens' parents (-1: none; a parent comes before its children)."""
+    parents = [int(p) for p in parents]
+    words = -(-len(parents) // 64) if words is None else words
+    if len(parents) > min(64 * words, MAX_TREE):
+        raise FTTSError(-2, f"a tree of {len(parents)} tokens does not fit {min(64 * words, MAX_TREE)}")
+    seen = []
+    for i, p in enumerate(parents):
+        if not -1 <= p < i:
+            raise FTTSError(-5, f"token {i}'s parent {p} does not come before it")
+        seen.append((seen[p] if p >= 0 else 0) | 1 << i)
+    words_of = [[m >> 64 * w & (1 << 64) - 1 for w in range(words)] for m in seen]
+    return torch.from_numpy(np.array(words_of, dtype=np.uint64).view(np.int64).reshape(len(parents), words))
+
+
+def tree_attention_workspace_bytes(n_head: int, n_kv_head: int, dtype: int, batch: int, rows: int, prefix_len: int,
+                                   max_pages: int) -> int:
+    """ftts_tree_attention_workspace_bytes (dtype F32 or BF16)."""
+    s = AttnShape(dtype, n_head, n_kv_head, 64)
+    n = lib().ftts_tree_attention_workspace_bytes(_c.byref(s), batch, rows, prefix_len, max_pages)
+    if n == 0:
+        raise FTTSError(-1, lib().ftts_last_error().decode())
+    return n
+
+
+def tree_attention(q, kv, layer: int, page_table, masks, row_offsets, out, ws, prefix=None, stream=None):
+    """ftts_tree_attention: rows q [T][n_head * 64] of the drafted trees of `page_table`'s sequences (row_offsets
+    [B + 1]; masks [T][words] int64), which all continue `prefix` (a SharedPrefix or None), to out [T][n_head * 64]."""
+    T, width = q.shape
+    B, dev, layers, heads = page_table.block_table.shape[0], q.get_device(), kv.pool.shape[0], kv.pool.shape[3]
+    if width % 64:
+        raise FTTSError(-2, "q must be [T][n_head * 64]")
+    if q.dtype != out.dtype or q.dtype != kv.pool.dtype:
+        raise FTTSError(-3, "q, out and the pool must have one dtype")
+    if masks.dtype != torch.int64:
+        raise FTTSError(-3, "masks must be int64")
+    if masks.dim() != 2 or masks.shape[0] != T:
+        raise FTTSError(-2, f"masks must be [{T}][words]")
+    if not 0 <= layer < layers:
+        raise FTTSError(-5, f"layer must be in [0, {layers})")
+    if page_table.seq_lens.numel() != B:
+        raise FTTSError(-2, f"the page table needs {B} lengths")
+    shared = [kv.pool, page_table.block_table, page_table.seq_lens]
+    if prefix is not None and prefix.len > 0:
+        shared.append(prefix.pages)
+    if any(t.get_device() != dev for t in shared):
+        raise FTTSError(-1, f"the pool, the page table and the prefix must be on {q.device}, as q is")
+    shape = AttnShape(_wdtype("q", q.dtype), width // 64, heads, 64)
+    _enqueue(dev, stream, lib().ftts_tree_attention, _c.byref(shape), *_rows("q", q, dev, (T, width)),
+             _int32("row_offsets", row_offsets, dev, B + 1), T, B, _data("masks", masks, dev), masks.shape[1],
+             None if prefix is None else _c.byref(prefix.c), _c.byref(page_table.c), _c.byref(kv.c), layer,
+             *_rows("out", out, dev, (T, width)), _data("ws", ws, dev), ws.numel() * ws.element_size())
 
 
 def shared_workspace_bytes(cfg: Config, max_batch: int, max_rows: int, prefix_len: int, max_pages: int) -> int:
