@@ -607,6 +607,34 @@ int ftts_tree_attention(const ftts_attn_shape* shape, const void* q, int64_t q_s
                         const ftts_shared_prefix* prefix, const ftts_page_table* pt, const ftts_kv_pool* kv,
                         int32_t layer, void* out, int64_t out_stride, void* ws, size_t ws_bytes, void* stream);
 
+/*
+ * Keeps the accepted path of each drafted tree.  From the tree's first token on, the path goes to the
+ * first child (parents[j] == the token's index, j above it) whose token is what the model chose at the
+ * token, choices (a negative choice matches nothing), and ends where no child is or with `max_path`
+ * tokens.  In every layer of the pool the keys and values of its i-th token, own token
+ * seq_lens[b] - n_b + path[i], move to own token seq_lens[b] - n_b + i; all other tokens stay as they
+ * were.
+ *   tokens, parents, choices  [n_rows] device, packed by row_offsets [B + 1] as the attention's rows:
+ *                drafted ids, indexes within the sequence's tree (-1: none; only tokens whose parents
+ *                lead back to its first one can be kept), and the model's choices behind each token
+ *                (ftts_sample over the rows' logits).
+ *   pt           block table and own lengths, the tree's n_b tokens among them.
+ *   kv, kv_dtype, n_layer, n_kv_head  the pool, all of whose layers are committed.
+ *   path         [B][max_path] out: indexes of the kept tokens, -1 behind them.
+ *   counts       [B] out: how many, at least 1.
+ *   next_tokens  [B] out: the choice behind the last kept token.
+ *   new_lens     [B] out: seq_lens - n_b + counts.
+ * A sequence without rows, or whose length is below n_b, keeps nothing: count 0, next token -1, its
+ * length as it was.  Only the first FTTS_MAX_TREE tokens of a tree count.  A token whose old or new
+ * page is outside the pool or the table is not moved.  Pages from the tree's first token on must be
+ * the sequence's own.  1 <= B <= FTTS_MAX_BATCH, n_rows <= 2^24, 1 <= max_path <= FTTS_MAX_TREE,
+ * n_layer * n_kv_head <= 2^16; no output may overlap an input or another output (FTTS_E_INVALID_ARG).
+ */
+int ftts_tree_commit(const int32_t* tokens, const int32_t* parents, const int32_t* choices,
+                     const int32_t* row_offsets, int32_t n_rows, int32_t B, const ftts_page_table* pt,
+                     const ftts_kv_pool* kv, int32_t kv_dtype, int32_t n_layer, int32_t n_kv_head, int32_t* path,
+                     int32_t max_path, int32_t* counts, int32_t* next_tokens, int32_t* new_lens, void* stream);
+
 /* ---- the model behind a shared prefix --------------------------------------------------------
  *
  * One voice prompt, many sentences: the prompt's rows are prefilled once, as a sequence of its

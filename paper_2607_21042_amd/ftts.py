@@ -179,6 +179,9 @@ def lib():
         L.ftts_tree_attention.restype = _c.c_int
         L.ftts_tree_attention.argtypes = [P(AttnShape), vp, i64, vp, i32, i32, vp, i32, P(SharedPrefixC), P(PageTable),
                                           P(KvPool), i32, vp, i64, vp, _c.c_size_t, vp]
+        L.ftts_tree_commit.restype = _c.c_int
+        L.ftts_tree_commit.argtypes = [vp, vp, vp, vp, i32, i32, P(PageTable), P(KvPool), i32, i32, i32, vp, i32, vp, vp,
+                                       vp, vp]
         L.ftts_shared_workspace_bytes.restype = _c.c_size_t
         L.ftts_shared_workspace_bytes.argtypes = [P(Config), i32, i32, i32, i32]
         L.ftts_prefill_shared.restype = _c.c_int
@@ -616,6 +619,23 @@ def tree_attention(q, kv, layer: int, page_table, masks, row_offsets, out, ws, p
              _int32("row_offsets", row_offsets, dev, B + 1), T, B, _data("masks", masks, dev), masks.shape[1],
              None if prefix is None else _c.byref(prefix.c), _c.byref(page_table.c), _c.byref(kv.c), layer,
              *_rows("out", out, dev, (T, width)), _data("ws", ws, dev), ws.numel() * ws.element_size())
+
+
+def tree_commit(tokens, parents, choices, row_offsets, page_table, kv, path, counts, next_tokens, new_lens, stream=None):
+    """ftts_tree_commit: the accepted path of each drafted tree (tokens, parents and the model's choices [T], packed by
+    row_offsets [B + 1]) into path [B][max_path], counts, next_tokens and new_lens [B]; its keys and values move together
+    in every layer of the pool."""
+    T, B, dev = tokens.numel(), page_table.block_table.shape[0], tokens.get_device()
+    if path.dim() != 2 or path.shape[0] != B:
+        raise FTTSError(-2, f"path must be [{B}][max_path]")
+    if page_table.seq_lens.numel() != B:
+        raise FTTSError(-2, f"the page table needs {B} lengths")
+    if any(t.get_device() != dev for t in (kv.pool, page_table.block_table, page_table.seq_lens)):
+        raise FTTSError(-1, f"the pool and the page table must be on {tokens.device}, as tokens are")
+    _enqueue(dev, stream, lib().ftts_tree_commit, _int32("tokens", tokens, dev), _int32("parents", parents, dev, T),
+             _int32("choices", choices, dev, T), _int32("row_offsets", row_offsets, dev, B + 1), T, B, _c.byref(page_table.c),
+             _c.byref(kv.c), kv.dtype, kv.pool.shape[0], kv.pool.shape[3], _int32("path", path, dev), path.shape[1],
+             _int32("counts", counts, dev, B), _int32("next_tokens", next_tokens, dev, B), _int32("new_lens", new_lens, dev, B))
 
 
 def shared_workspace_bytes(cfg: Config, max_batch: int, max_rows: int, prefix_len: int, max_pages: int) -> int:

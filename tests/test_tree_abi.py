@@ -81,3 +81,38 @@ def test_binding_refuses_before_the_library():
         with pytest.raises(ftts.FTTSError) as e:
             call(**bad)
         assert e.value.code == code, (bad, e.value)
+
+
+I = torch.int32
+
+
+def commit(tokens=FAKE, parents=FAKE * 2, choices=FAKE * 3, cu=FAKE * 4, rows=40, B=4, table=FAKE * 5, lens=FAKE * 6, width=8, base=FAKE * 64,
+           pages=9, dtype=1, layers=24, kvh=20, path=FAKE * 7, most=8, counts=FAKE * 8, nxt=FAKE * 9, new=FAKE * 10, pt=True):
+    t, kv = ftts.PageTable(table, lens, width), ftts.KvPool(base, pages)
+    return L.ftts_tree_commit(tokens, parents, choices, cu, rows, B, ctypes.byref(t) if pt else None, ctypes.byref(kv), dtype, layers, kvh,
+                              path, most, counts, nxt, new, None)
+
+
+@pytest.mark.parametrize("bad,code", [
+    (dict(dtype=2), -3), (dict(pt=False), -1), (dict(table=None), -1), (dict(lens=None), -1), (dict(base=None), -1), (dict(B=0), -2),
+    (dict(B=65), -2), (dict(rows=-1), -5), (dict(rows=(1 << 24) + 1), -5), (dict(width=0), -2), (dict(width=513), -2), (dict(pages=0), -2),
+    (dict(layers=0), -2), (dict(kvh=0), -2), (dict(kvh=257), -2), (dict(layers=1 << 20, kvh=1), -2), (dict(most=0), -2), (dict(most=257), -2),
+    (dict(tokens=None), -1), (dict(parents=None), -1), (dict(choices=None), -1), (dict(cu=None), -1), (dict(path=None), -1),
+    (dict(counts=None), -1), (dict(nxt=None), -1), (dict(new=None), -1), (dict(base=FAKE * 64 + 8), -4), (dict(path=FAKE * 7 + 1), -4),
+    (dict(tokens=FAKE + 2), -4), (dict(new=FAKE * 6), -1), (dict(path=FAKE * 3 + 16), -1), (dict(counts=FAKE * 9 - 8), -1),
+    (dict(nxt=FAKE * 64 + 64), -1), (dict(lens=FAKE * 64 + 4096), -1), (dict(counts=FAKE * 5 + 64), -1)])
+def test_commit_refused(bad, code):
+    assert commit(**bad) == code, L.ftts_last_error()
+
+
+def test_commit_binding_refuses_before_the_library():
+    def call(tokens=5, parents=5, choices=5, cu=3, path=(2, 4), counts=2, lens=2, dtype=I):
+        pool = type("kv", (), {"pool": torch.zeros((1, 2, 2, 2, 64, 64), dtype=torch.bfloat16), "dtype": ftts.BF16, "c": ftts.KvPool()})
+        pt = type("pt", (), {"block_table": torch.zeros((2, 2), dtype=I), "seq_lens": torch.zeros(lens, dtype=I), "c": ftts.PageTable()})
+        z = lambda n: torch.zeros(n, dtype=I)  # noqa: E731
+        ftts.tree_commit(torch.zeros(tokens, dtype=dtype), z(parents), z(choices), z(cu), pt, pool, z(path), z(counts), z(2), z(2))
+    for bad, code in ((dict(dtype=torch.int64), -3), (dict(parents=4), -2), (dict(choices=6), -2), (dict(cu=2), -2), (dict(path=(3, 4)), -2),
+                      (dict(path=(8,)), -2), (dict(counts=3), -2), (dict(lens=3), -2), ({}, -1)):
+        with pytest.raises(ftts.FTTSError) as e:
+            call(**bad)
+        assert e.value.code == code, (bad, e.value)
