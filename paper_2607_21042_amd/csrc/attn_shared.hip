@@ -1369,6 +1369,17 @@ size_t shared_attention_bytes(int n_head, int rows, int prefix_len, int max_page
     return (size_t)n * (kHeadDim + 2) * 4 + 256;
 }
 
+hipError_t launch_attn_join(bool f32, const SharedAttnArgs& a, int slots, float2* ml, float* o, hipStream_t st) {
+    SharedPlan p{};
+    p.s_pre = slots;
+    p.ml = ml;
+    p.o = o;
+    const dim3 g((unsigned)(((int64_t)a.rows * a.n_head + kJoinWaves - 1) / kJoinWaves)), t(kJoinWaves * 64);
+    if (f32) hipLaunchKernelGGL(shared_join_kernel<true>, g, t, 0, st, a, p);
+    else hipLaunchKernelGGL(shared_join_kernel<false>, g, t, 0, st, a, p);
+    return hipGetLastError();
+}
+
 // How a call runs (ftts_shared_attention_plan hands it out).
 struct SharedChoice {
     int kernel, slots;  // FTTS_SHARED_*; partials a row

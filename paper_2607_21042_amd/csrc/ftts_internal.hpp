@@ -337,6 +337,10 @@ struct SharedAttnArgs {
     bool q_f32, o_f32;            // (16-bit pool; an fp32 pool has both in fp32)
 };
 hipError_t launch_shared_attention(int dtype, const SharedAttnArgs& a, void* ws, size_t ws_bytes, hipStream_t st);
+// Joins `slots` partial results a row and head into a.o: (maximum, sum) of slot s at ml + s * rows * n_head, a sum of 0
+// where a slot saw nothing (and left nothing in o); outputs so far at o + s * rows * n_head * 64.  Of `a`: o, o_ld, n_head,
+// rows, row_offsets, B.
+hipError_t launch_attn_join(bool f32, const SharedAttnArgs& a, int slots, float2* ml, float* o, hipStream_t st);
 // Bytes of ws, for up to so many rows, prefix tokens and pages a sequence.
 size_t shared_attention_bytes(int n_head, int rows, int prefix_len, int max_pages);
 
