@@ -353,7 +353,7 @@ __global__ __launch_bounds__(W * 64, W == 4 ? 3 : 4) void tree_tile_kernel(const
     if (n > 0) fetch(0);
     uint4 qr[4];
     at_load_q(reinterpret_cast<const uint16_t*>(a.q) + (size_t)row * a.q_ld + head * kHeadDim, hh, qr);
-    const TreeMask mask = tree_mask(a, row, hh);
+    TreeMask mask = tree_mask(a, row, hh);
     auto load = [&](int i, int kv) {  // the wave's i-th half, K (kv 0) or V; zeros for what is not there
         const int tokens = __builtin_amdgcn_readlane(page.tokens, i & 63);
         const char* src = page_at(a, page, i & 63) + kv * to_v + (wave & 1) * kThTile;
@@ -431,6 +431,9 @@ __global__ __launch_bounds__(W * 64, W == 4 ? 3 : 4) void tree_tile_kernel(const
         th_pv(st, v, pw);
         th_pv(st, v, plo);
     };
+    // (queries and masks are waited for here: the compiler would wait for them in the loop, and so for the next half's loads)
+    at_tie4(qr);
+    asm volatile("" : "+v"(mask.even), "+v"(mask.odd));
     // halves that end before the tree are seen whole: the wave's first ones, of the run's 2 (n_pre - j0) + past / 32
     const int before = 2 * (w.n_pre - w.j0) + (w.past < 0 ? 0 : w.past / kThK), whole = min(max(before - wave + W - 1, 0) / W, n);
     for (int i = 0; i < whole; ++i) step(std::false_type{}, i);
@@ -502,24 +505,26 @@ __global__ __launch_bounds__(kTreeWaves * 64) void tree_row_kernel(const TreeArg
 
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Parts pay for a second launch and a row's partials, 8 waves a workgroup for fewer workgroups at once.  A part's chain of
-// pages costs 0.33 us a page with 4 waves and 0.30 with 8 while 610 (360) workgroups run, and that many times more where
-// there are more.  Fitted to 1,501 calls of 1 to 64 sequences, trees of 1 to 256, 20/20, 20/4, 12/12, 12/2, 32/16, 8/1 and
-// 4/4 heads, up to 16,000 own tokens behind up to 5000, each run with 4 and 8 waves in 1 to 48 parts: the choice costs
-// 1.8% of a call on average (always 4 waves and one part: 50%, always 8: 31%).  Own lengths are on the device, so the
-// table's width stands for them.
+// Parts pay for a second launch and a row's partials, 8 waves a workgroup for fewer workgroups at once and a longer hand-
+// over.  A part's chain of pages costs 0.40 us a page with 4 waves and 0.205 with 8 while 610 (280) workgroups run; where
+// there are more, so many times that and half a part that is begun late.  Fitted to 1,338 calls of 1 to 64 sequences, trees
+// of 1 to 256, 20/20, 20/4, 12/12, 12/2, 32/16, 8/1 and 4/4 heads, up to 16,000 own tokens behind up to 5000, each run with
+// 4 and 8 waves in 1 to 48 parts: the choice costs 1.4% of a call on average (always 4 waves and one part 35%, 8 waves
+// 28%).  Own lengths are on the device, so the table's width stands for them.
 constexpr int kTreeMaxParts = 48, kTreeMaxSlots = 1 << 18;  // partials of a call: 69 MB at most
 static TreePlan tree_plan(const TreeArgs& a, int& waves) {
-    const double g = a.n_head / a.n_kv_head, units = a.n_kv_head * (a.rows * g / 32 + a.B), row_heads = (double)a.rows * a.n_head;
+    const double g = a.n_head / a.n_kv_head, units = a.n_kv_head * (a.rows * g / 32 + 0.67 * a.B), row_heads = (double)a.rows * a.n_head;
     const int64_t pages = ceil_div(a.prefix_len, kPage) + a.max_pages;
+    const double chain = ceil_div(a.prefix_len, kPage) + 0.86 * a.max_pages;
     TreePlan p{};
     double least = 1e30;
     for (const int n : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, kTreeMaxParts}) {
         if (n > 1 && (2 * n > pages || n * row_heads > kTreeMaxSlots)) break;
         const int per = (int)ceil_div(pages, n), parts = (int)ceil_div(pages, per);
         for (const int w : {4, 8}) {
-            const double t = (w == 4 ? 0.33 : 0.30) * pages / parts * std::max(1.0, units * parts / (w == 4 ? 610 : 360)) +
-                             (parts > 1 ? 3.7 + 0.17e-3 * parts * row_heads : 0) + 3.6e-3 * units * parts;
+            const double full = units * parts / (w == 4 ? 610 : 280);
+            const double t = (w == 4 ? 0.0 : 1.5) + (w == 4 ? 0.40 : 0.205) * chain / parts * (full > 1 ? full + 0.48 : 1.0) +
+                             (parts > 1 ? 2.5 + 0.096e-3 * parts * row_heads : 0) + 5.5e-3 * units * parts;
             if (t >= least) continue;
             least = t;
             p.per = per;
@@ -538,7 +543,7 @@ static size_t tree_attention_bytes(int n_head, int rows) {
     return (size_t)std::min<int64_t>((int64_t)rows * n_head * kTreeMaxParts, kTreeMaxSlots) * (kHeadDim + 2) * 4 + 256;
 }
 
-static hipError_t launch_tree_attention(int dtype, const TreeArgs& a, void* ws, hipStream_t st) {
+static hipError_t launch_tree_attention(int dtype, const TreeArgs& a, void* ws, size_t ws_bytes, hipStream_t st) {
     (void)hipGetLastError();
     if (dtype == FTTS_F32) {
         const dim3 g((unsigned)(((int64_t)a.rows * a.n_head + kTreeWaves - 1) / kTreeWaves)), t(kTreeWaves * 64);
@@ -547,7 +552,8 @@ static hipError_t launch_tree_attention(int dtype, const TreeArgs& a, void* ws, 
     }
     int waves = 4;
     TreePlan p = tree_plan(a, waves);
-    const int64_t slots = (int64_t)p.parts * a.rows * a.n_head;
+    const int64_t slots = p.parts > 1 ? (int64_t)p.parts * a.rows * a.n_head : 0;
+    if ((size_t)slots * (kHeadDim + 2) * 4 > ws_bytes) return hipErrorInvalidValue;
     p.o = reinterpret_cast<float*>(ws);
     p.ml = reinterpret_cast<float2*>(p.o + slots * kHeadDim);
     const dim3 wg((unsigned)(p.tiles * a.n_kv_head * p.parts)), wt(waves * 64);
@@ -645,7 +651,7 @@ int ftts_tree_attention(const ftts_attn_shape* shape, const void* q, int64_t q_s
     a.prefix_len = P;
     a.B = B;
     a.rows = n_rows;
-    const hipError_t e = launch_tree_attention(shape->dtype, a, ws, (hipStream_t)stream);
+    const hipError_t e = launch_tree_attention(shape->dtype, a, ws, ws_bytes, (hipStream_t)stream);
     if (e != hipSuccess) return set_error(FTTS_E_HIP, "tree_attention launch: %s", hipGetErrorString(e));
     return FTTS_OK;
 }
