@@ -185,4 +185,35 @@ __device__ __forceinline__ void sa_take_out(uint64_t (&v)[2][2][4]) {
             }
 }
 
+// fp32: halves of a page, 32 tokens, as the first operand of products of 32x32x2.  A 16-byte piece c of row r lies at
+// c ^ (r % 16).  K: lane (key, hh) holds dims 32 hh .. + 31, one a step (kr: its 16-byte pieces).
+constexpr int kSfK = 32;
+__device__ __forceinline__ void sf_read_k(const uint32_t (&kr)[8], float4 (&k)[8]) {
+    at_bf16x8 x[8];  // (any 16-byte register type)
+    asm volatile(
+        "ds_read_b128 %0, %8\n\tds_read_b128 %1, %9\n\tds_read_b128 %2, %10\n\tds_read_b128 %3, %11\n\t"
+        "ds_read_b128 %4, %12\n\tds_read_b128 %5, %13\n\tds_read_b128 %6, %14\n\tds_read_b128 %7, %15\n\ts_waitcnt lgkmcnt(0)"
+        : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7])
+        : "v"(kr[0]), "v"(kr[1]), "v"(kr[2]), "v"(kr[3]), "v"(kr[4]), "v"(kr[5]), "v"(kr[6]), "v"(kr[7])
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 8; ++i) k[i] = __builtin_bit_cast(float4, x[i]);
+}
+// v[i] = value of key (i/4)*8 + hh*4 + i%4 in dim lane % 32 (+ 32: the addresses of the other half of a row).
+__device__ __forceinline__ void sf_read_v(const uint32_t (&a)[8], int flip, float (&v)[16]) {
+#define SF_R(O, A, OFF) "ds_read_b32 %" #O ", %" #A " offset:" #OFF "\n\t"
+    asm volatile(
+        SF_R(0, 16, 0) SF_R(1, 17, 256) SF_R(2, 18, 512) SF_R(3, 19, 768)
+        SF_R(4, 20, 2048) SF_R(5, 21, 2304) SF_R(6, 22, 2560) SF_R(7, 23, 2816)
+        SF_R(8, 16, 4096) SF_R(9, 17, 4352) SF_R(10, 18, 4608) SF_R(11, 19, 4864)
+        SF_R(12, 20, 6144) SF_R(13, 21, 6400) SF_R(14, 22, 6656) SF_R(15, 23, 6912)
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]), "=&v"(v[4]), "=&v"(v[5]), "=&v"(v[6]), "=&v"(v[7]),
+          "=&v"(v[8]), "=&v"(v[9]), "=&v"(v[10]), "=&v"(v[11]), "=&v"(v[12]), "=&v"(v[13]), "=&v"(v[14]), "=&v"(v[15])
+        : "v"(a[0 ^ flip]), "v"(a[1 ^ flip]), "v"(a[2 ^ flip]), "v"(a[3 ^ flip]), "v"(a[4 ^ flip]), "v"(a[5 ^ flip]),
+          "v"(a[6 ^ flip]), "v"(a[7 ^ flip])
+        : "memory");
+#undef SF_R
+}
+
 }  // namespace ftts

@@ -4,7 +4,9 @@
 // 0 .. L_b - n_b - 1, and the tree's tokens whose bits its mask has:  o = sum_j p_j v_j / sum_j p_j,
 // p_j = exp(q . k_j / 8 - m).
 //
-// A wave a row and head: lane t scores token t of a page, then sums dim t over the page's tokens that are seen.
+// A workgroup takes a tile of 32 (row, query head) pairs of one sequence that read one key head, and a run of the pages
+// that the sequence sees, cut into parts where the calls' tiles are few and the pages many; the shared-prefix attention's
+// second kernel joins the parts.  Its waves take the run's half pages in turn and join their sums through LDS.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -29,18 +31,6 @@ struct TreeArgs {
     int prefix_len;
     int B, rows;
 };
-
-// The tree's tokens j0 .. j0 + 63 that a row sees, of n: bits of its mask (j0 may be negative: tokens before the tree,
-// all of them seen).
-__device__ __forceinline__ uint64_t tree_bits(const uint64_t* mask, int words, int j0, int n) {
-    if (j0 <= -kPage) return ~0ull;
-    auto word = [&](int w) { return w >= 0 && w < words ? mask[w] : 0ull; };
-    const int w = j0 >> 6, s = j0 & 63;  // (a floor)
-    uint64_t bits = word(w) >> s | (s ? word(w + 1) << (64 - s) : 0);
-    if (j0 < 0) bits |= (1ull << -j0) - 1;
-    const int left = n - j0;
-    return left >= 64 ? bits : left <= 0 ? 0 : bits & ((1ull << left) - 1);
-}
 
 // The bits of tokens 0 .. n - 1.
 __device__ __forceinline__ uint64_t low_bits(int n) { return n >= 64 ? ~0ull : (1ull << max(n, 0)) - 1; }
@@ -454,82 +444,218 @@ __global__ __launch_bounds__(W * 64, W == 4 ? 3 : 4) void tree_tile_kernel(const
     tree_finish<false, W>(a, pl, w, st, idx < pairs ? row : -1, head, smem, wave, lane);
 }
 
-constexpr int kTreeWaves = 4;
-template <bool F32>
-__global__ __launch_bounds__(kTreeWaves * 64) void tree_row_kernel(const TreeArgs a) {
-    const int lane = threadIdx.x & 63;
-    const int64_t id = (int64_t)blockIdx.x * kTreeWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int row = (int)(id / a.n_head), head = (int)(id % a.n_head), kh = head / (a.n_head / a.n_kv_head);
-    if (row >= a.rows) return;
-    const int lo = lane < a.B ? a.row_offsets[lane] : 0, hi = lane < a.B ? a.row_offsets[lane + 1] : 0;
-    const int first = min(max(lo, 0), a.rows), n_of = min(max(hi, first), a.rows) - first;
-    const unsigned long long whose = __ballot(lane < a.B && row >= first && row < first + n_of);
-    if (!whose) return;
-    const int b = __builtin_ctzll(whose), n = __builtin_amdgcn_readlane(n_of, b), past = a.seq_lens[b] - n;
-    const int own = past < 0 ? 0 : (int)min((int64_t)past + n, (int64_t)a.max_pages * kPage);
-    const int n_pre = past < 0 ? 0 : (a.prefix_len + kPage - 1) / kPage, pages = n_pre + (own + kPage - 1) / kPage;
-    float q[kHeadDim];
+// fp32: the same with fp32 matrix products, all sums in fp32.  Bound by the products: 4096 cycles a wave and half of a
+// page, whatever the rows.
+constexpr int kTfTile = kSfK * kHeadDim * 4, kTfStage = 2 * kTfTile;
+// As th_add_not_finite; v0, v1: values of the keys that element i is for, in dims lane % 32 and 32 + lane % 32.
+__device__ __forceinline__ void tf_add_not_finite(SaState& a, const float (&v0)[16], const float (&v1)[16], uint32_t seen, int hh) {
+    const uint32_t x = seen >> (4 * hh);
 #pragma unroll
-    for (int d = 0; d < kHeadDim; ++d) q[d] = ld_act<F32>(a.q, (size_t)row * a.q_ld + head * kHeadDim + d);
-    float m = -INFINITY, l = 0.f, o = 0.f;
-    bool saw = false;
-    for (int j = 0; j < pages; ++j) {
-        const int k = j - n_pre, phys = k < 0 ? a.prefix_pages[j] : a.block_table[(size_t)b * a.max_pages + k];
-        if (phys < 0 || phys >= a.n_pages) continue;
-        const int tokens = min(k < 0 ? a.prefix_len - j * kPage : own - k * kPage, kPage);
-        uint64_t seen = tokens == kPage ? ~0ull : (1ull << tokens) - 1;
-        if (k >= 0) seen &= tree_bits(a.masks + (size_t)row * a.mask_words, a.mask_words, k * kPage - past, n);
-        if (!seen) continue;
-        saw = true;
-        const size_t key = kv_offset(a.layer, a.n_pages, phys, 0, a.n_kv_head, kh, 0), val = key + (size_t)a.n_kv_head * kPage * kHeadDim;
-        float s = -INFINITY;
-        if (seen >> lane & 1) {
-            s = 0.f;
+    for (int d = 0; d < 2; ++d)
 #pragma unroll
-            for (int d = 0; d < kHeadDim; ++d) s = fmaf(q[d], ld_act<F32>(a.kv_base, key + lane * kHeadDim + d), s);
-            s *= 0.125f;
+        for (int sign = 0; sign < 2; ++sign) {
+            at_f32x16 n;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) n[i] = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float v = d ? v1[i] : v0[i], of = fabsf(v) < INFINITY || v == (sign ? INFINITY : -INFINITY) ? 0.f : 1.f;
+                n = __builtin_amdgcn_mfma_f32_32x32x2f32(of, x >> ((i >> 2) * 8 + (i & 3)) & 1 ? 1.f : 0.f, n, 0, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) (d ? a.o1 : a.o0)[i] += n[i] > 0.f ? (sign ? -INFINITY : INFINITY) : 0.f;
+            __builtin_amdgcn_sched_barrier(0);  // (one after the other)
         }
-        const float mn = fmaxf(m, wave_max(s)), ref = mn == -INFINITY ? 0.f : mn, keep = expf(m - ref);
-        const float p = seen >> lane & 1 ? expf(s - ref) : 0.f;
-        m = mn;
-        l = l * keep + wave_sum(p);
-        o *= keep;
-        for (uint64_t x = seen; x; x &= x - 1) {
-            const int t = __builtin_ctzll(x);
-            o = fmaf(__shfl(p, t, kWave), ld_act<F32>(a.kv_base, val + t * kHeadDim + lane), o);
+}
+template <int W>
+__global__ __launch_bounds__(W * 64, 2) void tree_tile_f32_kernel(const TreeArgs a, const TreePlan pl) {
+    __shared__ __attribute__((aligned(1024))) char smem[W * kTfStage];  // the stages, then the waves' results
+    static_assert(kTfStage >= 34 * 256, "");
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ql = lane & 31, hh = lane >> 5;
+    TreeWork w;
+    if (!tree_work(a, pl, 32, lane, w)) return;
+    const int g = a.n_head / a.n_kv_head, pairs = w.n * g, idx = w.first + ql, last = min(idx, pairs - 1);
+    const int row = w.row0 + last / g, head = w.kh * g + last % g;  // this lane's pair, the tile's last one where it is past it
+    char* own = smem + wave * kTfStage;
+    const int halves = 2 * w.pages, n = halves > wave ? (halves - wave + W - 1) / W : 0;  // this wave's halves
+    const size_t to_v = (size_t)a.n_kv_head * (kPage * kHeadDim * 4);  // from a page's keys to its values
+    PageRef page{};
+    auto fetch = [&](int i0) {  // the wave's halves i0 .. i0 + 63, one a lane
+        const int i = i0 + lane, u = wave + W * i, j = w.j0 + (u >> 1), k = j - w.n_pre;
+        const int id = i >= n ? -1 : k < 0 ? a.prefix_pages[j] : a.block_table[(size_t)w.b * a.max_pages + k];
+        page = page_ref(a, w.kh, 4, id, i >= n ? 0 : k < 0 ? a.prefix_len - j * kPage : w.own - k * kPage);
+        page.tokens = min(max(page.tokens - (u & 1) * kSfK, 0), kSfK);
+    };
+    if (n > 0) fetch(0);
+    float4 q[8];
+    {
+        const float* qp = reinterpret_cast<const float*>(a.q) + (size_t)row * a.q_ld + head * kHeadDim + hh * 32;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = *reinterpret_cast<const float4*>(qp + 4 * i);
+    }
+    TreeMask mask = tree_mask(a, row, hh);
+    static_assert(W % 2 == 0, "a wave's halves are all first or all second ones");
+    auto load = [&](int i, int kv) {  // the wave's i-th half, K (kv 0) or V; zeros for what is not there
+        const int tokens = __builtin_amdgcn_readlane(page.tokens, i & 63);
+        const char* src = page_at(a, page, i & 63) + kv * to_v + (wave & 1) * kTfTile;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int r = k * 4 + (lane >> 4);
+            buffer_to_lds16(src, tokens * 256, own + kv * kTfTile + k * 1024, r * 256 + (((lane & 15) ^ (r & 15)) << 4), 0);
+        }
+        return tokens;
+    };
+    uint32_t kr[8], vr[8];
+    {
+        const uint32_t s0 = lds_address(own);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            kr[c] = s0 + ql * 256 + (((hh * 8 + c) ^ (ql & 15)) << 4);
+            // c = 4 (i / 4 % 2) + i % 4 for element i
+            vr[c] = s0 + kTfTile + hh * 1024 + (((ql >> 2) ^ ((c >> 2) * 8 + hh * 4 + (c & 3))) << 4) + (ql & 3) * 4;
         }
     }
-    // where nothing is seen 0, where every score is -inf NaN
-    st_act<F32>(a.o, (size_t)row * a.o_ld + head * kHeadDim + lane, saw ? o / l : 0.f);
+    SaState st;
+    sa_init(st);
+    bool saw = false, odd = false;  // a token; a value that is not finite where rows see different tokens
+    int next = 0;
+    if (n > 0) {
+        next = load(0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        load(0, 1);
+    }
+    auto tree0 = [&](int i) { return (w.j0 + ((wave + W * i) >> 1) - w.n_pre) * kPage + (wave & 1) * kSfK - w.past; };
+    auto step = [&](auto of_tree, int i) {  // half i; of_tree: rows may see different tokens of it
+        constexpr bool TREE = decltype(of_tree)::value;
+        const bool more = i + 1 < n;
+        const int tokens = next;
+        asm volatile("s_waitcnt vmcnt(8)" ::: "memory");  // K is in (this wave's own loads), V's 8 loads may be out
+        __builtin_amdgcn_sched_barrier(0);
+        float4 k[8];
+        sf_read_k(kr, k);
+        __builtin_amdgcn_sched_barrier(0);
+        if (more) {
+            if (((i + 1) & 63) == 0) fetch(i + 1);
+            next = load(i + 1, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        at_f32x16 s[1];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[0][e] = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            s[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e].x, q[e].x, s[0], 0, 0, 0);
+            s[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e].y, q[e].y, s[0], 0, 0, 0);
+            s[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e].z, q[e].z, s[0], 0, 0, 0);
+            s[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e].w, q[e].w, s[0], 0, 0, 0);
+        }
+        uint32_t seen = 0;
+        if constexpr (TREE) {
+            seen = tree_seen(mask, tree0(i), tokens, lane);
+            th_hide(s[0], seen, hh);
+            saw |= seen != 0;
+        } else {
+            if (tokens < kSfK) th_hide(s[0], (uint32_t)low_bits(tokens), hh);
+            saw |= tokens > 0;
+        }
+        sa_maximum(st, s);
+        const float ref = st.m == -INFINITY ? 0.f : st.m;  // nothing seen: every score is -inf and every weight 0
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            s[0][e] = __builtin_amdgcn_exp2f(fmaf(s[0][e], kSaScale, -ref));
+            st.l += s[0][e];
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (more) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");  // V is in, the next K may be out
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        float v0[16], v1[16];
+        sf_read_v(vr, 0, v0);
+        sf_read_v(vr, 4, v1);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (TREE) {
+            float z = 0.f;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) z = fmaf(v0[e], 0.f, fmaf(v1[e], 0.f, z));
+            if (__any(seen != (uint32_t)low_bits(tokens)) && __any(z != 0.f)) {  // (NaN)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    v0[e] = fabsf(v0[e]) < INFINITY ? v0[e] : 0.f;
+                    v1[e] = fabsf(v1[e]) < INFINITY ? v1[e] : 0.f;
+                }
+                odd = true;
+            }
+        }
+        if (more) load(i + 1, 1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            st.o0 = __builtin_amdgcn_mfma_f32_32x32x2f32(v0[e], s[0][e], st.o0, 0, 0, 0);
+            st.o1 = __builtin_amdgcn_mfma_f32_32x32x2f32(v1[e], s[0][e], st.o1, 0, 0, 0);
+        }
+    };
+    // (as in tree_tile_kernel)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) asm volatile("" : "+v"(q[i].x), "+v"(q[i].y), "+v"(q[i].z), "+v"(q[i].w));
+    asm volatile("" : "+v"(mask.even), "+v"(mask.odd));
+    const int before = 2 * (w.n_pre - w.j0) + (w.past < 0 ? 0 : w.past / kSfK), whole = min(max(before - wave + W - 1, 0) / W, n);
+    for (int i = 0; i < whole; ++i) step(std::false_type{}, i);
+    for (int i = whole; i < n; ++i) step(std::true_type{}, i);
+    if (odd)
+#pragma unroll 1
+        for (int i = whole; i < n; ++i) {
+            fetch(i);  // (to lane 0)
+            const int tokens = __builtin_amdgcn_readlane(page.tokens, 0);
+            load(0, 1);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            float v0[16], v1[16];
+            sf_read_v(vr, 0, v0);
+            sf_read_v(vr, 4, v1);
+            tf_add_not_finite(st, v0, v1, tree_seen(mask, tree0(i), tokens, lane), hh);
+        }
+    st.m = sa_marked(st.m, saw);
+    __syncthreads();
+    tree_finish<true, W>(a, pl, w, st, idx < pairs ? row : -1, head, smem, wave, lane);
 }
 
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Parts pay for a second launch and a row's partials, 8 waves a workgroup for fewer workgroups at once and a longer hand-
-// over.  A part's chain of pages costs 0.40 us a page with 4 waves and 0.205 with 8 while 610 (280) workgroups run; where
-// there are more, so many times that and half a part that is begun late.  Fitted to 1,338 calls of 1 to 64 sequences, trees
-// of 1 to 256, 20/20, 20/4, 12/12, 12/2, 32/16, 8/1 and 4/4 heads, up to 16,000 own tokens behind up to 5000, each run with
-// 4 and 8 waves in 1 to 48 parts: the choice costs 1.4% of a call on average (always 4 waves and one part 35%, 8 waves
-// 28%).  Own lengths are on the device, so the table's width stands for them.
+// over.  In bf16 a part's chain of pages costs 0.40 us a page with 4 waves and 0.205 with 8 while 610 (280) workgroups run;
+// where there are more, so many times that and half a part that is begun late.  Fitted to 1,338 calls (fp32: 1,229) of 1 to
+// 64 sequences, trees of 1 to 256, 20/20, 20/4, 12/12, 12/2, 32/16, 8/1 and 4/4 heads, up to 16,000 own tokens behind up to
+// 5000 (2000 and 1000), each run with 4 and 8 waves in 1 to 48 parts: the choice costs 1.4% (2.0%) of a call on average,
+// always 4 waves and one part 35% (47%), 8 waves 28% (47%).  Own lengths are on the device, so the table's width stands
+// for them.
 constexpr int kTreeMaxParts = 48, kTreeMaxSlots = 1 << 18;  // partials of a call: 69 MB at most
-static TreePlan tree_plan(const TreeArgs& a, int& waves) {
-    const double g = a.n_head / a.n_kv_head, units = a.n_kv_head * (a.rows * g / 32 + 0.67 * a.B), row_heads = (double)a.rows * a.n_head;
+struct TreeCost {
+    double begun, own;       // of a sequence's tiles the one that is begun, of the table's width what is filled
+    double room[2], page[2]; // workgroups at once, us a page of the chain: 4 waves, 8 waves
+    double eight, late;      // us for 8 waves; of a part that is begun late
+    double join, partial;    // us for the second launch, and a partial
+    double group;            // us a workgroup
+};
+static TreePlan tree_plan(const TreeArgs& a, bool f32, int& waves) {
+    static constexpr TreeCost kCost[2] = {{0.67, 0.86, {610, 280}, {0.40, 0.205}, 1.5, 0.48, 2.5, 0.096e-3, 5.5e-3},
+                                          {0.92, 1.61, {274, 213}, {0.61, 0.47}, 1.6, 0.34, 1.9, 0.19e-3, 1.9e-3}};
+    const TreeCost& c = kCost[f32];
+    const double g = a.n_head / a.n_kv_head, units = a.n_kv_head * (a.rows * g / 32 + c.begun * a.B), row_heads = (double)a.rows * a.n_head;
     const int64_t pages = ceil_div(a.prefix_len, kPage) + a.max_pages;
-    const double chain = ceil_div(a.prefix_len, kPage) + 0.86 * a.max_pages;
+    const double chain = ceil_div(a.prefix_len, kPage) + c.own * a.max_pages;
     TreePlan p{};
     double least = 1e30;
     for (const int n : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, kTreeMaxParts}) {
         if (n > 1 && (2 * n > pages || n * row_heads > kTreeMaxSlots)) break;
         const int per = (int)ceil_div(pages, n), parts = (int)ceil_div(pages, per);
-        for (const int w : {4, 8}) {
-            const double full = units * parts / (w == 4 ? 610 : 280);
-            const double t = (w == 4 ? 0.0 : 1.5) + (w == 4 ? 0.40 : 0.205) * chain / parts * (full > 1 ? full + 0.48 : 1.0) +
-                             (parts > 1 ? 2.5 + 0.096e-3 * parts * row_heads : 0) + 5.5e-3 * units * parts;
+        for (const int e : {0, 1}) {
+            const double full = units * parts / c.room[e];
+            const double t = e * c.eight + c.page[e] * chain / parts * (full > 1 ? full + c.late : 1.0) +
+                             (parts > 1 ? c.join + c.partial * parts * row_heads : 0) + c.group * units * parts;
             if (t >= least) continue;
             least = t;
             p.per = per;
             p.parts = parts;
-            waves = w;
+            waves = e ? 8 : 4;
         }
     }
     p.tiles = (int)((int64_t)a.rows * (a.n_head / a.n_kv_head) / 32) + a.B;
@@ -544,20 +670,18 @@ static size_t tree_attention_bytes(int n_head, int rows) {
 }
 
 static hipError_t launch_tree_attention(int dtype, const TreeArgs& a, void* ws, size_t ws_bytes, hipStream_t st) {
-    (void)hipGetLastError();
-    if (dtype == FTTS_F32) {
-        const dim3 g((unsigned)(((int64_t)a.rows * a.n_head + kTreeWaves - 1) / kTreeWaves)), t(kTreeWaves * 64);
-        hipLaunchKernelGGL(tree_row_kernel<true>, g, t, 0, st, a);
-        return hipGetLastError();
-    }
+    const bool f32 = dtype == FTTS_F32;
     int waves = 4;
-    TreePlan p = tree_plan(a, waves);
+    TreePlan p = tree_plan(a, f32, waves);
     const int64_t slots = p.parts > 1 ? (int64_t)p.parts * a.rows * a.n_head : 0;
     if ((size_t)slots * (kHeadDim + 2) * 4 > ws_bytes) return hipErrorInvalidValue;
     p.o = reinterpret_cast<float*>(ws);
     p.ml = reinterpret_cast<float2*>(p.o + slots * kHeadDim);
     const dim3 wg((unsigned)(p.tiles * a.n_kv_head * p.parts)), wt(waves * 64);
-    if (waves == 8) hipLaunchKernelGGL(tree_tile_kernel<8>, wg, wt, 0, st, a, p);
+    (void)hipGetLastError();
+    if (f32 && waves == 8) hipLaunchKernelGGL(tree_tile_f32_kernel<8>, wg, wt, 0, st, a, p);
+    else if (f32) hipLaunchKernelGGL(tree_tile_f32_kernel<4>, wg, wt, 0, st, a, p);
+    else if (waves == 8) hipLaunchKernelGGL(tree_tile_kernel<8>, wg, wt, 0, st, a, p);
     else hipLaunchKernelGGL(tree_tile_kernel<4>, wg, wt, 0, st, a, p);
     if (hipError_t e = hipGetLastError()) return e;
     if (p.parts == 1) return hipSuccess;
@@ -568,7 +692,7 @@ static hipError_t launch_tree_attention(int dtype, const TreeArgs& a, void* ws, 
     join.rows = a.rows;
     join.row_offsets = a.row_offsets;
     join.B = a.B;
-    return launch_attn_join(false, join, p.parts, p.ml, p.o, st);
+    return launch_attn_join(f32, join, p.parts, p.ml, p.o, st);
 }
 
 }  // namespace ftts
