@@ -35,10 +35,10 @@ struct TreeArgs {
 // The bits of tokens 0 .. n - 1.
 __device__ __forceinline__ uint64_t low_bits(int n) { return n >= 64 ? ~0ull : (1ull << max(n, 0)) - 1; }
 
-// How a call is cut: tiles of so many rows of a sequence, `per` pages of its chain a workgroup, `parts` of them along it;
-// partials of part p (where there are several) at ml + p * T H and o + p * T H * 64.
+// How a call is cut: tiles of 32 rows of a sequence, its chain of pages in so many equal parts; partials of part p (where
+// there are several) at ml + p * T H and o + p * T H * 64.
 struct TreePlan {
-    int tiles, per, parts;
+    int tiles, parts;
     bool blocks;  // (tree_work)
     float2* ml;
     float* o;
@@ -65,7 +65,8 @@ __device__ __forceinline__ int sum_up(int v) {
 // False: no such tile.
 __device__ __forceinline__ bool tree_work(const TreeArgs& a, const TreePlan& pl, int size, int lane, TreeWork& w) {
     static_assert(FTTS_MAX_BATCH <= kWave, "one sequence per lane");
-    // Heads fastest, so that neighbouring blocks of a page are read at about the same time.  blocks: in blocks of 8 tiles
+    // Heads fastest, so that neighbouring blocks of a page are read at about the same time (heads times parts are a multiple
+    // of 8, where there are parts: a sequence's tiles are then on one XCD).  blocks: in blocks of 8 tiles
     // whose (head, tile) pairs go to the 8 XCDs (workgroups are dealt to them in turn) in runs, tiles fastest: a sequence's
     // tiles, and in a block all sequences behind a prefix, read a head's pages through one L2.
     int tile, i = blockIdx.x;
@@ -103,8 +104,9 @@ __device__ __forceinline__ bool tree_work(const TreeArgs& a, const TreePlan& pl,
     w.past = __builtin_amdgcn_readlane(length, w.b) - w.n;  // (both within int: n >= 1)
     w.own = w.past < 0 ? 0 : (int)min((int64_t)w.past + w.n, (int64_t)a.max_pages * kPage);
     w.n_pre = w.past < 0 ? 0 : (a.prefix_len + kPage - 1) / kPage;
-    w.j0 = w.part * pl.per;
-    w.pages = max(min(pl.per, w.n_pre + (w.own + kPage - 1) / kPage - w.j0), 0);
+    const int every = w.n_pre + (w.own + kPage - 1) / kPage, per = (every + pl.parts - 1) / pl.parts;
+    w.j0 = w.part * per;
+    w.pages = max(min(per, every - w.j0), 0);
     return true;
 }
 
@@ -621,12 +623,12 @@ __global__ __launch_bounds__(W * 64, 2) void tree_tile_f32_kernel(const TreeArgs
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Parts pay for a second launch and a row's partials, 8 waves a workgroup for fewer workgroups at once and a longer hand-
-// over.  In bf16 a part's chain of pages costs 0.40 us a page with 4 waves and 0.205 with 8 while 610 (280) workgroups run;
-// where there are more, so many times that and half a part that is begun late.  Fitted to 1,338 calls (fp32: 1,229) of 1 to
-// 64 sequences, trees of 1 to 256, 20/20, 20/4, 12/12, 12/2, 32/16, 8/1 and 4/4 heads, up to 16,000 own tokens behind up to
-// 5000 (2000 and 1000), each run with 4 and 8 waves in 1 to 48 parts: the choice costs 1.4% (2.0%) of a call on average,
-// always 4 waves and one part 35% (47%), 8 waves 28% (47%).  Own lengths are on the device, so the table's width stands
-// for them.
+// over.  In bf16 a part's chain of pages costs 0.42 us a page with 4 waves and 0.27 with 8 while 805 (295) workgroups run;
+// where there are more, so many times that and one and a half parts that are begun late.  Fitted to 1,455 calls (fp32: 963)
+// of 1 to 64 sequences, trees of 1 to 256, 20/20, 20/4, 12/12, 12/2, 32/16, 8/1 and 4/4 heads, up to 16,000 own tokens behind
+// up to 5000 (2000 and 1000), each run with 4 and 8 waves in 1 to 48 parts: the choice costs 1.0% (1.6%) of a call on
+// average, always 4 waves and one part 33% (43%), 8 waves 25% (44%).  Own lengths are on the device, so the table's width
+// stands for them.
 constexpr int kTreeMaxParts = 48, kTreeMaxSlots = 1 << 18;  // partials of a call: 69 MB at most
 struct TreeCost {
     double begun, own;       // of a sequence's tiles the one that is begun, of the table's width what is filled
@@ -636,24 +638,25 @@ struct TreeCost {
     double group;            // us a workgroup
 };
 static TreePlan tree_plan(const TreeArgs& a, bool f32, int& waves) {
-    static constexpr TreeCost kCost[2] = {{0.67, 0.86, {610, 280}, {0.40, 0.205}, 1.5, 0.48, 2.5, 0.096e-3, 5.5e-3},
-                                          {0.92, 1.61, {274, 213}, {0.61, 0.47}, 1.6, 0.34, 1.9, 0.19e-3, 1.9e-3}};
+    static constexpr TreeCost kCost[2] = {{0.99, 1.11, {805, 295}, {0.417, 0.269}, 0.7, 1.47, 3.3, 0.115e-3, 5.8e-3},
+                                          {1.41, 1.46, {410, 306}, {0.48, 0.346}, 2.1, 0.30, 1.28, 0.23e-3, 4.0e-3}};
     const TreeCost& c = kCost[f32];
     const double g = a.n_head / a.n_kv_head, units = a.n_kv_head * (a.rows * g / 32 + c.begun * a.B), row_heads = (double)a.rows * a.n_head;
     const int64_t pages = ceil_div(a.prefix_len, kPage) + a.max_pages;
     const double chain = ceil_div(a.prefix_len, kPage) + c.own * a.max_pages;
     TreePlan p{};
     double least = 1e30;
+    // (4 trees of 40-64 behind 6,000-14,000, 20 heads: 51 us in 4 parts, 64 in 3 and 70 in 5, whose tiles read through two L2)
+    const int step = a.n_kv_head % 8 == 0 ? 1 : a.n_kv_head % 4 == 0 ? 2 : a.n_kv_head % 2 == 0 ? 4 : 8;
     for (const int n : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, kTreeMaxParts}) {
-        if (n > 1 && (2 * n > pages || n * row_heads > kTreeMaxSlots)) break;
-        const int per = (int)ceil_div(pages, n), parts = (int)ceil_div(pages, per);
+        const int parts = n > 1 ? (int)ceil_div(n, step) * step : 1;
+        if (n > 1 && (2 * parts > pages || parts * row_heads > kTreeMaxSlots)) break;
         for (const int e : {0, 1}) {
             const double full = units * parts / c.room[e];
             const double t = e * c.eight + c.page[e] * chain / parts * (full > 1 ? full + c.late : 1.0) +
                              (parts > 1 ? c.join + c.partial * parts * row_heads : 0) + c.group * units * parts;
             if (t >= least) continue;
             least = t;
-            p.per = per;
             p.parts = parts;
             waves = e ? 8 : 4;
         }
