@@ -623,23 +623,23 @@ __global__ __launch_bounds__(W * 64, 2) void tree_tile_f32_kernel(const TreeArgs
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Parts pay for a second launch and a row's partials, 8 waves a workgroup for fewer workgroups at once and a longer hand-
-// over.  In bf16 a part's chain of pages costs 0.42 us a page with 4 waves and 0.27 with 8 while 805 (295) workgroups run;
-// where there are more, so many times that and one and a half parts that are begun late.  Fitted to 1,455 calls (fp32: 963)
-// of 1 to 64 sequences, trees of 1 to 256, 20/20, 20/4, 12/12, 12/2, 32/16, 8/1 and 4/4 heads, up to 16,000 own tokens behind
-// up to 5000 (2000 and 1000), each run with 4 and 8 waves in 1 to 48 parts: the choice costs 1.0% (1.6%) of a call on
-// average, always 4 waves and one part 33% (43%), 8 waves 25% (44%).  Own lengths are on the device, so the table's width
-// stands for them.
+// over.  In bf16 a part's chain of pages costs 0.40 us a page with 4 waves and 0.25 with 8 while fewer than 590 (270)
+// workgroups run, and so many times that where there are more, with a bend between.  Fitted to 1,455 calls (fp32: 963) of 1
+// to 64 sequences, trees of 1 to 256, 20/20, 20/4, 12/12, 12/2, 32/16, 8/1 and 4/4 heads, up to 16,000 own tokens behind up
+// to 5000 (2000 and 1000), each run with 4 and 8 waves in 1 to 48 parts: the choice costs 1.1% (1.7%) of a call on average,
+// always 4 waves and one part 33% (43%), 8 waves 25% (44%).  Own lengths are on the device, so the table's width stands for
+// them.
 constexpr int kTreeMaxParts = 48, kTreeMaxSlots = 1 << 18;  // partials of a call: 69 MB at most
 struct TreeCost {
     double begun, own;       // of a sequence's tiles the one that is begun, of the table's width what is filled
     double room[2], page[2]; // workgroups at once, us a page of the chain: 4 waves, 8 waves
-    double eight, late;      // us for 8 waves; of a part that is begun late
+    double eight, bend;      // us for 8 waves; how sharp the bend is
     double join, partial;    // us for the second launch, and a partial
     double group;            // us a workgroup
 };
 static TreePlan tree_plan(const TreeArgs& a, bool f32, int& waves) {
-    static constexpr TreeCost kCost[2] = {{0.99, 1.11, {805, 295}, {0.417, 0.269}, 0.7, 1.47, 3.3, 0.115e-3, 5.8e-3},
-                                          {1.41, 1.46, {410, 306}, {0.48, 0.346}, 2.1, 0.30, 1.28, 0.23e-3, 4.0e-3}};
+    static constexpr TreeCost kCost[2] = {{0.75, 0.83, {590, 270}, {0.40, 0.246}, 1.0, 3.9, 2.7, 0.155e-3, 4.9e-3},
+                                          {1.40, 1.37, {400, 306}, {0.48, 0.367}, 1.4, 3.1, 1.27, 0.168e-3, 4.5e-3}};
     const TreeCost& c = kCost[f32];
     const double g = a.n_head / a.n_kv_head, units = a.n_kv_head * (a.rows * g / 32 + c.begun * a.B), row_heads = (double)a.rows * a.n_head;
     const int64_t pages = ceil_div(a.prefix_len, kPage) + a.max_pages;
@@ -653,7 +653,7 @@ static TreePlan tree_plan(const TreeArgs& a, bool f32, int& waves) {
         if (n > 1 && (2 * parts > pages || parts * row_heads > kTreeMaxSlots)) break;
         for (const int e : {0, 1}) {
             const double full = units * parts / c.room[e];
-            const double t = e * c.eight + c.page[e] * chain / parts * (full > 1 ? full + c.late : 1.0) +
+            const double t = e * c.eight + c.page[e] * chain / parts * std::pow(1.0 + std::pow(full, c.bend), 1.0 / c.bend) +
                              (parts > 1 ? c.join + c.partial * parts * row_heads : 0) + c.group * units * parts;
             if (t >= least) continue;
             least = t;
