@@ -666,6 +666,28 @@ int ftts_decode_step_shared(const ftts_weights* w, const ftts_shared_prefix* pre
                             float* logits_out, float* hidden_out, int32_t* sampled_out, const float* uniforms,
                             const ftts_sampling* samp, int32_t B, void* ws, size_t ws_bytes, void* stream);
 
+/* Bytes of workspace for ftts_tree_step over up to max_rows rows (covers ftts_workspace_bytes of max_batch sequences, for
+ * the other calls on the same workspace).  Returns 0 for invalid arguments. */
+size_t ftts_tree_workspace_bytes(const ftts_config* cfg, int32_t max_batch, int32_t max_rows);
+
+/*
+ * One pass of the model over drafted trees: the embeddings of tokens [n_rows] at positions [n_rows] (a drafted token's
+ * position is its parent's + 1), every layer's keys and values written behind the cached tokens, attention by
+ * ftts_tree_attention's rules, and the logits behind every row, which ftts_sample and ftts_tree_commit take.
+ *   prefix       the shared prefix, or NULL for none.
+ *   row_offsets, masks, mask_words  as in ftts_tree_attention.
+ *   pt           block table and own lengths, the trees' tokens among them (as ftts_build_tables leaves them).
+ *   logits_out   [n_rows][vocab] fp32.
+ *   ws           workspace of at least ftts_tree_workspace_bytes(cfg, B, n_rows); no prefill of it is needed.
+ * A row whose token or position is out of range, or whose page is, writes no key and value; its own logits, and those of
+ * rows whose masks have it, are unspecified.  So are the logits of rows of no sequence.  1 <= B <= FTTS_MAX_BATCH,
+ * 1 <= n_rows <= 2^20.
+ */
+int ftts_tree_step(const ftts_weights* w, const ftts_shared_prefix* prefix, const int32_t* tokens,
+                   const int32_t* positions, const int32_t* row_offsets, int32_t n_rows, int32_t B,
+                   const int64_t* masks, int32_t mask_words, const ftts_page_table* pt, const ftts_kv_pool* kv,
+                   float* logits_out, void* ws, size_t ws_bytes, void* stream);
+
 /* ---- Semantic-to-Mel flow-matching DiT: one guided Euler step ------------------------
  *
  * Sec. II-A: the Semantic-to-Mel module is conditional flow matching with a

@@ -16,22 +16,6 @@
 
 namespace ftts {
 
-struct TreeArgs {
-    const void* q;
-    void* o;
-    int64_t q_ld, o_ld;
-    const void* kv_base;
-    int n_pages, layer, n_head, n_kv_head, max_pages;
-    const int32_t* block_table;
-    const int32_t* seq_lens;
-    const int32_t* row_offsets;
-    const uint64_t* masks;
-    int mask_words;
-    const int32_t* prefix_pages;
-    int prefix_len;
-    int B, rows;
-};
-
 // The bits of tokens 0 .. n - 1.
 __device__ __forceinline__ uint64_t low_bits(int n) { return n >= 64 ? ~0ull : (1ull << max(n, 0)) - 1; }
 
@@ -668,11 +652,11 @@ static TreePlan tree_plan(const TreeArgs& a, bool f32, int& waves) {
     return p;
 }
 
-static size_t tree_attention_bytes(int n_head, int rows) {
+size_t tree_attention_bytes(int n_head, int rows) {
     return (size_t)std::min<int64_t>((int64_t)rows * n_head * kTreeMaxParts, kTreeMaxSlots) * (kHeadDim + 2) * 4 + 256;
 }
 
-static hipError_t launch_tree_attention(int dtype, const TreeArgs& a, void* ws, size_t ws_bytes, hipStream_t st) {
+hipError_t launch_tree_attention(int dtype, const TreeArgs& a, void* ws, size_t ws_bytes, hipStream_t st) {
     const bool f32 = dtype == FTTS_F32;
     int waves = 4;
     TreePlan p = tree_plan(a, f32, waves);

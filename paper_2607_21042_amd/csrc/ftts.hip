@@ -986,6 +986,157 @@ int ftts_prefill_shared(const ftts_weights* w, const ftts_shared_prefix* prefix,
 
 }  // extern "C"
 
+// ---- drafted trees ------------------------------------------------------------------------
+
+namespace {
+
+// What a tree step needs after the prefill's regions: the attention's partials, the head's split-K scratch.
+struct TreeWs {
+    void* attn;
+    size_t attn_bytes;
+    float* part;
+    uint32_t* count;
+};
+// Whether the head of many rows runs on the matrix cores.
+bool tree_head_batched(const ftts_config& c, int rows) {
+    return c.wdtype != FTTS_F32 && rows >= batched_min(FTTS_BF16) && bgemm_supported(FTTS_BF16, c.d_model, false);
+}
+size_t tree_bytes(const ftts_config& c, int rows, PrefillWs* P, TreeWs* out, char* base) {
+    size_t off = prefill_bytes(c, 1, rows, P, base);
+    auto take = [&](size_t n) { size_t o = off; off += round256(n); return base ? base + o : nullptr; };
+    const size_t n = tree_attention_bytes(c.n_head, rows);
+    char* attn = take(n);
+    const int S = c.wdtype == FTTS_F32 ? 1 : bgemm_splits(FTTS_BF16, c.vocab, c.d_model, false);
+    char* part = take(S > 1 ? (size_t)S * 32 * c.vocab * 4 : 0);
+    char* count = take((size_t)bgemm_counters(c) * 4);
+    if (out) *out = TreeWs{attn, n, (float*)part, (uint32_t*)count};
+    return off;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t ftts_tree_workspace_bytes(const ftts_config* cfg, int32_t max_batch, int32_t max_rows) {
+    const size_t n = ftts_workspace_bytes(cfg, max_batch, max_rows);
+    if (n == 0) return 0;
+    if (max_rows < 1 || max_rows > (1 << 20)) {
+        fail(FTTS_E_RANGE, "max_rows must be in [1, 2^20]");
+        return 0;
+    }
+    return std::max(n, tree_bytes(*cfg, max_rows, nullptr, nullptr, nullptr));
+}
+
+int ftts_tree_step(const ftts_weights* w, const ftts_shared_prefix* prefix, const int32_t* tokens, const int32_t* positions,
+                   const int32_t* row_offsets, int32_t n_rows, int32_t B, const int64_t* masks, int32_t mask_words,
+                   const ftts_page_table* pt, const ftts_kv_pool* kv, float* logits_out, void* ws, size_t ws_bytes,
+                   void* stream) {
+    TRY(check_weights(w));
+    const ftts_config& c = w->cfg;
+    if (B < 1 || B > FTTS_MAX_BATCH) return fail(FTTS_E_SHAPE, "B must be in [1, %d]", FTTS_MAX_BATCH);
+    if (n_rows < 1 || n_rows > (1 << 20)) return fail(FTTS_E_RANGE, "n_rows must be in [1, 2^20]");
+    if (mask_words < 1 || mask_words > FTTS_MAX_TREE / 64)
+        return fail(FTTS_E_SHAPE, "mask_words must be in [1, %d]", FTTS_MAX_TREE / 64);
+    if (!tokens || !positions || !row_offsets || !masks || !logits_out)
+        return fail(FTTS_E_INVALID_ARG, "tokens/positions/row_offsets/masks/logits_out is NULL");
+    if (reinterpret_cast<uintptr_t>(masks) & 7u) return fail(FTTS_E_ALIGN, "masks not 8-byte aligned");
+    TRY(check_kv(pt, kv, true));
+    if (prefix) TRY(check_prefix(prefix));
+    TRY(check_ptr(ws, "workspace"));
+    PrefillWs P;
+    TreeWs W;
+    const size_t need = tree_bytes(c, n_rows, &P, &W, reinterpret_cast<char*>(ws));
+    if (ws_bytes < need) return fail(FTTS_E_WORKSPACE, "workspace too small: %zu < %zu", ws_bytes, need);
+
+    hipStream_t st = (hipStream_t)stream;
+    const int d = c.d_model, F = c.d_ff, V = c.vocab, M = n_rows;
+    const bool batched = tree_head_batched(c, M);
+    (void)hipGetLastError();
+    hipError_t e;
+    const TreeRowsArgs rows{w->tok_emb, w->pos_emb, V, c.n_pos, d, tokens, positions, row_offsets, pt->seq_lens, pt->block_table,
+                            M, B, pt->max_pages, kv->n_pages, P.x, P.slots, {P.count, W.count},
+                            {P.count ? P.split.n_count : 0, bgemm_counters(c)}};
+    if ((e = launch_tree_rows(c.wdtype, rows, st)) != hipSuccess) return hip_fail(e, "tree rows");
+
+    TreeArgs ta{};
+    ta.q = P.qkv;
+    ta.q_ld = 3 * d;
+    ta.o = P.a;
+    ta.o_ld = d;
+    ta.kv_base = kv->base;
+    ta.n_pages = kv->n_pages;
+    ta.n_head = ta.n_kv_head = c.n_head;
+    ta.max_pages = pt->max_pages;
+    ta.block_table = pt->block_table;
+    ta.seq_lens = pt->seq_lens;
+    ta.row_offsets = row_offsets;
+    ta.masks = reinterpret_cast<const uint64_t*>(masks);
+    ta.mask_words = mask_words;
+    ta.prefix_pages = prefix && prefix->len > 0 ? prefix->pages : nullptr;
+    ta.prefix_len = prefix ? prefix->len : 0;
+    ta.B = B;
+    ta.rows = M;
+
+    auto gemm = [&](int epi, const ftts_linear& L, const void* a, int N, int K, void* out, int layer) {
+        GemmArgs g{};
+        g.part = P.part;
+        g.count = P.count;
+        g.part_floats = P.split.part_floats;
+        g.n_count = P.split.n_count;
+        g.a = a;
+        g.w = L.w;
+        g.scale = (const uint16_t*)L.scale;
+        g.zero = (const uint16_t*)L.zero;
+        g.bias = L.bias;
+        g.M = M;
+        g.N = N;
+        g.K = K;
+        g.out = out;
+        g.kv.base = kv->base;
+        g.kv.n_pages = kv->n_pages;
+        g.kv.n_head = c.n_head;
+        g.kv.d_model = d;
+        g.kv.slots = P.slots;
+        g.kv.layer = layer;
+        return launch_gemm(c.wdtype, epi, g, gemm_plan(c.wdtype, M, N, K), st);
+    };
+    for (int l = 0; l < c.n_layer; ++l) {
+        const ftts_layer& L = w->layers[l];
+        if ((e = launch_ln_rows(c.wdtype, P.x, L.ln1_g, L.ln1_b, c.ln_eps, M, d, P.a, st)) != hipSuccess) return hip_fail(e, "ln1");
+        if ((e = gemm(EPI_QKV, L.qkv, P.a, 3 * d, d, P.qkv, l)) != hipSuccess) return hip_fail(e, "qkv gemm");
+        ta.layer = l;
+        if ((e = launch_tree_attention(shared_dtype(c), ta, W.attn, W.attn_bytes, st)) != hipSuccess) return hip_fail(e, "tree attention");
+        if ((e = gemm(EPI_RESID, L.out, P.a, d, d, P.x, l)) != hipSuccess) return hip_fail(e, "out gemm");
+        if ((e = launch_ln_rows(c.wdtype, P.x, L.ln2_g, L.ln2_b, c.ln_eps, M, d, P.a, st)) != hipSuccess) return hip_fail(e, "ln2");
+        if ((e = gemm(EPI_GELU, L.fc1, P.a, F, d, P.h, l)) != hipSuccess) return hip_fail(e, "fc1 gemm");
+        if ((e = gemm(EPI_RESID, L.fc2, P.h, d, F, P.x, l)) != hipSuccess) return hip_fail(e, "fc2 gemm");
+    }
+    if (batched) {
+        if ((e = launch_ln_rows(c.wdtype, P.x, w->lnf_g, w->lnf_b, c.ln_eps, M, d, P.a, st)) != hipSuccess) return hip_fail(e, "ln_f");
+        BgemmArgs g{};
+        g.w = w->head.w;
+        g.bias = w->head.bias;
+        g.N = V;
+        g.K = d;
+        g.B = M;
+        g.act = P.a;
+        g.out = logits_out;
+        g.out_stride = V;
+        g.part = W.part;
+        g.count = W.count;
+        if ((e = launch_bgemm(FTTS_BF16, EPI_STORE, g, st)) != hipSuccess) return hip_fail(e, "lm head");
+        return FTTS_OK;
+    }
+    GemvArgs g = gemv_args(w->head, V, d, M, P.x, logits_out, V);
+    g.ln_g = w->lnf_g;
+    g.ln_b = w->lnf_b;
+    g.eps = c.ln_eps;
+    if ((e = launch_gemv(c.wdtype, EPI_STORE, true, g, st)) != hipSuccess) return hip_fail(e, "lm head");
+    return FTTS_OK;
+}
+
+}  // extern "C"
+
 // ---- flow-matching DiT step -------------------------------------------------------------
 
 static_assert(2 * FTTS_DIT_MAX_BATCH <= kMaxPrefillSeqs, "both guidance branches of every utterance need a sequence");

@@ -344,6 +344,39 @@ hipError_t launch_attn_join(bool f32, const SharedAttnArgs& a, int slots, float2
 // Bytes of ws, for up to so many rows, prefix tokens and pages a sequence.
 size_t shared_attention_bytes(int n_head, int rows, int prefix_len, int max_pages);
 
+// Attention of trees of drafted tokens over the paged cache.
+struct TreeArgs {
+    const void* q;
+    void* o;
+    int64_t q_ld, o_ld;
+    const void* kv_base;
+    int n_pages, layer, n_head, n_kv_head, max_pages;
+    const int32_t* block_table;
+    const int32_t* seq_lens;
+    const int32_t* row_offsets;
+    const uint64_t* masks;
+    int mask_words;
+    const int32_t* prefix_pages;
+    int prefix_len;
+    int B, rows;
+};
+hipError_t launch_tree_attention(int dtype, const TreeArgs& a, void* ws, size_t ws_bytes, hipStream_t st);
+// Bytes of ws, for up to so many rows.
+size_t tree_attention_bytes(int n_head, int rows);
+// The rows of drafted trees: x [rows][d] = tok_emb[token] + pos_emb[position] (0 where one is out of range), the slot of
+// each row's key and value (-1: none), and zero[0 .. n_zero) = 0.
+struct TreeRowsArgs {
+    const void *tok_emb, *pos_emb;
+    int vocab, n_pos, d;
+    const int32_t *tokens, *positions, *row_offsets, *seq_lens, *block_table;
+    int rows, B, max_pages, n_pages;
+    float* x;
+    int32_t* slots;
+    uint32_t* zero[2];
+    int n_zero[2];
+};
+hipError_t launch_tree_rows(int wdtype, const TreeRowsArgs& a, hipStream_t st);
+
 // Flow-matching DiT step (bf16): time embedding, input rows and guidance.
 struct DitPrepareArgs {
     int T, n_mel, d_cond, d_model;

@@ -60,6 +60,41 @@ hipError_t launch_embed(int wdtype, const void* tok_emb, const void* pos_emb, in
     return hipGetLastError();
 }
 
+// A workgroup a row of the drafted trees.
+template <bool F32>
+__global__ __launch_bounds__(256) void tree_rows_kernel(const TreeRowsArgs a) {
+    const int r = blockIdx.x, lane = threadIdx.x & 63;
+    const int t = a.tokens[r], p = a.positions[r];
+    const bool ok = t >= 0 && t < a.vocab && p >= 0 && p < a.n_pos;
+    for (int z = 0; z < 2; ++z)
+        for (int i = r * 256 + threadIdx.x; i < a.n_zero[z]; i += a.rows * 256) a.zero[z][i] = 0u;
+    const int tc = min(max(t, 0), a.vocab - 1), pc = min(max(p, 0), a.n_pos - 1);
+    for (int k = threadIdx.x; k < a.d; k += blockDim.x) {
+        const float v = ld_act<F32>(a.tok_emb, (size_t)tc * a.d + k) + ld_act<F32>(a.pos_emb, (size_t)pc * a.d + k);
+        a.x[(size_t)r * a.d + k] = ok ? v : 0.f;
+    }
+    if (threadIdx.x >= kWave) return;
+    static_assert(FTTS_MAX_BATCH <= kWave, "one sequence per lane");
+    const int lo = lane < a.B ? a.row_offsets[lane] : 0, hi = lane < a.B ? a.row_offsets[lane + 1] : 0;
+    const int first = min(max(lo, 0), a.rows), n = min(max(hi, first), a.rows) - first;
+    const unsigned long long whose = __ballot(lane < a.B && r >= first && r < first + n);
+    const int b = whose ? __builtin_ctzll(whose) : 0;
+    const int64_t past = (int64_t)(whose ? a.seq_lens[b] : -1) - __builtin_amdgcn_readlane(n, b);
+    const int64_t at = past + r - __builtin_amdgcn_readlane(first, b);
+    int slot = -1;
+    if (whose && ok && past >= 0 && at < a.max_pages * kPage) {
+        const int phys = a.block_table[(size_t)b * a.max_pages + at / kPage];
+        if (phys >= 0 && phys < a.n_pages) slot = phys * kPage + (int)(at % kPage);
+    }
+    if (lane == 0) a.slots[r] = slot;
+}
+
+hipError_t launch_tree_rows(int wdtype, const TreeRowsArgs& a, hipStream_t st) {
+    if (wdtype == FTTS_F32) hipLaunchKernelGGL(tree_rows_kernel<true>, dim3(a.rows), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL(tree_rows_kernel<false>, dim3(a.rows), dim3(256), 0, st, a);
+    return hipGetLastError();
+}
+
 // ---- block reductions -------------------------------------------------------------------
 __device__ __forceinline__ float block_sum256(float v, float* red) {
     v = wave_sum(v);

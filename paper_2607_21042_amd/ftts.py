@@ -182,6 +182,11 @@ def lib():
         L.ftts_tree_commit.restype = _c.c_int
         L.ftts_tree_commit.argtypes = [vp, vp, vp, vp, i32, i32, P(PageTable), P(KvPool), i32, i32, i32, vp, i32, vp, vp,
                                        vp, vp]
+        L.ftts_tree_workspace_bytes.restype = _c.c_size_t
+        L.ftts_tree_workspace_bytes.argtypes = [P(Config), i32, i32]
+        L.ftts_tree_step.restype = _c.c_int
+        L.ftts_tree_step.argtypes = [P(Weights), P(SharedPrefixC), vp, vp, vp, i32, i32, vp, i32, P(PageTable), P(KvPool), vp,
+                                     vp, _c.c_size_t, vp]
         L.ftts_shared_workspace_bytes.restype = _c.c_size_t
         L.ftts_shared_workspace_bytes.argtypes = [P(Config), i32, i32, i32, i32]
         L.ftts_prefill_shared.restype = _c.c_int
@@ -695,6 +700,31 @@ def decode_step_shared(model, prefix, tokens, positions, page_table, kv, logits_
                                          _c.byref(page_table.c), _c.byref(kv.c), _ptr(logits_out), _ptr(hidden_out),
                                          _ptr(sampled_out), _ptr(uniforms), _c.byref(sampling), tokens.numel(),
                                          _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def tree_workspace_bytes(cfg: Config, max_batch: int, max_rows: int) -> int:
+    """ftts_tree_workspace_bytes."""
+    n = lib().ftts_tree_workspace_bytes(_c.byref(cfg), max_batch, max_rows)
+    if n == 0:
+        raise FTTSError(-1, lib().ftts_last_error().decode())
+    return n
+
+
+def tree_step(model, tokens, positions, row_offsets, masks, page_table, kv, logits_out, ws, prefix=None, stream=None):
+    """ftts_tree_step: one pass over drafted trees, tokens and positions [T] packed by row_offsets [B + 1], masks
+    [T][words] int64, lengths of the page table with the trees' tokens; logits of every row to logits_out [T][vocab]."""
+    T, B = tokens.numel(), row_offsets.numel() - 1
+    for name, t, n in (("tokens", tokens, T), ("positions", positions, T), ("row_offsets", row_offsets, B + 1)):
+        _sized(name, t, n, torch.int32)
+    _sized("logits_out", logits_out, T * model.shape.vocab, torch.float32)
+    if masks.dim() != 2 or masks.shape[0] != T:
+        raise FTTSError(-2, f"masks must be [{T}][words]")
+    _sized("masks", masks, masks.numel(), torch.int64)
+    _table_of(page_table, B)
+    _check(lib().ftts_tree_step(_c.byref(model.c), None if prefix is None else _c.byref(prefix.c), _ptr(tokens),
+                                _ptr(positions), _ptr(row_offsets), T, B, _ptr(masks), masks.shape[1],
+                                _c.byref(page_table.c), _c.byref(kv.c), _ptr(logits_out), _ptr(ws),
+                                ws.numel() * ws.element_size(), _stream(stream)))
 
 
 # --------------------------------------------------------------------------- device state

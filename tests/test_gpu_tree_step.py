@@ -1,0 +1,191 @@
+"""The model over drafted trees: ftts_tree_step against the oracle's full forward along each token's path, and generation
+by draft, step, sample and commit against step-by-step greedy decoding.  Bars as in tests/helpers.py (fp32 1e-4 normwise,
+bf16 storage 3e-2 absolute on logits)."""
+import numpy as np
+import pytest
+
+from oracle import gpt as ogpt
+from oracle import tree
+from paper_2607_21042_amd import ftts, workload
+from tests import helpers
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+SHAPE = workload.ModelShape(n_layer=2, d_model=256, n_head=4, d_head=64, d_ff=512, vocab=642)
+MODES = {"f32": ftts.F32, "bf16": ftts.BF16, "w8a16": ftts.W8A16, "w4a16": ftts.W4A16}
+
+
+def weights(mode):
+    master = workload.master_weights(SHAPE, seed=3)
+    return master if mode == "f32" else workload.bf16_weights(master) if mode == "bf16" else workload.quantisable_weights(master)
+
+
+def i32(v):
+    return torch.tensor(np.ascontiguousarray(v), dtype=torch.int32, device="cuda")
+
+
+class Run:
+    """Sequences of lens[b] prefilled rows (behind a shared prefix of P), with pages for `room` more tokens each."""
+
+    def __init__(self, dm, mode, lens, room, P=0, seed=5):
+        self.dm, self.lens, B, adt = dm, list(lens), len(lens), ftts.act_dtype(MODES[mode])
+        bf16 = mode != "f32"
+        self.pre = workload.prefix_embeddings([max(P, 1)], SHAPE.d_model, seed=seed, bf16=bf16)[:P]
+        self.rows = np.split(workload.prefix_embeddings(lens, SHAPE.d_model, seed=seed + 1, bf16=bf16), np.cumsum(lens)[:-1])
+        bt, n_own = helpers.make_block_table([n + room for n in lens], seed=seed)
+        n_pre = -(-P // 64)
+        self.kv = ftts.KVCache(SHAPE, MODES[mode], n_own + n_pre, fill=float("nan"))
+        self.pt = ftts.PageTableView(torch.from_numpy(bt).cuda(), i32([0] * B))
+        up = lambda a: torch.from_numpy(np.ascontiguousarray(a, np.float32)).cuda().to(adt)  # noqa: E731
+        ws = torch.zeros(ftts.shared_workspace_bytes(dm.cfg, B, max(sum(lens), P, 1), P, bt.shape[1]), dtype=torch.uint8, device="cuda")
+        self.prefix = None
+        if P:
+            pages = i32(np.arange(n_own, n_own + n_pre))
+            ftts.prefill(dm, up(self.pre), [P], ftts.PageTableView(pages[None], i32([0])), self.kv, None, ws)
+            self.prefix = ftts.SharedPrefix(pages, P)
+            ftts.prefill_shared(dm, self.prefix, up(np.concatenate(self.rows)), self.lens, None, [0] * B, 0, 0, self.pt, self.kv, None, ws)
+        else:
+            ftts.prefill(dm, up(np.concatenate(self.rows)), self.lens, self.pt, self.kv, None, ws)
+        torch.cuda.synchronize()
+
+    def step(self, cached, trees, done, words=1):
+        """trees: (tokens, parents) of each sequence, whose first token stands at position done[b]; cached: own tokens."""
+        tokens = np.concatenate([t for t, _ in trees])
+        positions = np.concatenate([d + tree.depths(p) for d, (_, p) in zip(done, trees)])
+        masks = torch.cat([ftts.tree_masks(p, words) for _, p in trees]).cuda()
+        self.cu = i32(np.concatenate([[0], np.cumsum([len(p) for _, p in trees])]))
+        self.pt.seq_lens.copy_(i32([c + len(p) for c, (_, p) in zip(cached, trees)]))
+        self.tokens, self.parents = i32(tokens), i32(np.concatenate([p for _, p in trees]))
+        ws = torch.full((ftts.tree_workspace_bytes(self.dm.cfg, len(trees), len(tokens)),), 0xFF, dtype=torch.uint8, device="cuda")
+        self.logits = torch.full((len(tokens), SHAPE.vocab), float("nan"), device="cuda")
+        ftts.tree_step(self.dm, self.tokens, i32(positions), self.cu, masks, self.pt, self.kv, self.logits, ws, prefix=self.prefix)
+        torch.cuda.synchronize()
+        return self.logits.cpu().numpy()
+
+
+def random_tree(rng, n):
+    return rng.integers(0, SHAPE.vocab, n), [-1] + [int(rng.integers(max(0, i - 5), i)) for i in range(1, n)]
+
+
+@pytest.mark.parametrize("mode", list(MODES))
+@pytest.mark.parametrize("P,lens,sizes", [(0, [5], [1]), (0, [62], [9]), (0, [1, 64, 130], [3, 40, 12]), (70, [33, 2], [20, 7]),
+                                          (0, [20 + 7 * i % 60 for i in range(12)], [1 + 5 * i % 17 for i in range(12)]), (0, [30], [100])])
+def test_parity(mode, P, lens, sizes):
+    inputs = weights(mode)
+    dm = ftts.DeviceModel(inputs, SHAPE, MODES[mode])
+    om = ogpt.GPT(helpers.oracle_weights(inputs, mode), SHAPE.n_head, SHAPE.d_head)
+    rng = np.random.default_rng(sum(sizes))
+    trees = [random_tree(rng, n) for n in sizes]
+    print(f"tree step: {mode}, prefix {P}, own {lens}, trees of {sizes}", flush=True)
+    r = Run(dm, mode, lens, max(sizes), P)
+    got = r.step(lens, trees, [0] * len(lens), words=2)
+    r0 = 0
+    for b, (tokens, parents) in enumerate(trees):
+        nodes = range(len(tokens)) if len(tokens) < 15 else sorted({0, 1, len(tokens) // 2, len(tokens) - 2, len(tokens) - 1})
+        for i in nodes:
+            path = [i]
+            while parents[path[0]] >= 0:
+                path.insert(0, parents[path[0]])
+            ref, _ = om.full_forward(om.rows(np.concatenate([r.pre, r.rows[b]]), tokens[path]))
+            err = np.abs(got[r0 + i] - ref[-1]).max()
+            assert err <= (1e-4 * np.abs(ref[-1]).max() if mode == "f32" else 3e-2), (b, i, err)
+        r0 += len(tokens)
+
+
+@pytest.mark.parametrize("P", [0, 70])
+def test_generation_by_drafts_is_step_by_step_generation(P):
+    """fp32: drafts of 12 tokens of which some follow what greedy decoding chooses; each round keeps what it accepts."""
+    inputs = weights("f32")
+    dm = ftts.DeviceModel(inputs, SHAPE, ftts.F32)
+    om = ogpt.GPT(inputs, SHAPE.n_head, SHAPE.d_head, dtype=np.float64)
+    lens, N = [7, 60, 64], 24
+    r = Run(dm, "f32", lens, N + 14, P)
+    want = [om.greedy_decode(np.concatenate([r.pre, r.rows[b]]), N, SHAPE.start_token) for b in range(3)]
+    rng = np.random.default_rng(8)
+    fed = [[int(SHAPE.start_token)] for _ in range(3)]      # what was fed; its last token is not yet in the cache
+    cached, kept = list(lens), []
+    path, counts, nxt, new = i32(np.zeros((3, 6))), i32([0] * 3), i32([0] * 3), i32([0] * 3)
+    choices, greedy = i32([0] * 36), ftts.Sampling(1.0, 1, 1.0)
+    while min(len(f) for f in fed) < N:
+        trees = []
+        for b in range(3):
+            tokens, parents = random_tree(rng, 12)
+            tokens[0] = fed[b][-1]
+            right, at = want[b][len(fed[b]) - 1:], 0
+            for depth in range(int(rng.integers(0, 5))):   # plant the right continuation somewhere in the tree
+                below = [i for i in range(at + 1, 12) if parents[i] == at]
+                if not below or depth >= len(right):
+                    break
+                at = below[-1]
+                tokens[at] = right[depth]
+            trees.append((tokens, parents))
+        r.step(cached, trees, [len(f) - 1 for f in fed])
+        ftts.sample(r.logits, greedy, None, choices)
+        ftts.tree_commit(r.tokens, r.parents, choices, r.cu, r.pt, r.kv, path, counts, nxt, new)
+        torch.cuda.synchronize()
+        for b, (tokens, _) in enumerate(trees):
+            p = path[b].tolist()[:int(counts[b])]
+            fed[b] += [int(tokens[i]) for i in p[1:]] + [int(nxt[b])]
+            kept.append(len(p))
+        assert new.tolist() == [c + int(k) for c, k in zip(cached, counts.tolist())]
+        cached = new.tolist()
+    for b in range(3):
+        n = min(len(fed[b]) - 1, N)
+        assert fed[b][1:n + 1] == [int(x) for x in want[b][:n]], b
+    assert max(kept) > 3 and min(kept) == 1
+
+
+def test_rows_out_of_range_write_nothing():
+    """A drafted token or position out of range, pages outside the pool: no key or value is written, and rows that do not
+    see the token are as they were without it."""
+    inputs = weights("bf16")
+    dm = ftts.DeviceModel(inputs, SHAPE, ftts.BF16)
+    r = Run(dm, "bf16", [30, 50], 40)
+    clean = r.kv.pool.clone()
+    trees = [(np.array([5, 6, 7, 8]), [-1, 0, 0, 1]), (np.array([9, 10, 11]), [-1, 0, 1])]
+    want = r.step([30, 50], trees, [0, 0])
+    r.kv.pool.copy_(clean)
+    trees[0][0][2], trees[1][0][1] = SHAPE.vocab, -4
+    got = r.step([30, 50], trees, [0, SHAPE.n_pos - 2])
+    slot = r.kv.pool[:, int(r.pt.block_table[0, 0]), :, :, 32]
+    assert torch.isnan(slot.float()).all()                             # token 2 of the first tree: slot 32
+    last = r.kv.pool[:, int(r.pt.block_table[1, 0]), :, :, 52]
+    assert torch.isnan(last.float()).all()                             # position n_pos of the second tree's last token
+    assert np.array_equal(got[[0, 1, 3]], want[[0, 1, 3]])
+    r.kv.pool.copy_(clean)
+    r.pt.block_table[0, 0] = 10 ** 6
+    before = r.kv.pool.clone()
+    r.step([30, 50], trees, [0, 0])
+    changed = (r.kv.pool != before) & ~(torch.isnan(r.kv.pool.float()) & torch.isnan(before.float()))
+    assert set(torch.nonzero(changed)[:, 1].tolist()) <= {int(r.pt.block_table[1, 0])}
+
+
+def test_replayed_from_a_graph():
+    inputs = weights("bf16")
+    dm = ftts.DeviceModel(inputs, SHAPE, ftts.BF16)
+    r = Run(dm, "bf16", [30, 70], 40)
+    rng = np.random.default_rng(2)
+    trees = [random_tree(rng, 9), random_tree(rng, 23)]
+    r.step([30, 70], trees, [0, 0])
+    masks = torch.cat([ftts.tree_masks(p, 1) for _, p in trees]).cuda()
+    positions = i32(np.concatenate([tree.depths(p) for _, p in trees]))
+    ws = torch.zeros(ftts.tree_workspace_bytes(dm.cfg, 2, 32), dtype=torch.uint8, device="cuda")
+    out, tokens = torch.zeros((32, SHAPE.vocab), device="cuda"), r.tokens.clone()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        def once(to):
+            ftts.tree_step(dm, tokens, positions, r.cu, masks, r.pt, r.kv, to, ws)
+        once(out)
+        side.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            once(out)
+    for k in range(4):
+        tokens.copy_(i32(rng.integers(0, SHAPE.vocab, 32)))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = torch.zeros_like(out)
+        once(eager)
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager)
