@@ -380,7 +380,9 @@ def _int32(name, t, dev, n=None):
         raise FTTSError(-3, f"{name} must be int32")
     if n is not None and t.numel() != n:
         raise FTTSError(-2, f"{name} must have {n} elements, not {t.numel()}")
-    return _data(name, t, dev)
+    if t.get_device() != dev or not t.is_contiguous():
+        return _data(name, t, dev)
+    return t.data_ptr()
 
 
 def _data(name, t, dev):
@@ -394,17 +396,22 @@ def _data(name, t, dev):
 
 def _rows(name, t, dev, shape):
     """Data pointer and row stride of a 2-D tensor of that shape with contiguous rows."""
-    if t.shape != shape or (shape[1] > 1 and t.stride(1) != 1):
+    strides = t.stride()
+    if t.shape != shape or (strides[1] != 1 and shape[1] > 1):
         raise FTTSError(-2, f"{name} must be {list(shape)} with contiguous rows")
     if t.get_device() != dev:
         raise FTTSError(-1, f"{name} is on {t.device}, other tensors are not")
-    return t.data_ptr(), t.stride(0) if shape[0] > 1 else shape[1]  # (the stride of a lone row says nothing)
+    return t.data_ptr(), strides[0] if shape[0] > 1 else shape[1]  # (the stride of a lone row says nothing)
+
+
+_WDTYPES = {torch.float32: F32, torch.bfloat16: BF16}
 
 
 def _wdtype(name, dtype):
-    if dtype not in (torch.float32, torch.bfloat16):
+    wdtype = _WDTYPES.get(dtype)
+    if wdtype is None:
         raise FTTSError(-3, f"{name} must be fp32 or bf16")
-    return F32 if dtype == torch.float32 else BF16
+    return wdtype
 
 
 # torch's own shortcut to a GPU's current stream handle (the stream object costs 1.8 us a call), where it has one
@@ -482,7 +489,7 @@ def rotate(x, rotary, positions, out, stream=None):
     dev = x.get_device()
     if width % 64:
         raise FTTSError(-2, "x must be [T][n_head * 64]")
-    _enqueue(dev, stream, lib().ftts_rotate, _wdtype("x", x.dtype), _wdtype("out", out.dtype), _c.byref(rotary.c),
+    _enqueue(dev, stream, lib().ftts_rotate, _wdtype("x", x.dtype), _wdtype("out", out.dtype), rotary.c,
              *_rows("x", x, dev, (T, width)), T, width // 64, _int32("positions", positions, dev, T),
              *_rows("out", out, dev, (T, width)))
 
@@ -490,26 +497,28 @@ def rotate(x, rotary, positions, out, stream=None):
 def append_rotated(k, v, rotary, positions, slots, kv, layer: int, q=None, q_out=None, stream=None):
     """ftts_append_rotated: append_kv of keys turned by their positions [T], and queries q [T][n_head * 64] of the same
     rows turned into q_out (the pool's dtype; may be q itself)."""
-    dev, layers, heads, T = k.get_device(), kv.pool.shape[0], kv.pool.shape[3], k.shape[0]
+    dev, pool, T = k.get_device(), kv.pool, k.shape[0]
+    dims = pool.shape
+    layers, heads = dims[0], dims[3]
     if (q is None) != (q_out is None):
         raise FTTSError(-1, "q and q_out come together")
     if k.dtype != v.dtype or (q is not None and q.dtype != k.dtype):
         raise FTTSError(-3, "q, k and v must have one dtype")
     if not 0 <= layer < layers:
         raise FTTSError(-5, f"layer must be in [0, {layers})")
-    if kv.pool.get_device() != dev:
-        raise FTTSError(-1, f"the pool is on {kv.pool.device}, k is not")
+    if pool.get_device() != dev:
+        raise FTTSError(-1, f"the pool is on {pool.device}, k is not")
     queries = (None, 0, 0, None, 0)
     if q is not None:
         if q.dim() != 2 or q.shape[1] % 64:
             raise FTTSError(-2, "q must be [T][n_head * 64]")
-        if q_out.dtype != kv.pool.dtype:
+        if q_out.dtype != pool.dtype:
             raise FTTSError(-3, "q_out must have the pool's dtype")
         shape = (T, q.shape[1])
         queries = (*_rows("q", q, dev, shape), shape[1] // 64, *_rows("q_out", q_out, dev, shape))
-    _enqueue(dev, stream, lib().ftts_append_rotated, _wdtype("k", k.dtype), kv.dtype, _c.byref(rotary.c), *queries,
+    _enqueue(dev, stream, lib().ftts_append_rotated, _wdtype("k", k.dtype), kv.dtype, rotary.c, *queries,
              *_rows("k", k, dev, (T, heads * 64)), *_rows("v", v, dev, (T, heads * 64)), T,
-             _int32("positions", positions, dev, T), _int32("slots", slots, dev, T), _c.byref(kv.c), layer, heads)
+             _int32("positions", positions, dev, T), _int32("slots", slots, dev, T), kv.c, layer, heads)
 
 
 class SharedPrefix:
@@ -601,7 +610,8 @@ def tree_attention(q, kv, layer: int, page_table, masks, row_offsets, out, ws, p
     """ftts_tree_attention: rows q [T][n_head * 64] of the drafted trees of `page_table`'s sequences (row_offsets
     [B + 1]; masks [T][words] int64), which all continue `prefix` (a SharedPrefix or None), to out [T][n_head * 64]."""
     T, width = q.shape
-    B, dev, layers, heads = page_table.block_table.shape[0], q.get_device(), kv.pool.shape[0], kv.pool.shape[3]
+    B, dev, pool = page_table.block_table.shape[0], q.get_device(), kv.pool.shape
+    layers, heads = pool[0], pool[3]
     if width % 64:
         raise FTTSError(-2, "q must be [T][n_head * 64]")
     if q.dtype != out.dtype or q.dtype != kv.pool.dtype:
@@ -614,15 +624,13 @@ def tree_attention(q, kv, layer: int, page_table, masks, row_offsets, out, ws, p
         raise FTTSError(-5, f"layer must be in [0, {layers})")
     if page_table.seq_lens.numel() != B:
         raise FTTSError(-2, f"the page table needs {B} lengths")
-    shared = [kv.pool, page_table.block_table, page_table.seq_lens]
-    if prefix is not None and prefix.len > 0:
-        shared.append(prefix.pages)
-    if any(t.get_device() != dev for t in shared):
+    if (kv.pool.get_device() != dev or page_table.block_table.get_device() != dev or page_table.seq_lens.get_device() != dev
+            or (prefix is not None and prefix.len > 0 and prefix.pages.get_device() != dev)):
         raise FTTSError(-1, f"the pool, the page table and the prefix must be on {q.device}, as q is")
     shape = AttnShape(_wdtype("q", q.dtype), width // 64, heads, 64)
-    _enqueue(dev, stream, lib().ftts_tree_attention, _c.byref(shape), *_rows("q", q, dev, (T, width)),
+    _enqueue(dev, stream, lib().ftts_tree_attention, shape, *_rows("q", q, dev, (T, width)),
              _int32("row_offsets", row_offsets, dev, B + 1), T, B, _data("masks", masks, dev), masks.shape[1],
-             None if prefix is None else _c.byref(prefix.c), _c.byref(page_table.c), _c.byref(kv.c), layer,
+             None if prefix is None else prefix.c, page_table.c, kv.c, layer,
              *_rows("out", out, dev, (T, width)), _data("ws", ws, dev), ws.numel() * ws.element_size())
 
 
@@ -635,11 +643,12 @@ def tree_commit(tokens, parents, choices, row_offsets, page_table, kv, path, cou
         raise FTTSError(-2, f"path must be [{B}][max_path]")
     if page_table.seq_lens.numel() != B:
         raise FTTSError(-2, f"the page table needs {B} lengths")
-    if any(t.get_device() != dev for t in (kv.pool, page_table.block_table, page_table.seq_lens)):
+    pool = kv.pool
+    if pool.get_device() != dev or page_table.block_table.get_device() != dev or page_table.seq_lens.get_device() != dev:
         raise FTTSError(-1, f"the pool and the page table must be on {tokens.device}, as tokens are")
     _enqueue(dev, stream, lib().ftts_tree_commit, _int32("tokens", tokens, dev), _int32("parents", parents, dev, T),
-             _int32("choices", choices, dev, T), _int32("row_offsets", row_offsets, dev, B + 1), T, B, _c.byref(page_table.c),
-             _c.byref(kv.c), kv.dtype, kv.pool.shape[0], kv.pool.shape[3], _int32("path", path, dev), path.shape[1],
+             _int32("choices", choices, dev, T), _int32("row_offsets", row_offsets, dev, B + 1), T, B, page_table.c,
+             kv.c, kv.dtype, (dims := pool.shape)[0], dims[3], _int32("path", path, dev), path.shape[1],
              _int32("counts", counts, dev, B), _int32("next_tokens", next_tokens, dev, B), _int32("new_lens", new_lens, dev, B))
 
 
