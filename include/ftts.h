@@ -679,6 +679,8 @@ size_t ftts_tree_workspace_bytes(const ftts_config* cfg, int32_t max_batch, int3
  *   pt           block table and own lengths, the trees' tokens among them (as ftts_build_tables leaves them).
  *   logits_out   [n_rows][vocab] fp32.
  *   ws           workspace of at least ftts_tree_workspace_bytes(cfg, B, n_rows); no prefill of it is needed.
+ * Rows are computed as a prefill's: over a bf16 pool their queries are rounded to bf16, where ftts_decode_step keeps 16
+ * bits, so logits of the two agree to that rounding and a near-tied choice can differ.
  * A row whose token or position is out of range, or whose page is, writes no key and value; its own logits, and those of
  * rows whose masks have it, are unspecified.  So are the logits of rows of no sequence.  1 <= B <= FTTS_MAX_BATCH,
  * 1 <= n_rows <= 2^20.

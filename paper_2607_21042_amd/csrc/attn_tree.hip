@@ -306,7 +306,15 @@ __device__ __forceinline__ void tree_finish(const TreeArgs& a, const TreePlan& p
 }
 
 // bf16: the waves take the halves of the run's pages in turn (wave w: w, w + W, ...) by direct-to-LDS loads into a stage of
-// their own, the next half's K (V) on its way once this one's is in registers; no barrier in the loop.
+// their own, the next half's K (V) on its way once this one's is in registers; no barrier in the loop.  Halves before the
+// tree come first and need no mask; those of the tree follow.  Queries and masks are waited for before the loop: a wait for
+// them in it would be one for the next half's loads too.
+//
+// Bound by reading where the pages are many (a half costs a wave 1,285 cycles of vector work, two waves a SIMD hide the
+// loads up to 5.1 TB/s), by one tile's chain of halves, start and hand-over (5 us) where they are few.  Captured: 32 trees of
+// 8-64 tokens behind 64-1,200 at 20 heads, 123 MB, 32.4 us; 4 of 40-64 behind 6,000-14,000, 188 MB, 46.2 and the join 4.9;
+// one of 16 behind 300 7.5.  A wave a row without matrix products took 1,352 us for the first and 4,113 for the second.
+// Slower or level: whole pages a step, two tiles a wave (spills), four waves a SIMD, two halves in flight, 16 waves.
 template <int W>
 __global__ __launch_bounds__(W * 64, W == 4 ? 3 : 4) void tree_tile_kernel(const TreeArgs a, const TreePlan pl) {
     __shared__ __attribute__((aligned(1024))) char smem[W * 34 * 256];  // the stages, then the waves' results
@@ -431,7 +439,7 @@ __global__ __launch_bounds__(W * 64, W == 4 ? 3 : 4) void tree_tile_kernel(const
 }
 
 // fp32: the same with fp32 matrix products, all sums in fp32.  Bound by the products: 4096 cycles a wave and half of a
-// page, whatever the rows.
+// page, whatever the rows.  4 trees of 8-32 behind 50-700 at 20 heads, 20 MB, 15.0 us and the join 3.9.
 constexpr int kTfTile = kSfK * kHeadDim * 4, kTfStage = 2 * kTfTile;
 // As th_add_not_finite; v0, v1: values of the keys that element i is for, in dims lane % 32 and 32 + lane % 32.
 __device__ __forceinline__ void tf_add_not_finite(SaState& a, const float (&v0)[16], const float (&v1)[16], uint32_t seen, int hh) {

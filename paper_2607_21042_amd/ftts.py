@@ -722,18 +722,18 @@ def tree_workspace_bytes(cfg: Config, max_batch: int, max_rows: int) -> int:
 def tree_step(model, tokens, positions, row_offsets, masks, page_table, kv, logits_out, ws, prefix=None, stream=None):
     """ftts_tree_step: one pass over drafted trees, tokens and positions [T] packed by row_offsets [B + 1], masks
     [T][words] int64, lengths of the page table with the trees' tokens; logits of every row to logits_out [T][vocab]."""
-    T, B = tokens.numel(), row_offsets.numel() - 1
-    for name, t, n in (("tokens", tokens, T), ("positions", positions, T), ("row_offsets", row_offsets, B + 1)):
-        _sized(name, t, n, torch.int32)
+    T, B, dev = tokens.numel(), row_offsets.numel() - 1, tokens.get_device()
     _sized("logits_out", logits_out, T * model.shape.vocab, torch.float32)
     if masks.dim() != 2 or masks.shape[0] != T:
         raise FTTSError(-2, f"masks must be [{T}][words]")
     _sized("masks", masks, masks.numel(), torch.int64)
     _table_of(page_table, B)
-    _check(lib().ftts_tree_step(_c.byref(model.c), None if prefix is None else _c.byref(prefix.c), _ptr(tokens),
-                                _ptr(positions), _ptr(row_offsets), T, B, _ptr(masks), masks.shape[1],
-                                _c.byref(page_table.c), _c.byref(kv.c), _ptr(logits_out), _ptr(ws),
-                                ws.numel() * ws.element_size(), _stream(stream)))
+    if any(t.get_device() != dev for t in (kv.pool, page_table.block_table, page_table.seq_lens)):
+        raise FTTSError(-1, f"the pool and the page table must be on {tokens.device}, as tokens are")
+    _enqueue(dev, stream, lib().ftts_tree_step, model.c, None if prefix is None else prefix.c, _int32("tokens", tokens, dev),
+             _int32("positions", positions, dev, T), _int32("row_offsets", row_offsets, dev), T, B, _data("masks", masks, dev),
+             masks.shape[1], page_table.c, kv.c, _data("logits_out", logits_out, dev), _data("ws", ws, dev),
+             ws.numel() * ws.element_size())
 
 
 # --------------------------------------------------------------------------- device state

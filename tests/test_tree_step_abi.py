@@ -54,7 +54,7 @@ def bound(T=9, B=2, tokens=9, positions=9, masks=(9, 1), logits=None, tdtype=tor
     i = lambda n, t=torch.int32: torch.zeros(n, dtype=t)  # noqa: E731
     pt = SimpleNamespace(block_table=i((table, 2)), seq_lens=i(table), c=ftts.PageTable())
     ftts.tree_step(SimpleNamespace(shape=SHAPE, wdtype=ftts.BF16, c=ftts.Weights()), i(tokens, tdtype), i(positions), i(B + 1),
-                   i(masks, mdtype), pt, SimpleNamespace(c=ftts.KvPool()), torch.zeros(T * SHAPE.vocab if logits is None else logits),
+                   i(masks, mdtype), pt, SimpleNamespace(pool=torch.zeros(1), c=ftts.KvPool()), torch.zeros(T * SHAPE.vocab if logits is None else logits),
                    torch.zeros(16, dtype=torch.uint8))
 
 
