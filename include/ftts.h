@@ -682,8 +682,9 @@ size_t ftts_tree_workspace_bytes(const ftts_config* cfg, int32_t max_batch, int3
  * Rows are computed as a prefill's: over a bf16 pool their queries are rounded to bf16, where ftts_decode_step keeps 16
  * bits, so logits of the two agree to that rounding and a near-tied choice can differ.
  * A row whose token or position is out of range, or whose page is, writes no key and value; its own logits, and those of
- * rows whose masks have it, are unspecified.  So are the logits of rows of no sequence.  1 <= B <= FTTS_MAX_BATCH,
- * 1 <= n_rows <= 2^20.
+ * rows whose masks have it, are unspecified.  Rows of no sequence and those of an inactive one (a length below n_b) write
+ * none either, and their logits are unspecified: a captured call may have room for more rows than its trees take.
+ * 1 <= B <= FTTS_MAX_BATCH, 1 <= n_rows <= 2^20.
  */
 int ftts_tree_step(const ftts_weights* w, const ftts_shared_prefix* prefix, const int32_t* tokens,
                    const int32_t* positions, const int32_t* row_offsets, int32_t n_rows, int32_t B,

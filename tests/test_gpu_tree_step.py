@@ -189,3 +189,75 @@ def test_replayed_from_a_graph():
         once(eager)
         torch.cuda.synchronize()
         assert torch.equal(out, eager)
+
+
+@pytest.mark.parametrize("mode", ["f32", "bf16"])
+def test_padded_rows_and_inactive_sequences(mode):
+    """Rows behind the last sequence and those of a sequence whose length is below its rows write nothing, whatever their
+    tokens and positions; the others' logits are as without them."""
+    dm = ftts.DeviceModel(weights(mode), SHAPE, MODES[mode])
+    rng = np.random.default_rng(4)
+    trees = [random_tree(rng, n) for n in (5, 9, 3)]
+    r = Run(dm, mode, [30, 4, 61], 40)
+    clean = r.kv.pool.clone()
+    want = r.step([30, -7, 61], trees, [0, 0, 0])          # the second one's length: 2 for 9 rows
+    own = set(r.pt.block_table[0].tolist() + r.pt.block_table[2].tolist())
+    changed = (r.kv.pool != clean) & ~(torch.isnan(r.kv.pool.float()) & torch.isnan(clean.float()))
+    assert set(torch.nonzero(changed)[:, 1].tolist()) <= own
+    r.kv.pool.copy_(clean)
+    T, room = 17, 40
+    tokens = i32(rng.integers(-5, 10 ** 6, room))
+    tokens[:T] = r.tokens
+    positions = i32(rng.integers(-5, 10 ** 6, room))
+    positions[:T] = i32(np.concatenate([tree.depths(p) for _, p in trees]))
+    masks = torch.full((room, 1), -1, dtype=torch.int64, device="cuda")
+    masks[:T] = torch.cat([ftts.tree_masks(p, 1) for _, p in trees]).cuda()
+    out = torch.zeros((room, SHAPE.vocab), device="cuda")
+    ws = torch.full((ftts.tree_workspace_bytes(dm.cfg, 3, room),), 0xFF, dtype=torch.uint8, device="cuda")
+    ftts.tree_step(dm, tokens, positions, r.cu, masks, r.pt, r.kv, out, ws)
+    torch.cuda.synchronize()
+    bar = 1e-4 * np.abs(want[:5]).max() if mode == "f32" else 3e-2   # (other row counts may take other tiles)
+    for rows in (slice(0, 5), slice(14, 17)):
+        assert np.abs(out[rows].cpu().numpy() - want[rows]).max() <= bar
+    changed = (r.kv.pool != clean) & ~(torch.isnan(r.kv.pool.float()) & torch.isnan(clean.float()))
+    assert set(torch.nonzero(changed)[:, 1].tolist()) <= own
+
+
+def test_steps_by_drafts_and_by_token_share_a_workspace():
+    """fp32: tokens one by one, a draft of which a part is right, tokens one by one again, all in one workspace."""
+    inputs = weights("f32")
+    dm = ftts.DeviceModel(inputs, SHAPE, ftts.F32)
+    om = ogpt.GPT(inputs, SHAPE.n_head, SHAPE.d_head, dtype=np.float64)
+    r = Run(dm, "f32", [21], 30)
+    want = [int(t) for t in om.greedy_decode(r.rows[0], 12, SHAPE.start_token)]
+    size = max(ftts.tree_workspace_bytes(dm.cfg, 1, 8), ftts.workspace_bytes(dm.cfg, 1, 21))
+    ws = torch.zeros(size, dtype=torch.uint8, device="cuda")
+    ftts.prefill(dm, torch.from_numpy(np.ascontiguousarray(r.rows[0], np.float32)).cuda(), [21], r.pt, r.kv, None, ws)
+    greedy, fed, cached = ftts.Sampling(1.0, 1, 1.0), [int(SHAPE.start_token)], 21
+    one, logits = i32([0]), torch.empty((1, SHAPE.vocab), device="cuda")
+
+    def by_token(n):
+        nonlocal cached
+        for _ in range(n):
+            r.pt.seq_lens.copy_(i32([cached]))
+            ftts.decode_step(dm, i32([fed[-1]]), i32([len(fed) - 1]), r.pt, r.kv, logits, one, None, greedy, ws)
+            torch.cuda.synchronize()
+            fed.append(int(one))
+            cached += 1
+
+    by_token(3)
+    tokens, parents = i32([fed[-1], want[3], 5, want[4], 6, 7, want[5], 8]), [-1, 0, 0, 1, 1, 3, 3, 6]
+    pos = i32(len(fed) - 1 + np.asarray(tree.depths(parents)))
+    cu, out = i32([0, 8]), torch.empty((8, SHAPE.vocab), device="cuda")
+    r.pt.seq_lens.copy_(i32([cached + 8]))
+    ftts.tree_step(dm, tokens, pos, cu, ftts.tree_masks(parents, 1).cuda(), r.pt, r.kv, out, ws)
+    choices, path, count, nxt, new = i32([0] * 8), i32(np.zeros((1, 8))), i32([0]), i32([0]), i32([0])
+    ftts.sample(out, greedy, None, choices)
+    ftts.tree_commit(tokens, i32(parents), choices, cu, r.pt, r.kv, path, count, nxt, new)
+    torch.cuda.synchronize()
+    assert int(count) >= 4 and path[0].tolist()[:4] == [0, 1, 3, 6]
+    fed += [int(tokens[i]) for i in path[0].tolist()[1:int(count)]] + [int(nxt)]
+    cached = int(new)
+    by_token(4)
+    n = min(len(fed) - 1, 12)
+    assert n >= 11 and fed[1:n + 1] == want[:n]
