@@ -173,3 +173,18 @@ def test_replayed_from_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         d.check()
+
+
+def test_far_pages():
+    """Element offsets past 2^31 in a large pool."""
+    n_pages = 13200                                    # x 2 x 20 heads x 4096: 1.08e9 elements a layer
+    d = Drafts("bf16", 2, 20, [55], [30], chain_plan(3, 9), 12).gpu()
+    pool = torch.zeros((2, n_pages, 2, 20, 64, 64), device="cuda", dtype=torch.bfloat16)
+    far, ids = [n_pages - 1, n_pages - 2], d.table[0, :2].tolist()
+    pool[:, far] = d.kv.pool[:, ids]
+    near = d.kv
+    d.call()
+    d.check()
+    d.kv, d.pt = ftts.KVCache.over(pool), ftts.PageTableView(dev([far]), dev(d.lens))
+    d.call()
+    assert torch.equal(pool[:, far], near.pool[:, ids]) and not pool[:, :n_pages - 2].any()

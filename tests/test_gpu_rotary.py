@@ -180,3 +180,31 @@ def test_append_equals_rotate_and_append():
         ftts.append_kv(k_rot, x[:, a + b:].contiguous(), slots, ftts.KVCache.over(theirs), 0)
         torch.cuda.synchronize()
         assert torch.equal(ours, theirs) and torch.equal(work[:, :a], q_rot) and torch.equal(work[:, a:], x[:, a:])
+
+
+@pytest.mark.parametrize("T,H", [(1, 256), (9, 100), (700, 256), (4097, 20)])
+@pytest.mark.parametrize("layout,dim", [(tree.HALVES, 64), (tree.HALVES, 20), (tree.PAIRS, 64)])
+def test_many_heads_in_place(T, H, layout, dim):
+    rng = np.random.default_rng([T, H])
+    x = rows(rng, (T, H * 64), "bf16")
+    pos = rng.integers(0, 5000, T)
+    f, scale = tree.frequencies(dim, 10000.0)
+    print(f"in place: {T} rows of {H} heads, layout {layout}, {dim} columns", flush=True)
+    a = dev(x, torch.bfloat16)
+    ftts.rotate(a, ftts.Rotary(dim, layout), dev(pos), a)
+    torch.cuda.synchronize()
+    some = sorted({0, T // 2, T - 1} | set(rng.integers(0, T, 40).tolist()))
+    check(a[some].float().cpu().numpy(), x[some], pos[some], dim, layout, f, scale, "bf16", (T, H))
+
+
+def test_far_pages():
+    """Element offsets past 2^31 in a large pool."""
+    n_pages, T = 13200, 70                             # x 2 x 20 heads x 4096: 1.08e9 elements a layer
+    pool = torch.zeros((2, n_pages, 2, 20, 64, 64), device="cuda", dtype=torch.bfloat16)
+    near = torch.zeros((1, 2, 2, 20, 64, 64), device="cuda", dtype=torch.bfloat16)
+    x = dev(rows(np.random.default_rng(1), (T, 40 * 64), "bf16"), torch.bfloat16)
+    rot, pos = ftts.Rotary(64), dev(np.arange(T) * 13)
+    ftts.append_rotated(x[:, :1280], x[:, 1280:], rot, pos, dev(np.arange(T)), ftts.KVCache.over(near), 0)
+    ftts.append_rotated(x[:, :1280], x[:, 1280:], rot, pos, dev((n_pages - 2) * 64 + np.arange(T)), ftts.KVCache.over(pool), 1)
+    torch.cuda.synchronize()
+    assert torch.equal(pool[1, n_pages - 2:], near[0]) and not pool[0].any() and not pool[1, :n_pages - 2].any()
