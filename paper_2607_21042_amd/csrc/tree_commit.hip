@@ -40,7 +40,8 @@ __global__ __launch_bounds__(kTcWaves * 64) void tree_commit_kernel(const Commit
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int b = blockIdx.x / a.groups, mine = blockIdx.x % a.groups * kTcWaves + wave, waves = a.groups * kTcWaves;
     const int r0 = min(max(a.row_offsets[b], 0), a.rows), all = min(max(a.row_offsets[b + 1], r0), a.rows) - r0;
-    const int n = min(all, FTTS_MAX_TREE), len = a.seq_lens[b], past = len - all;
+    const int n = min(all, FTTS_MAX_TREE), len = a.seq_lens[b];
+    const int past = len < all ? -1 : len - all;  // (compared first: a length may be -2^31)
     if ((int)threadIdx.x < n) {
         const int r = r0 + threadIdx.x;
         s_node[threadIdx.x] = make_int3(a.tokens[r], a.parents[r], a.choices[r]);
