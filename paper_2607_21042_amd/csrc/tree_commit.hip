@@ -85,8 +85,8 @@ __global__ __launch_bounds__(kTcWaves * 64) void tree_commit_kernel(const Commit
     constexpr int kLanes = COLS / 16, kRows = kWave / kLanes;
     const int heads2 = 2 * a.n_kv_head, blocks = a.n_layer * heads2;
     const size_t page_bytes = (size_t)kPage * COLS, layer_bytes = (size_t)a.n_pages * heads2 * page_bytes;
-    auto place = [&](int t, int64_t& at) {  // of own token t in a (layer 0, keys, head 0) block
-        const int page = t / kPage;
+    auto place = [&](int64_t t, int64_t& at) {  // of own token t in a (layer 0, keys, head 0) block
+        const int64_t page = t / kPage;
         const int phys = page < a.max_pages ? a.block_table[(size_t)b * a.max_pages + page] : -1;
         at = (int64_t)phys * heads2 * page_bytes + (t % kPage) * COLS;
         return phys >= 0 && phys < a.n_pages;
@@ -95,7 +95,8 @@ __global__ __launch_bounds__(kTcWaves * 64) void tree_commit_kernel(const Commit
         const int i = i0 + lane / kLanes, from = i < kept ? path[i] : i;
         if (!__any(from != i)) continue;
         int64_t src = 0, dst = 0;
-        const bool there = place(past + from, src), move = place(past + i, dst) && there && from != i;
+        // (in 64 bits: lanes behind the path look past a length that may be 2^31 - 1)
+        const bool there = place((int64_t)past + from, src), move = place((int64_t)past + i, dst) && there && from != i;
         src += lane % kLanes * 16;
         dst += lane % kLanes * 16;
         for (int u0 = mine; u0 < blocks; u0 += kTcAhead * waves) {

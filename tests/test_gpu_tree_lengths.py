@@ -23,3 +23,17 @@ def test_commit_keeps_nothing_of_the_least_lengths(dtype):
     d.lens = [LEAST + b for b in range(64)]
     d.gpu().call()
     assert not d.check()[1].any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("step", [1, 2, 29])
+def test_commit_behind_the_largest_lengths(dtype, step):
+    """Paths whose places lie past every table move nothing; counts and new lengths are a path's as elsewhere."""
+    rows = [3, 9, 256, 30, 200]
+    d = Drafts(dtype, 2, 3, [60, 0, 20, 5, 9], rows, chain_plan(step, 999), 200, width=5)
+    for b, n in ((0, 2 ** 31 - 1), (1, 2 ** 31 - 1), (2, 2 ** 31 - 1), (3, 2 ** 31 - 9)):
+        d.lens[b] = n
+    print(f"commit: {dtype}, step {step}, lengths {d.lens}", flush=True)
+    d.gpu().call()
+    want = d.check()
+    assert want[1].tolist() == [min(-(-n // step), 200) for n in rows]
