@@ -32,7 +32,7 @@ struct TreePlan {
 // that the sequence sees, the prefix's before its own.
 struct TreeWork {
     int b, kh, row0, n, first;  // the tile's first pair of the sequence's n * g
-    int past, own, n_pre;       // own tokens before the tree, and in all (0: inactive); pages of the prefix
+    int past, own, n_pre;       // own tokens before the tree (-1: inactive), and in all; pages of the prefix
     int j0, pages;              // of the run
     int part;
 };
@@ -85,7 +85,8 @@ __device__ __forceinline__ bool tree_work(const TreeArgs& a, const TreePlan& pl,
     w.row0 = __builtin_amdgcn_readlane(first, w.b);
     w.n = __builtin_amdgcn_readlane(rows, w.b);
     w.first = (tile - __builtin_amdgcn_readlane(upto - mine, w.b)) * size;
-    w.past = __builtin_amdgcn_readlane(length, w.b) - w.n;  // (both within int: n >= 1)
+    const int own = __builtin_amdgcn_readlane(length, w.b);
+    w.past = own < w.n ? -1 : own - w.n;  // (compared first: a length may be -2^31)
     w.own = w.past < 0 ? 0 : (int)min((int64_t)w.past + w.n, (int64_t)a.max_pages * kPage);
     w.n_pre = w.past < 0 ? 0 : (a.prefix_len + kPage - 1) / kPage;
     const int every = w.n_pre + (w.own + kPage - 1) / kPage, per = (every + pl.parts - 1) / pl.parts;
