@@ -728,8 +728,9 @@ def tree_step(model, tokens, positions, row_offsets, masks, page_table, kv, logi
         raise FTTSError(-2, f"masks must be [{T}][words]")
     _sized("masks", masks, masks.numel(), torch.int64)
     _table_of(page_table, B)
-    if any(t.get_device() != dev for t in (kv.pool, page_table.block_table, page_table.seq_lens)):
-        raise FTTSError(-1, f"the pool and the page table must be on {tokens.device}, as tokens are")
+    if (any(t.get_device() != dev for t in (kv.pool, page_table.block_table, page_table.seq_lens))
+            or (prefix is not None and prefix.len > 0 and prefix.pages.get_device() != dev)):
+        raise FTTSError(-1, f"the pool, the page table and the prefix must be on {tokens.device}, as tokens are")
     _enqueue(dev, stream, lib().ftts_tree_step, model.c, None if prefix is None else prefix.c, _int32("tokens", tokens, dev),
              _int32("positions", positions, dev, T), _int32("row_offsets", row_offsets, dev), T, B, _data("masks", masks, dev),
              masks.shape[1], page_table.c, kv.c, _data("logits_out", logits_out, dev), _data("ws", ws, dev),

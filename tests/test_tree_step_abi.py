@@ -65,3 +65,17 @@ def bound(T=9, B=2, tokens=9, positions=9, masks=(9, 1), logits=None, tdtype=tor
 def test_binding_refuses_before_the_library(bad, what):
     with pytest.raises(ftts.FTTSError, match=what):
         bound(**bad)
+
+
+def test_binding_refuses_a_prefix_on_another_device():
+    def call(length):
+        pages = SimpleNamespace(get_device=lambda: 1)
+        i = lambda *n: torch.zeros(n, dtype=torch.int32)  # noqa: E731
+        ftts.tree_step(SimpleNamespace(shape=SHAPE, wdtype=ftts.BF16, c=ftts.Weights()), i(9), i(9), i(3), torch.zeros((9, 1), dtype=torch.int64),
+                       SimpleNamespace(block_table=i(2, 2), seq_lens=i(2), c=ftts.PageTable()), SimpleNamespace(pool=torch.zeros(1), c=ftts.KvPool()),
+                       torch.zeros(9 * SHAPE.vocab), torch.zeros(16, dtype=torch.uint8),
+                       prefix=SimpleNamespace(pages=pages, len=length, c=ftts.SharedPrefixC()))
+    with pytest.raises(ftts.FTTSError, match="prefix must be on"):
+        call(5)
+    with pytest.raises(ftts.FTTSError, match="GPU"):        # (a prefix of no tokens has no pages to read)
+        call(0)
