@@ -597,7 +597,9 @@ size_t ftts_tree_attention_workspace_bytes(const ftts_attn_shape* shape, int32_t
  *   mask_words   1 .. FTTS_MAX_TREE / 64.
  *   row_offsets  [B + 1] device, as in ftts_shared_attention; not NULL.
  * Everything else is as in ftts_shared_attention, but that a length below n_b (a negative one among
- * them) makes its sequence inactive.  In bf16 the scores, sums and weights are held in fp32, the
+ * them) makes its sequence inactive, and that n_rows * n_head ends below 2^29: the tiles of 32 rows and
+ * heads, n_kv_head * (n_rows * (n_head / n_kv_head) / 32 + B, from 16 on the next multiple of 8), have
+ * to be fewer than 2^24 (FTTS_E_RANGE otherwise).  In bf16 the scores, sums and weights are held in fp32, the
  * weights meet the values as two bf16 parts of each (within 2^-16 of it), and the output is rounded
  * once.  Equal calls give equal bits.  `ws` holds intermediate results of the call only; calls that
  * can run at the same time need one each.

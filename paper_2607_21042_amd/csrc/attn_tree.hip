@@ -615,6 +615,15 @@ __global__ __launch_bounds__(W * 64, 2) void tree_tile_f32_kernel(const TreeArgs
 
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// Tiles of 32 rows that so many sequences have at most; in one part many of them go in blocks of 8 (36 us for 32 trees of
+// 8-64 tokens behind up to 1200, 40 without the blocks; few tiles would leave a block's idle).
+static int64_t tree_tiles(int n_head, int n_kv_head, int rows, int B, int parts) {
+    const int64_t n = (int64_t)rows * (n_head / n_kv_head) / 32 + B;
+    return parts == 1 && n >= 16 ? ceil_div(n, 8) * 8 : n;
+}
+// A grid has fewer than 2^32 threads.
+static bool tree_fits(int64_t workgroups, int waves) { return workgroups * waves * kWave < 1LL << 32; }
+
 // Parts pay for a second launch and a row's partials, 8 waves a workgroup for fewer workgroups at once and a longer hand-
 // over.  In bf16 a part's chain of pages costs 0.40 us a page with 4 waves and 0.25 with 8 while fewer than 590 (270)
 // workgroups run, and so many times that where there are more, with a bend between.  Fitted to 1,455 calls (fp32: 963) of 1
@@ -644,20 +653,20 @@ static TreePlan tree_plan(const TreeArgs& a, bool f32, int& waves) {
     for (const int n : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, kTreeMaxParts}) {
         const int parts = n > 1 ? (int)ceil_div(n, step) * step : 1;
         if (n > 1 && (2 * parts > pages || parts * row_heads > kTreeMaxSlots)) break;
+        const int64_t tiles = tree_tiles(a.n_head, a.n_kv_head, a.rows, a.B, parts);
         for (const int e : {0, 1}) {
+            if (!tree_fits(tiles * a.n_kv_head * parts, e ? 8 : 4)) continue;  // (4 waves and one part: check_shape)
             const double full = units * parts / c.room[e];
             const double t = e * c.eight + c.page[e] * chain / parts * std::pow(1.0 + std::pow(full, c.bend), 1.0 / c.bend) +
                              (parts > 1 ? c.join + c.partial * parts * row_heads : 0) + c.group * units * parts;
             if (t >= least) continue;
             least = t;
             p.parts = parts;
+            p.tiles = (int)tiles;
             waves = e ? 8 : 4;
         }
     }
-    p.tiles = (int)((int64_t)a.rows * (a.n_head / a.n_kv_head) / 32) + a.B;
-    // (36 us for 32 trees of 8-64 tokens behind up to 1200, 40 without the blocks; few tiles would leave a block's idle)
     p.blocks = p.parts == 1 && p.tiles >= 16;
-    if (p.blocks) p.tiles = (int)ceil_div(p.tiles, 8) * 8;
     return p;
 }
 
@@ -705,8 +714,10 @@ int check_shape(const ftts_attn_shape* s, int B, int n_rows, int prefix_len, int
     if (s->n_head < 1 || s->n_head > 256 || s->n_kv_head < 1 || s->n_head % s->n_kv_head)
         return set_error(FTTS_E_SHAPE, "tree_attention: n_head must be in [1, 256] and a multiple of n_kv_head");
     if (B < 1 || B > FTTS_MAX_BATCH) return set_error(FTTS_E_SHAPE, "tree_attention: B must be in [1, %d]", FTTS_MAX_BATCH);
-    if (n_rows < 0 || n_rows > (1 << 24) || (int64_t)n_rows * s->n_head > 0x7FFFFFFF)
-        return set_error(FTTS_E_RANGE, "tree_attention: n_rows must be in [0, 2^24] and n_rows * n_head below 2^31");
+    if (n_rows < 0 || n_rows > (1 << 24)) return set_error(FTTS_E_RANGE, "tree_attention: n_rows must be in [0, 2^24]");
+    const int64_t groups = tree_tiles(s->n_head, s->n_kv_head, n_rows, B, 1) * s->n_kv_head;
+    if (!tree_fits(groups, 4))
+        return set_error(FTTS_E_RANGE, "tree_attention: %lld tiles of 32 rows and heads, a launch takes fewer than 2^24", (long long)groups);
     if (prefix_len < 0 || prefix_len > FTTS_MAX_SHARED_PREFIX)
         return set_error(FTTS_E_RANGE, "tree_attention: prefix length must be in [0, %d]", FTTS_MAX_SHARED_PREFIX);
     if (max_pages < 1 || max_pages > kMaxPages)

@@ -116,3 +116,21 @@ def test_commit_binding_refuses_before_the_library():
         with pytest.raises(ftts.FTTSError) as e:
             call(**bad)
         assert e.value.code == code, (bad, e.value)
+
+
+@pytest.mark.parametrize("heads,kvh,B,most", [(256, 256, 4, 65524 * 32 + 31), (64, 1, 64, ((1 << 24) - 72) // 2), (20, 4, 33, None)])
+def test_attention_refuses_more_tiles_than_a_launch_takes(heads, kvh, B, most):
+    """Tiles of 32 (row, head) pairs, in blocks of 8 where they are 16 and more: fewer than 2^24 of them, 2^32 threads."""
+    def tiles(rows):
+        n = rows * (heads // kvh) // 32 + B
+        return kvh * (-(-n // 8) * 8 if n >= 16 else n)
+    lo, hi = 1, 1 << 24
+    while hi - lo > 1:                                     # (lo fits, hi does not)
+        mid = (lo + hi) // 2
+        lo, hi = (mid, hi) if tiles(mid) < 1 << 24 else (lo, mid)
+    assert most in (None, lo) and (tiles(hi) >= 1 << 24 or hi == 1 << 24)
+    sh, wide = shape(heads=heads, kvh=kvh), 64 * heads
+    size = lambda rows: L.ftts_tree_attention_workspace_bytes(ctypes.byref(sh), B, rows, 0, 4)  # noqa: E731
+    assert size(lo) > 0 and attend(sh=sh, rows=lo, B=B, qs=wide, outs=wide, size=16) == -8
+    if hi < 1 << 24:
+        assert size(hi) == 0 and attend(sh=sh, rows=hi, B=B, qs=wide, outs=wide) == -5
