@@ -609,6 +609,17 @@ int ftts_tree_attention(const ftts_attn_shape* shape, const void* q, int64_t q_s
                         const ftts_shared_prefix* prefix, const ftts_page_table* pt, const ftts_kv_pool* kv,
                         int32_t layer, void* out, int64_t out_stride, void* ws, size_t ws_bytes, void* stream);
 
+/* How ftts_tree_attention runs a call of these sizes.  Host only: a pure function of its arguments that touches no
+ * device.  n_rows at least 1 (FTTS_E_SHAPE); other errors as ftts_tree_attention's. */
+typedef struct {
+    int32_t waves;  /* of a workgroup, which take its run of half pages in turn: 4 or 8 */
+    int32_t parts;  /* equal runs of each sequence's pages, joined by a second launch where there are several */
+    int32_t tiles;  /* of 32 (row, query head) pairs, at most */
+    int32_t blocks; /* 1: tiles in blocks of 8 that share a cache; 0: heads in turn */
+} ftts_tree_launch;
+int ftts_tree_attention_plan(const ftts_attn_shape* shape, int32_t B, int32_t n_rows, int32_t prefix_len, int32_t max_pages,
+                             ftts_tree_launch* out);
+
 /*
  * Keeps the accepted path of each drafted tree.  From the tree's first token on, the path goes to the
  * first child (parents[j] == the token's index, j above it) whose token is what the model chose at the

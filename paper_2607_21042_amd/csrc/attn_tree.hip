@@ -735,6 +735,24 @@ size_t ftts_tree_attention_workspace_bytes(const ftts_attn_shape* shape, int32_t
     return tree_attention_bytes(shape->n_head, n_rows);
 }
 
+int ftts_tree_attention_plan(const ftts_attn_shape* shape, int32_t B, int32_t n_rows, int32_t prefix_len, int32_t max_pages,
+                             ftts_tree_launch* out) {
+    if (!out) return set_error(FTTS_E_INVALID_ARG, "tree_attention_plan: out is NULL");
+    if (int rc = check_shape(shape, B, n_rows, prefix_len, max_pages)) return rc;
+    if (n_rows < 1) return set_error(FTTS_E_SHAPE, "tree_attention_plan: n_rows must be at least 1");
+    TreeArgs a{};
+    a.n_head = shape->n_head;
+    a.n_kv_head = shape->n_kv_head;
+    a.max_pages = max_pages;
+    a.prefix_len = prefix_len;
+    a.B = B;
+    a.rows = n_rows;
+    int waves = 4;
+    const TreePlan p = tree_plan(a, shape->dtype == FTTS_F32, waves);
+    *out = ftts_tree_launch{waves, p.parts, p.tiles, p.blocks};
+    return FTTS_OK;
+}
+
 int ftts_tree_attention(const ftts_attn_shape* shape, const void* q, int64_t q_stride, const int32_t* row_offsets,
                         int32_t n_rows, int32_t B, const int64_t* masks, int32_t mask_words,
                         const ftts_shared_prefix* prefix, const ftts_page_table* pt, const ftts_kv_pool* kv, int32_t layer,

@@ -97,6 +97,10 @@ class SharedLaunch(_c.Structure):
                 ("own_pages", i32), ("partials", i32)]
 
 
+class TreeLaunch(_c.Structure):
+    _fields_ = [("waves", i32), ("parts", i32), ("tiles", i32), ("blocks", i32)]
+
+
 class RotaryC(_c.Structure):
     _fields_ = [("dim", i32), ("layout", i32), ("scale", f32), ("turns", _c.c_double * ROTARY_MAX_PAIRS)]
 
@@ -176,6 +180,8 @@ def lib():
                                             P(KvPool), i32, vp, i64, vp, _c.c_size_t, vp]
         L.ftts_tree_attention_workspace_bytes.restype = _c.c_size_t
         L.ftts_tree_attention_workspace_bytes.argtypes = [P(AttnShape), i32, i32, i32, i32]
+        L.ftts_tree_attention_plan.restype = _c.c_int
+        L.ftts_tree_attention_plan.argtypes = [P(AttnShape), i32, i32, i32, i32, P(TreeLaunch)]
         L.ftts_tree_attention.restype = _c.c_int
         L.ftts_tree_attention.argtypes = [P(AttnShape), vp, i64, vp, i32, i32, vp, i32, P(SharedPrefixC), P(PageTable),
                                           P(KvPool), i32, vp, i64, vp, _c.c_size_t, vp]
@@ -604,6 +610,15 @@ def tree_attention_workspace_bytes(n_head: int, n_kv_head: int, dtype: int, batc
     if n == 0:
         raise FTTSError(-1, lib().ftts_last_error().decode())
     return n
+
+
+def tree_attention_plan(n_head: int, n_kv_head: int, dtype: int, batch: int, rows: int, prefix_len: int,
+                        max_pages: int) -> TreeLaunch:
+    """ftts_tree_attention_plan: how a call of those sizes is launched (host only)."""
+    out = TreeLaunch()
+    s = AttnShape(dtype, n_head, n_kv_head, 64)
+    _check(lib().ftts_tree_attention_plan(_c.byref(s), batch, rows, prefix_len, max_pages, _c.byref(out)))
+    return out
 
 
 def tree_attention(q, kv, layer: int, page_table, masks, row_offsets, out, ws, prefix=None, stream=None):
