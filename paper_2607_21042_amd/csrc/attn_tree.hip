@@ -312,8 +312,8 @@ __device__ __forceinline__ void tree_finish(const TreeArgs& a, const TreePlan& p
 // them in it would be one for the next half's loads too.
 //
 // Bound by reading where the pages are many (a half costs a wave 1,285 cycles of vector work, two waves a SIMD hide the
-// loads up to 5.1 TB/s), by one tile's chain of halves, start and hand-over (5 us) where they are few.  Captured: 32 trees of
-// 8-64 tokens behind 64-1,200 at 20 heads, 123 MB, 32.4 us; 4 of 40-64 behind 6,000-14,000, 188 MB, 46.2 and the join 4.9;
+// loads up to 5.1 TB/s), by one tile's chain of halves, start and hand-over (5 us) where they are few.  Traced: 32 trees of
+// 8-64 tokens behind 64-1,200 at 20 heads, 123 MB, 32.5 us; 4 of 40-64 behind 6,000-14,000, 188 MB, 46.4 and the join 4.9;
 // one of 16 behind 300 7.5.  A wave a row without matrix products took 1,352 us for the first and 4,113 for the second.
 // Slower or level: whole pages a step, two tiles a wave (spills), four waves a SIMD, two halves in flight, 16 waves.
 template <int W>
@@ -439,8 +439,9 @@ __global__ __launch_bounds__(W * 64, W == 4 ? 3 : 4) void tree_tile_kernel(const
     tree_finish<false, W>(a, pl, w, st, idx < pairs ? row : -1, head, smem, wave, lane);
 }
 
-// fp32: the same with fp32 matrix products, all sums in fp32.  Bound by the products: 4096 cycles a wave and half of a
-// page, whatever the rows.  4 trees of 8-32 behind 50-700 at 20 heads, 20 MB, 15.0 us and the join 3.9.
+// fp32: the same with fp32 matrix products, all sums in fp32: 4096 cycles of products (1.7 us) a wave and half page, whatever
+// the tile's rows.  4 trees of 8-32 behind 50-700 at 20 heads, 20 MB, 15.0 us and the join 4.0: a wave has one to three half
+// pages there, and products are 26% of the waves' cycles (4.9 M of 19 M); start, loads and hand-over are the rest.
 constexpr int kTfTile = kSfK * kHeadDim * 4, kTfStage = 2 * kTfTile;
 // As th_add_not_finite; v0, v1: values of the keys that element i is for, in dims lane % 32 and 32 + lane % 32.
 __device__ __forceinline__ void tf_add_not_finite(SaState& a, const float (&v0)[16], const float (&v1)[16], uint32_t seen, int hh) {
@@ -615,8 +616,8 @@ __global__ __launch_bounds__(W * 64, 2) void tree_tile_f32_kernel(const TreeArgs
 
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Tiles of 32 rows that so many sequences have at most; in one part many of them go in blocks of 8 (36 us for 32 trees of
-// 8-64 tokens behind up to 1200, 40 without the blocks; few tiles would leave a block's idle).
+// Tiles of 32 rows that so many sequences have at most; in one part many of them go in blocks of 8 (captured, 32 trees of
+// 8-64 tokens behind up to 1200: 32.6 us, 38.4 without the blocks; few tiles would leave a block's idle).
 static int64_t tree_tiles(int n_head, int n_kv_head, int rows, int B, int parts) {
     const int64_t n = (int64_t)rows * (n_head / n_kv_head) / 32 + B;
     return parts == 1 && n >= 16 ? ceil_div(n, 8) * 8 : n;

@@ -8,8 +8,8 @@
 // to place i of the tree, which is never behind the old one and never a later one's, so whole groups read in ascending
 // order and then written lose nothing.
 //
-// Captured: one sequence, 4 of 16 tokens kept in 24 layers of 20 heads, 3.9 us (2.5 without a move), 16 sequences that
-// keep 1 to 8 8.3 us: rows of 128 bytes, 17 MB.  A thousand waves that each read the tree from memory took 16 us for it.
+// Captured: one sequence, 4 of 16 tokens kept in 24 layers of 20 heads, 3.8 us (2.5 without a move), 16 sequences that
+// keep 1 to 8 8.0 us: rows of 128 bytes, 17 MB.  A thousand waves that each read the tree from memory took 16 us for it.
 #include <algorithm>
 
 #include "decode_entry.hpp"
