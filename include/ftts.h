@@ -614,7 +614,7 @@ int ftts_tree_attention(const ftts_attn_shape* shape, const void* q, int64_t q_s
 typedef struct {
     int32_t waves;  /* of a workgroup, which take its run of half pages in turn: 4 or 8 */
     int32_t parts;  /* equal runs of each sequence's pages, joined by a second launch where there are several */
-    int32_t tiles;  /* of 32 (row, query head) pairs, at most */
+    int32_t tiles;  /* of 32 (row, query head) pairs, at most, for each key head */
     int32_t blocks; /* 1: tiles in blocks of 8 that share a cache; 0: heads in turn */
 } ftts_tree_launch;
 int ftts_tree_attention_plan(const ftts_attn_shape* shape, int32_t B, int32_t n_rows, int32_t prefix_len, int32_t max_pages,
